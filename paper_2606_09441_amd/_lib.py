@@ -51,6 +51,13 @@ class SiftPlanInfo(ctypes.Structure):
                 ("scratch_bytes", ctypes.c_int64)]
 
 
+class SiftScore(ctypes.Structure):
+    _fields_ = [("softmax_scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("slopes", ctypes.c_void_p)]
+
+
+MASKS = {"causal": 0, "document": 1, "prefix": 2}
+
 _P = ctypes.c_void_p
 _SIGS = {
     "sift_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
@@ -78,6 +85,10 @@ _SIGS = {
     "sift_plan_run_paged": (ctypes.c_int, [_P, ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
                                            ctypes.POINTER(SiftTensor), _P, _P, _P, ctypes.c_float,
                                            ctypes.POINTER(SiftTensor), _P]),
+    "sift_plan_dense": (ctypes.c_int, [_P, ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
+                                       ctypes.POINTER(SiftTensor), ctypes.c_int32,
+                                       ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor), _P,
+                                       _P]),
     "sift_sparse_prefill": (ctypes.c_int, [ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
                                            ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftLayout),
                                            _P, _P, ctypes.c_int32, ctypes.POINTER(SiftTensor), _P]),
@@ -357,6 +368,36 @@ class Plan:
             _ptr(la), _ptr(ca), ctypes.c_float(0.0 if scale is None else scale), ctypes.byref(od),
             _stream_ptr(stream)))
         return out
+
+
+    def dense(self, q, k, v, mask="causal", scale=None, cap=0.0, slopes=None, out=None, lse=None,
+              stream=None):
+        """Dense attention with transformed scores (sift_plan_dense): mask "causal",
+        "document" or "prefix"; scores capped by cap * tanh(s / cap) (cap > 0) and
+        biased by -slopes[h] * distance (float32 [Hq]).  lse: float32 [tokens, Hq]
+        buffer that receives the rows' log sum exp."""
+        torch = _torch()
+        fn = "sift_plan_dense"
+        if mask not in MASKS:
+            raise SiftError(fn, 4, f"mask must be one of {sorted(MASKS)}")
+        score = score_struct(fn, scale, cap, slopes, self.info["num_q_heads"], self.device)
+        if lse is not None:
+            require(fn, lse, "lse", "float32", self.info["num_tokens"] * self.info["num_q_heads"],
+                    self.device)
+        if out is None:
+            out = torch.empty_like(q)
+        qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
+        check(fn, lib().sift_plan_dense(
+            self._h, ctypes.byref(qd), ctypes.byref(kd), ctypes.byref(vd), MASKS[mask],
+            ctypes.byref(score), ctypes.byref(od), _ptr(lse), _stream_ptr(stream)))
+        return out
+
+
+def score_struct(fn, scale, cap, slopes, num_q_heads, device) -> SiftScore:
+    """The score transform's arguments, its slopes checked."""
+    if slopes is not None:
+        require(fn, slopes, "slopes", "float32", num_q_heads, device)
+    return SiftScore(0.0 if scale is None else scale, cap, 0 if slopes is None else slopes.data_ptr())
 
 
 def sparse_prefill(q, k, v, seg_offsets, prompt_seg_ptr, la, ca, tile=64, out=None, stream=None):

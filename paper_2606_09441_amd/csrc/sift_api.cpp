@@ -17,6 +17,7 @@
 #include <numeric>
 #include <vector>
 
+#include "score_api.h"
 #include "sift.h"
 #include "sift_internal.h"
 
@@ -47,6 +48,8 @@ struct sift_plan {
   unsigned long long decode_capture = 0;  // the graph capture it was part of (0: none, or
                                           // sift_plan_run's, whose attention follows it)
   bool unsorted = false;       // bf16 calls leave the schedule pass out (kFewChunked)
+  const int4* dense[3] = {};   // per sift_mask: the dense attention's records, num_dense each
+  int32_t num_dense = 0;       // (sift_plan_create's plans alone)
   hipStream_t last_stream = nullptr;  // the stream of the plan's last enqueued work
 };
 
@@ -607,6 +610,8 @@ struct PlanImage {
   size_t seg_tile0, seg_pages, seg_kind, seg_first, seg_la, seg_ca;
   size_t tile_seg, tile_tok0, tile_len, tile_lo, tile_info;
   size_t urec, rec, launch, splits, hist;
+  std::vector<int4> dense_recs;  // per sift_mask (make_dense)
+  size_t dense;
   size_t upload;  // bytes of the tables
   // of the scratch
   size_t counts, segbase, headtot, camark, segcross, crosscol, crossrows, rowptr, col, steps, kvb;
@@ -618,8 +623,36 @@ struct PlanImage {
 // the decode's finished-block count: zeros, uploaded with the tables
 constexpr size_t kHistWords = sift::kNumXcd * sift::kSchedBuckets + 4 + sift::kNumXcd;
 
+// Records of the dense attention: under each mask 128 rows of a segment at a
+// time, those of most keys first.
+std::vector<int4> make_dense(const sift_layout& lay) {
+  std::vector<int4> all;
+  for (int32_t mask = SIFT_MASK_CAUSAL; mask <= SIFT_MASK_PREFIX; ++mask) {
+    std::vector<int4> recs;
+    for (int32_t b = 0; b < lay.num_prompts; ++b) {
+      const int32_t s0 = lay.prompt_seg_ptr[b], query = lay.prompt_seg_ptr[b + 1] - 1;
+      for (int32_t s = s0; s <= query; ++s) {
+        const int32_t a = lay.seg_offsets[s], z = lay.seg_offsets[s + 1];
+        const bool alone = mask == SIFT_MASK_DOCUMENT && s < query;
+        const bool prefix = mask == SIFT_MASK_PREFIX && s < query;
+        for (int32_t r = a, n; r < z; r += n) {
+          n = std::min(z - r, sift::kDenseRows);
+          recs.push_back(int4{r, n, alone ? a : lay.seg_offsets[s0],
+                              prefix ? lay.seg_offsets[query] : r});
+        }
+      }
+    }
+    const auto keys = [](const int4& x) { return std::max(x.x + x.y, x.w) - x.z; };
+    std::stable_sort(recs.begin(), recs.end(),
+                     [&](const int4& x, const int4& y) { return keys(x) > keys(y); });
+    all.insert(all.end(), recs.begin(), recs.end());
+  }
+  return all;
+}
+
+// dense: with the dense attention's records.
 sift_status make_image(const sift_layout* layout, int32_t num_q_heads, int32_t num_kv_heads,
-                       int32_t head_dim, int32_t tile, PlanImage& im) {
+                       int32_t head_dim, int32_t tile, PlanImage& im, bool dense = false) {
   if (layout == nullptr) return SIFT_E_NULL;
   if (num_q_heads < 1 || num_kv_heads < 1 || num_q_heads % num_kv_heads != 0) return SIFT_E_SHAPE;
   if (head_dim != 64 && head_dim != 128) return SIFT_E_UNSUPPORTED;
@@ -657,6 +690,8 @@ sift_status make_image(const sift_layout* layout, int32_t num_q_heads, int32_t n
   im.launch = place((hp.scheduled ? slots : 0) * sizeof(sift::WorkRec));  // by the schedule pass
   im.splits = place(hp.num_splits * 4 * sizeof(int32_t));
   im.hist = place(kHistWords * sizeof(int32_t));
+  if (dense) im.dense_recs = make_dense(*layout);
+  im.dense = place(im.dense_recs.size() * sizeof(int4));
   im.upload = at;
   const int64_t rows = static_cast<int64_t>(hp.num_tiles) * num_q_heads;
   const int64_t segs = static_cast<int64_t>(hp.num_segments) * num_q_heads;
@@ -716,6 +751,8 @@ void write_tables(const PlanImage& im, uint8_t* out) {
     std::fill_n(reinterpret_cast<sift::WorkRec*>(out + im.launch), slots, empty);
   write_splits(hp, reinterpret_cast<int32_t*>(out + im.splits));
   std::memset(out + im.hist, 0, kHistWords * sizeof(int32_t));
+  if (!im.dense_recs.empty())
+    std::memcpy(out + im.dense, im.dense_recs.data(), im.dense_recs.size() * sizeof(int4));
 }
 
 // The plan of an image.  Its device memory: with ws == nullptr a hipMalloc of
@@ -820,6 +857,9 @@ sift_status create_plan(const PlanImage& im, void* ws, size_t ws_bytes, hipStrea
   if (hp.chunked && !hp.scheduled) run_in_place(plan->wt);
   plan->unsorted = im.hkv == sift::kNumXcd && hp.scheduled &&
                    hp.num_work <= sift::kFewChunked && im.tile >= 64 && im.head_dim == 128;
+  plan->num_dense = static_cast<int32_t>(im.dense_recs.size() / 3);
+  for (int m = 0; m < 3; ++m)
+    plan->dense[m] = reinterpret_cast<const int4*>(P(im.dense)) + int64_t(m) * plan->num_dense;
   plan->counts = P(im.counts);
   plan->row_ptr = P(im.rowptr);
   plan->col_idx = P(im.col);
@@ -898,7 +938,7 @@ sift_status sift_plan_create(const sift_layout* layout, int32_t num_q_heads,
   if (plan_out == nullptr) return SIFT_E_NULL;
   *plan_out = nullptr;
   PlanImage im;
-  const sift_status st = make_image(layout, num_q_heads, num_kv_heads, head_dim, tile, im);
+  const sift_status st = make_image(layout, num_q_heads, num_kv_heads, head_dim, tile, im, true);
   if (st != SIFT_OK) return st;
   return create_plan(im, nullptr, 0, nullptr, Upload::kBlocking, plan_out);
 }
@@ -1160,6 +1200,42 @@ sift_status sift_plan_run_paged(sift_plan* plan, const sift_tensor* q, const sif
   a.pages = pages;
   e = q->dtype == SIFT_BF16 ? sift::launch_attn_bf16(plan->pt, wt, a, s)
                             : sift::launch_attn_f32(plan->pt, &wt, a, s);
+  plan->last_stream = s;
+  return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
+}
+
+sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_tensor* k,
+                            const sift_tensor* v, int32_t mask, const sift_score* score,
+                            sift_tensor* out, float* lse, void* stream) {
+  if (plan == nullptr) return SIFT_E_NULL;
+  const sift_plan_info& in = plan->info;
+  sift_status st;
+  if ((st = check_tensor(q, in.num_tokens, in.num_q_heads, in.head_dim)) != SIFT_OK) return st;
+  if ((st = check_tensor(k, in.num_tokens, in.num_kv_heads, in.head_dim)) != SIFT_OK) return st;
+  if ((st = check_tensor(v, in.num_tokens, in.num_kv_heads, in.head_dim)) != SIFT_OK) return st;
+  if ((st = check_tensor(out, in.num_tokens, in.num_q_heads, in.head_dim)) != SIFT_OK) return st;
+  if (q->dtype != k->dtype || q->dtype != v->dtype || q->dtype != out->dtype)
+    return SIFT_E_UNSUPPORTED;
+  for (const void* p : {q->data, k->data, v->data, out->data})
+    if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return SIFT_E_UNSUPPORTED;
+  if (mask < SIFT_MASK_CAUSAL || mask > SIFT_MASK_PREFIX) return SIFT_E_UNSUPPORTED;
+  sift::DenseArgs a{};
+  if ((st = sift::make_score(score, in.head_dim, &a.sc)) != SIFT_OK) return st;
+  if ((st = check_device(plan)) != SIFT_OK) return st;
+  // a grid holds fewer than 2^32 threads
+  if (sift::dense_grid(plan->num_dense, in.num_q_heads, in.num_kv_heads) >= int64_t(1) << 24)
+    return SIFT_E_CAPACITY;
+  a.q = q->data;
+  a.k = k->data;
+  a.v = v->data;
+  a.out = out->data;
+  a.lse = lse;
+  a.recs = plan->dense[mask];
+  a.num_recs = plan->num_dense;
+  a.hq = in.num_q_heads;
+  a.hkv = in.num_kv_heads;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = sift::launch_attn_dense(a, q->dtype == SIFT_BF16, in.head_dim, s);
   plan->last_stream = s;
   return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
 }

@@ -385,4 +385,42 @@ hipError_t launch_rms_norm(const void* x, const void* weight, int64_t rows, int 
 hipError_t launch_silu_mul(const void* gate, const void* up, int64_t count, void* out,
                            hipStream_t stream);
 
+// Scores of the dense and the cache attention: z = scale * q.k, then
+// cap * tanh(z / cap) where cap > 0, then - slope[head] * |distance|; all in
+// the log2 domain, t = s * log2(e).
+struct ScoreArgs {
+  float c;        // scale * log2(e)
+  float x;        // scale / cap: x z0 is the tanh's argument (z0 = q.k); 0: no cap
+  float cap2;     // cap * log2(e)
+  float a[5];     // t = z0 * poly(z0^2) where |x z0| <= kTanhSmall
+  const float* slopes;  // [Hq] or nullptr
+};
+
+// tanh(y) / y over |y| <= kTanhSmall as a polynomial in y^2 of degree 4:
+// minimax fit of the relative error (1.4e-8), made by reweighted least squares.
+constexpr float kTanhSmall = 0.5f;
+constexpr double kTanhPoly[5] = {0.9999999869, -0.3333306939, 0.1332477931, -0.05298607504,
+                                 0.01713500614};
+
+// Dense attention (attn_dense.hip).  A record: 128 query rows of a segment,
+// {first row, rows, first key, upto}: row i sees the keys j from the first on
+// with j < upto or j <= i.
+constexpr int kDenseRows = 128;
+
+struct DenseArgs {
+  const void* q;        // [tokens][hq][D]
+  const void* k;        // [tokens][hkv][D]
+  const void* v;
+  void* out;            // [tokens][hq][D]
+  float* lse;           // [tokens][hq] or nullptr
+  const int4* recs;     // longest first
+  int32_t num_recs;
+  int32_t hq, hkv;
+  ScoreArgs sc;
+};
+
+// Workgroups of a launch.
+int64_t dense_grid(int32_t num_recs, int32_t hq, int32_t hkv);
+hipError_t launch_attn_dense(const DenseArgs& a, bool bf16, int head_dim, hipStream_t stream);
+
 }  // namespace sift

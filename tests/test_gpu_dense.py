@@ -1,0 +1,191 @@
+"""GPU tests of the dense attention with transformed scores (sift_plan_dense)
+against the fp64 oracle, element by element."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from gpu_helpers import device, max_abs, say
+from oracle import serve_oracle as S
+
+pytestmark = pytest.mark.gpu
+
+# Inputs are N(0, 1) with a few keys four times as long.  Outputs: the project's
+# bars.  The log sum: a score is a sum of up to 128 products in fp32 (error at
+# most 128 * 2^-24 * sum|q k| * scale, about 1e-4 at |s| ~ 16 and 1e-5 in
+# practice); the hardware's exp2 and the polynomial add a few 2^-24 of it.
+TOL = {"f32": 1e-5, "bf16": 2e-2}
+LSE_TOL = 1e-4
+
+LAYOUTS = {
+    # prompts as lists of segment lengths, the query last
+    "one_token": [[1, 0]],
+    "edges": [[64, 63, 65, 1, 33], [1, 128, 1], [127, 129, 32, 0]],
+    "long": [[200, 300, 77]],
+    "query_only": [[130], [1]],
+}
+
+
+def layout(prompts):
+    so, ps = [0], [0]
+    for p in prompts:
+        for n in p:
+            so.append(so[-1] + n)
+        ps.append(len(so) - 1)
+    return so, ps
+
+
+def inputs(n, hq, hkv, d, dtype, seed=0):
+    import torch
+    rng = np.random.default_rng(seed)
+    q = rng.standard_normal((n, hq, d)).astype(np.float32)
+    k = rng.standard_normal((n, hkv, d)).astype(np.float32)
+    k *= np.where(rng.random((n, hkv, 1)) < 0.05, 4.0, 1.0).astype(np.float32)
+    v = rng.standard_normal((n, hkv, d)).astype(np.float32)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    dev = [torch.from_numpy(x).to(device()).to(dt) for x in (q, k, v)]
+    return dev, [x.float().cpu().numpy() for x in dev]
+
+
+def run(prompts, hq, hkv, d, dtype, mask, cap=0.0, bias=False, scale=None, seed=0, poison=None,
+        tile=64):
+    """(out, lse) of the library and of the oracle."""
+    import torch
+    from paper_2606_09441_amd import Plan
+    so, ps = layout(prompts)
+    n = so[-1]
+    (q, k, v), (qn, kn, vn) = inputs(n, hq, hkv, d, dtype, seed)
+    if poison is not None:
+        poison(k, v)
+        kn, vn = k.float().cpu().numpy(), v.float().cpu().numpy()
+    slopes = (2.0 ** (-4.0 * np.arange(1, hq + 1) / hq)).astype(np.float32) if bias else None
+    lse = torch.full((n, hq), 7.0, device=q.device)
+    with Plan(so, ps, hq, hkv, d, tile) as plan:
+        out = plan.dense(q, k, v, mask=mask, scale=scale, cap=cap, lse=lse,
+                         slopes=None if slopes is None else torch.from_numpy(slopes).to(q.device))
+        torch.cuda.synchronize()
+    want = S.dense(qn, kn, vn, so, ps, mask, scale, cap, slopes)
+    return out.float().cpu().numpy(), lse.cpu().numpy(), *want
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("mask", ["causal", "document", "prefix"])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (2.0, False), (50.0, False), (0.0, True),
+                                      (20.0, True)])
+def test_masks_and_scores(dtype, d, mask, cap, bias):
+    for name, prompts in LAYOUTS.items():
+        out, lse, ref, ref_lse = run(prompts, 6, 2, d, dtype, mask, cap, bias)
+        e, el = max_abs(out, ref), max_abs(lse, ref_lse)
+        say(f"{name} {dtype} {d} {mask} cap {cap} bias {bias}: {e:.2e}, lse {el:.2e}")
+        assert e <= TOL[dtype] and el <= LSE_TOL
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 5), (6, 3), (16, 16), (12, 4)])
+def test_head_layouts(hq, hkv):
+    """Every assignment of records and heads to workgroups."""
+    for dtype in ("bf16", "f32"):
+        out, lse, ref, ref_lse = run([[130, 70, 40], [20, 5]], hq, hkv, 64, dtype, "causal")
+        assert max_abs(out, ref) <= TOL[dtype] and max_abs(lse, ref_lse) <= LSE_TOL
+
+
+def test_scale():
+    out, lse, ref, ref_lse = run([[100, 30]], 2, 1, 128, "bf16", "causal", scale=0.03)
+    assert max_abs(out, ref) <= TOL["bf16"] and max_abs(lse, ref_lse) <= LSE_TOL
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_unseen_keys_do_not_matter(dtype, value):
+    """A key with such values only reaches the rows that see it: under the causal
+    mask the rows from it on, and no other prompt's."""
+    import torch
+    from paper_2606_09441_amd import Plan
+    so, ps = layout([[90, 60], [40, 10]])
+    n, bad = so[-1], 70
+    (q, k, v), (qn, kn, vn) = inputs(n, 2, 1, 128, dtype)
+    k[bad], v[bad] = value, value
+    v[bad, :, 3:] = 0.5         # the other dims of a visible key stay as they are ...
+    k[bad] = 0.25               # ... where its scores are finite
+    kn, vn = k.float().cpu().numpy(), v.float().cpu().numpy()
+    with Plan(so, ps, 2, 1, 128, 64) as plan:
+        out = plan.dense(q, k, v).float().cpu().numpy()
+        k[bad] = value          # and a score that is none
+        worse = plan.dense(q, k, v).float().cpu().numpy()
+    rows = np.r_[0:bad, 150:n]
+    with np.errstate(all="ignore"):
+        ref, _ = S.dense(qn, kn, vn, so, ps, "causal")
+    assert max_abs(out[rows], ref[rows]) <= TOL[dtype]
+    assert max_abs(worse[rows], ref[rows]) <= TOL[dtype]
+    assert max_abs(out[bad:150, :, 3:], ref[bad:150, :, 3:]) <= TOL[dtype]
+    got, want = out[bad:150, :, :3], ref[bad:150, :, :3]
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(got[~np.isnan(got)], want[~np.isnan(want)])
+
+
+def test_same_as_sparse_path():
+    """All-ones bits make the sparse attention dense causal: the two agree, on a
+    plan that has run both in turn."""
+    import torch
+    import workloads as W
+    from gpu_helpers import DevWorkload
+    wl = W.all_ones(W.custom([[200, 64, 70], [96, 33]], tile=64, hq=4, hkv=2, d=128, dtype="bf16",
+                             seed=1))
+    dw = DevWorkload(wl)
+    a = dw.run().clone()
+    b = dw.plan.dense(dw.q, dw.k, dw.v)
+    c = dw.run()
+    torch.cuda.synchronize()
+    dw.close()
+    assert torch.equal(a, c)
+    assert max_abs(a.float().cpu(), b.float().cpu()) <= TOL["bf16"]
+
+
+def test_streams_and_repeats():
+    """The same bits on another stream, in a captured graph and on its replays."""
+    import torch
+    from paper_2606_09441_amd import Plan
+    so, ps = layout([[150, 60], [33, 0]])
+    (q, k, v), _ = inputs(so[-1], 4, 2, 128, "bf16")
+    with Plan(so, ps, 4, 2, 128, 64) as plan:
+        first = plan.dense(q, k, v, mask="prefix", cap=30.0)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        out = torch.zeros_like(q)
+        with torch.cuda.stream(side):
+            plan.dense(q, k, v, mask="prefix", cap=30.0, out=out)
+        side.synchronize()
+        assert torch.equal(out, first)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            plan.dense(q, k, v, mask="prefix", cap=30.0, out=out)
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, first)
+
+
+def test_refusals():
+    import torch
+    from paper_2606_09441_amd import Plan, SiftError
+    so, ps = layout([[100, 30]])
+    (q, k, v), _ = inputs(130, 4, 2, 128, "bf16")
+    with Plan(so, ps, 4, 2, 128, 64) as plan:
+        def refused(status, *a, **kw):
+            with pytest.raises(SiftError) as e:
+                plan.dense(*a, **kw)
+            assert e.value.status == status
+        refused(4, q, k, v, mask="sideways")
+        refused(4, q, k, v, cap=-1.0)
+        refused(4, q, k, v, cap=float("nan"))
+        refused(4, q, k, v, cap=float("inf"))
+        refused(2, q[:-1], k, v)
+        refused(2, q, k[:, :1].contiguous(), v)
+        refused(4, q, k.float(), v)
+        refused(4, q, k, v, out=q.float())
+        refused(5, q, k, v, slopes=torch.zeros(3, device=q.device))
+        refused(4, q, k, v, slopes=torch.zeros(4))
+        refused(5, q, k, v, lse=torch.zeros(130, 3, device=q.device))
+        odd = torch.empty(q.numel() + 1, dtype=q.dtype, device=q.device)[1:].view_as(q)
+        refused(4, odd, k, v)
