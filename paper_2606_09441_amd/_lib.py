@@ -14,6 +14,7 @@ import numpy as np
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsift.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "sift.h")
+SERVE_HEADER = os.path.join(os.path.dirname(HERE), "include", "sift_serve.h")
 
 SIFT_F32 = 0
 SIFT_BF16 = 1
@@ -85,10 +86,6 @@ _SIGS = {
     "sift_plan_run_paged": (ctypes.c_int, [_P, ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
                                            ctypes.POINTER(SiftTensor), _P, _P, _P, ctypes.c_float,
                                            ctypes.POINTER(SiftTensor), _P]),
-    "sift_plan_dense": (ctypes.c_int, [_P, ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
-                                       ctypes.POINTER(SiftTensor), ctypes.c_int32,
-                                       ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor), _P,
-                                       _P]),
     "sift_sparse_prefill": (ctypes.c_int, [ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
                                            ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftLayout),
                                            _P, _P, ctypes.c_int32, ctypes.POINTER(SiftTensor), _P]),
@@ -116,6 +113,14 @@ _SIGS = {
                                          ctypes.c_size_t, _P]),
 }
 
+# include/sift_serve.h
+_SERVE_SIGS = {
+    "sift_plan_dense": (ctypes.c_int, [_P, ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
+                                       ctypes.POINTER(SiftTensor), ctypes.c_int32,
+                                       ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor), _P,
+                                       _P]),
+}
+
 # entries of the decoder layer (csrc/layer_api.h), not part of sift.h
 _LAYER_SIGS = {
     "sift_layer_rms_norm": (ctypes.c_int, [_P, _P, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, _P,
@@ -126,9 +131,9 @@ _LAYER_SIGS = {
 _lib = None
 
 
-def header_functions() -> list[str]:
-    """Names of the functions include/sift.h declares."""
-    with open(HEADER) as f:
+def header_functions(header: str = HEADER) -> list[str]:
+    """Names of the functions include/sift.h (or another header) declares."""
+    with open(header) as f:
         text = f.read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     return sorted(set(re.findall(r"\b(sift_[a-z_]+)\s*\(", text)))
@@ -143,7 +148,7 @@ def lib() -> ctypes.CDLL:
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2606_09441_amd.build` (no fallback exists)")
         L = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in (*_SIGS.items(), *_LAYER_SIGS.items()):
+        for name, (res, args) in (*_SIGS.items(), *_SERVE_SIGS.items(), *_LAYER_SIGS.items()):
             fn = getattr(L, name)
             fn.restype = res
             fn.argtypes = args

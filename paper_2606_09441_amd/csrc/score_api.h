@@ -4,8 +4,8 @@
 
 #include <cmath>
 
-#include "sift.h"
 #include "sift_internal.h"
+#include "sift_serve.h"
 
 namespace sift {
 

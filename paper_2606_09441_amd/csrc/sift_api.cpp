@@ -20,6 +20,7 @@
 #include "score_api.h"
 #include "sift.h"
 #include "sift_internal.h"
+#include "sift_serve.h"
 
 namespace {
 
