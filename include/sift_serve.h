@@ -64,6 +64,87 @@ sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_te
                             const sift_tensor* v, int32_t mask, const sift_score* score,
                             sift_tensor* out, float* lse, void* stream);
 
+/*
+ * The paged cache of a batch of sequences, of one layer.
+ *
+ * Slots: sequence b owns max_pages pages of `page` slots.  Slot i is row
+ *   i % page of pool page page_table[b][i / page] (the pools of
+ *   sift_plan_run_paged, whose T is the page here); it holds a key where
+ *   i < lens[b] and, where page_lens are given, i % page <
+ *   page_lens[b][i / page] (a document's last page may end early).  Pages may
+ *   be shared by sequences; the order of the slots means nothing but the
+ *   positions: key_pos[b][kv head][i], or i itself where none are given.
+ * Tables are device memory, read when the work runs, so that a captured graph
+ *   serves growing caches.  Values outside their range are clamped: no access
+ *   leaves the given buffers, and the result for such sequences is meaningless.
+ */
+typedef struct sift_cache_kv {
+  const sift_tensor* k_pages;  /* [num_pages * page][Hkv][D]                     */
+  const sift_tensor* v_pages;
+  const int32_t* page_table;   /* [num_seqs][max_pages]                          */
+  const int32_t* lens;         /* [num_seqs], 0 .. max_pages * page              */
+  const int32_t* page_lens;    /* [num_seqs][max_pages], or NULL: full pages     */
+  const int32_t* key_pos;      /* [num_seqs][Hkv][max_pages * page], or NULL     */
+} sift_cache_kv;
+
+/* The new tokens of the sequences, rows row_ptr[b] .. row_ptr[b+1]-1 (at most
+ * max_rows) of q for sequence b. */
+typedef struct sift_cache_rows {
+  const int32_t* row_ptr;      /* device [num_seqs + 1], or NULL: as many of each */
+  const int32_t* row_pos;      /* device [rows]: positions, or NULL: lens[b] and
+                                  on, in order                                   */
+} sift_cache_rows;
+
+/* Opaque: the sizes of a batch's caches, and device scratch. */
+typedef struct sift_cache sift_cache;
+
+/*
+ * Make a handle for caches of these sizes.  Allocates device memory on the
+ * current device (scratch for partial results and for the eviction); the
+ * calls below allocate nothing.  Calls on one handle must be ordered.
+ *   num_seqs, num_q_heads, num_kv_heads >= 1, Hq % Hkv == 0
+ *   head_dim   D: 64 or 128;  page: 16, 32, 64 or 128
+ *   max_pages  pages of a sequence at most, >= 1
+ *   max_rows   new tokens of a sequence in one call at most, >= 1
+ * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (D, page),
+ *   SIFT_E_CAPACITY (slots or rows x heads beyond 2^31 - 256), SIFT_E_HIP.
+ */
+sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                              int32_t head_dim, int32_t page, int32_t max_pages,
+                              int32_t max_rows, sift_cache** cache_out);
+
+/* Free a handle and its scratch (waits first for the stream of its last
+ * enqueued work).  NULL is accepted. */
+sift_status sift_cache_destroy(sift_cache* cache);
+
+/*
+ * Attention of the new tokens over the cache and over each other: a single
+ * token, a chain or a drafted tree for each sequence, in one call.
+ *   q, out       [rows][Hq][D];  k_new, v_new: [rows][Hkv][D], the new tokens'
+ *                own keys, which the cache does not hold yet.  All tensors and
+ *                the pools SIFT_BF16 or all SIFT_F32, 16-byte aligned.
+ *   tree_mask    device uint64 [rows][mask_words], mask_words >=
+ *                ceil(max_rows / 64): bit j % 64 of word j / 64 says whether the
+ *                row sees new token j of its sequence (its ancestors and
+ *                itself); every key of the cache is visible to every row.
+ *                NULL: a chain, each row sees those up to itself.
+ *   score        see sift_score
+ *   lse          device float [rows][Hq], or NULL: the rows' log sum exp
+ * A row that sees no key gets 0, and -infinity for its log sum; so does one
+ * whose every visible score is -infinity.  Keys that a row does not see have no
+ * influence on it.  Rows that row_ptr leaves out are not written.  Results
+ * depend on nothing but the arguments (no atomics).
+ * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, alignment,
+ *   cap), SIFT_E_CAPACITY (mask_words; rows x heads beyond 2^26), SIFT_E_PLAN
+ *   (another device is current), SIFT_E_HIP.
+ */
+sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
+                                 const sift_cache_rows* new_rows, const sift_tensor* q,
+                                 const sift_tensor* k_new, const sift_tensor* v_new,
+                                 const uint64_t* tree_mask, int32_t mask_words,
+                                 const sift_score* score, sift_tensor* out, float* lse,
+                                 void* stream);
+
 #ifdef __cplusplus
 }
 #endif

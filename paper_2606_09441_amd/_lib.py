@@ -57,6 +57,16 @@ class SiftScore(ctypes.Structure):
                 ("slopes", ctypes.c_void_p)]
 
 
+class SiftCacheKv(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.POINTER(SiftTensor)), ("v_pages", ctypes.POINTER(SiftTensor)),
+                ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
+                ("page_lens", ctypes.c_void_p), ("key_pos", ctypes.c_void_p)]
+
+
+class SiftCacheRows(ctypes.Structure):
+    _fields_ = [("row_ptr", ctypes.c_void_p), ("row_pos", ctypes.c_void_p)]
+
+
 MASKS = {"causal": 0, "document": 1, "prefix": 2}
 
 _P = ctypes.c_void_p
@@ -192,10 +202,11 @@ def tensor_desc(t) -> SiftTensor:
 def require(fn: str, t, name: str, dtype: str, min_numel: int, device=None) -> None:
     """Check a device buffer before its pointer goes to the library, which
     cannot see buffer sizes: a GPU tensor (on `device` when given), of
-    `dtype` ("uint8", "int32", "float32"), contiguous, with at least
+    `dtype` ("uint8", "int32", "int64", "float32"), contiguous, with at least
     min_numel elements.  Raises SiftError otherwise."""
     torch = _torch()
-    want = {"uint8": torch.uint8, "int32": torch.int32, "float32": torch.float32}[dtype]
+    want = {"uint8": torch.uint8, "int32": torch.int32, "int64": torch.int64,
+            "float32": torch.float32}[dtype]
     if t is None:
         if min_numel > 0:
             raise SiftError(fn, 1, f"{name} is required")
@@ -628,3 +639,112 @@ def silu_mul(gate, up, stream=None):
 
 def default_scale(head_dim: int) -> float:
     return 1.0 / math.sqrt(head_dim)
+
+
+class CachePages:
+    """The page pools and tables of a batch's caches (sift_cache_kv): k_pages and
+    v_pages [num_pages * page, Hkv, D], page_table int32 [seqs, max_pages], lens
+    int32 [seqs]; page_lens int32 [seqs, max_pages] where pages end early, key_pos
+    int32 [seqs, Hkv, max_pages * page] where a key's position is not its slot.
+    The tensors are used where they are: write into them, or make another."""
+
+    def __init__(self, k_pages, v_pages, page_table, lens, page_lens=None, key_pos=None):
+        fn = "CachePages"
+        kd, vd = tensor_desc(k_pages), tensor_desc(v_pages)
+        dev = k_pages.device
+        for name, t in (("page_table", page_table), ("lens", lens), ("page_lens", page_lens),
+                        ("key_pos", key_pos)):
+            if t is not None or name in ("page_table", "lens"):
+                require(fn, t, name, "int32", 1, dev)
+        if v_pages.device != dev:
+            raise SiftError(fn, 7, f"v_pages is on {v_pages.device}, k_pages on {dev}")
+        self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
+        self.page_lens, self.key_pos = page_lens, key_pos
+        self._kd, self._vd = kd, vd
+        self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
+                                  lens.data_ptr(), 0 if page_lens is None else page_lens.data_ptr(),
+                                  0 if key_pos is None else key_pos.data_ptr())
+
+
+class Cache:
+    """A handle for the paged caches of a batch (sift_cache_*): sizes and scratch."""
+
+    def __init__(self, num_seqs, num_q_heads, num_kv_heads, head_dim, page=64, max_pages=1,
+                 max_rows=1):
+        self._h = None
+        h = ctypes.c_void_p()
+        check("sift_cache_create", lib().sift_cache_create(
+            num_seqs, num_q_heads, num_kv_heads, head_dim, page, max_pages, max_rows,
+            ctypes.byref(h)))
+        self._h = h
+        torch = _torch()
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.num_seqs, self.hq, self.hkv, self.d = num_seqs, num_q_heads, num_kv_heads, head_dim
+        self.page, self.max_pages, self.max_rows = page, max_pages, max_rows
+        self.slots = max_pages * page
+
+    def close(self):
+        if self._h is not None:
+            check("sift_cache_destroy", lib().sift_cache_destroy(self._h))
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _kv(self, fn, kv):
+        """The tables' sizes, which the library cannot see."""
+        pages = self.num_seqs * self.max_pages
+        if kv.k_pages.device != self.device:
+            raise SiftError(fn, 7, f"the pages are on {kv.k_pages.device}, the cache on {self.device}")
+        for name, t, n in (("page_table", kv.page_table, pages), ("lens", kv.lens, self.num_seqs),
+                           ("page_lens", kv.page_lens, pages),
+                           ("key_pos", kv.key_pos, self.num_seqs * self.hkv * self.slots)):
+            if t is not None and t.numel() < n:
+                raise SiftError(fn, 5, f"{name} holds {t.numel()} elements, needs {n}")
+        return ctypes.byref(kv.struct)
+
+    def _rows(self, fn, q, row_ptr, row_pos):
+        if row_ptr is not None:
+            require(fn, row_ptr, "row_ptr", "int32", self.num_seqs + 1, self.device)
+        if row_pos is not None:
+            require(fn, row_pos, "row_pos", "int32", q.shape[0], self.device)
+        return SiftCacheRows(0 if row_ptr is None else row_ptr.data_ptr(),
+                             0 if row_pos is None else row_pos.data_ptr())
+
+    def attention(self, q, k_new, v_new, kv, row_ptr=None, tree_mask=None, row_pos=None, scale=None,
+                  cap=0.0, slopes=None, out=None, lse=None, stream=None):
+        """Attention of new tokens over the cache and each other
+        (sift_cache_attention): q [rows, Hq, D], k_new and v_new [rows, Hkv, D], kv a
+        CachePages.  row_ptr int32 [seqs + 1] delimits the sequences' rows (None: as
+        many of each); tree_mask int64 [rows, words] holds each row's visible new
+        tokens as bits (None: those up to itself); row_pos int32 [rows].  lse: float32
+        [rows, Hq] buffer that receives the rows' log sum exp."""
+        torch = _torch()
+        fn = "sift_cache_attention"
+        rows = self._rows(fn, q, row_ptr, row_pos)
+        words = 0
+        if tree_mask is not None:
+            words = (self.max_rows + 63) // 64
+            if tree_mask.dim() == 2:
+                words = max(words, tree_mask.shape[1])
+            require(fn, tree_mask, "tree_mask", "int64", q.shape[0] * words, self.device)
+        score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
+        if lse is not None:
+            require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
+        if out is None:
+            out = torch.empty_like(q)
+        qd, kd, vd, od = tensor_desc(q), tensor_desc(k_new), tensor_desc(v_new), tensor_desc(out)
+        check(fn, lib().sift_cache_attention(
+            self._h, self._kv(fn, kv), ctypes.byref(rows), ctypes.byref(qd), ctypes.byref(kd),
+            ctypes.byref(vd), _ptr(tree_mask), words, ctypes.byref(score), ctypes.byref(od),
+            _ptr(lse), _stream_ptr(stream)))
+        return out

@@ -1,0 +1,192 @@
+// C ABI of the page cache (include/sift_serve.h): the handle with its scratch,
+// and the host checks of its calls.  The kernels are in cache_attn.hip.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <initializer_list>
+#include <limits>
+#include <new>
+
+#include "score_api.h"
+#include "sift.h"
+#include "sift_internal.h"
+#include "sift_serve.h"
+
+struct sift_cache {
+  int device = 0;
+  int32_t num_seqs = 0, hq = 0, hkv = 0, head_dim = 0, page = 0, max_pages = 0, max_rows = 0;
+  int32_t cus = 0;           // compute units of the device
+  void* dev = nullptr;
+  float* part_o = nullptr;
+  float4* part_ml = nullptr;
+  hipStream_t last_stream = nullptr;  // the stream of the last enqueued work
+};
+
+namespace {
+
+constexpr int64_t kMost = std::numeric_limits<int32_t>::max() - 255;
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+int32_t log2_of(int32_t x) {
+  int32_t s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+
+sift_status check_tensor(const sift_tensor* t, int32_t tokens, int32_t heads, int32_t dim,
+                         int32_t dtype) {
+  if (t == nullptr) return SIFT_E_NULL;
+  if (t->data == nullptr && static_cast<int64_t>(t->tokens) * t->heads * t->head_dim > 0)
+    return SIFT_E_NULL;
+  if (t->dtype != SIFT_F32 && t->dtype != SIFT_BF16) return SIFT_E_UNSUPPORTED;
+  if (t->tokens != tokens || t->heads != heads || t->head_dim != dim) return SIFT_E_SHAPE;
+  if (t->dtype != dtype || !aligned16(t->data)) return SIFT_E_UNSUPPORTED;
+  return SIFT_OK;
+}
+
+// The cache's own arguments; a's device-side view of them.
+sift_status check_kv(const sift_cache* c, const sift_cache_kv* kv, sift::CacheArgs* a) {
+  if (c == nullptr || kv == nullptr || kv->k_pages == nullptr || kv->v_pages == nullptr)
+    return SIFT_E_NULL;
+  const int32_t rows = kv->k_pages->tokens, dtype = kv->k_pages->dtype;
+  if (rows < c->page || rows % c->page != 0) return SIFT_E_SHAPE;
+  sift_status st;
+  if ((st = check_tensor(kv->k_pages, rows, c->hkv, c->head_dim, dtype)) != SIFT_OK) return st;
+  if ((st = check_tensor(kv->v_pages, rows, c->hkv, c->head_dim, dtype)) != SIFT_OK) return st;
+  if (kv->page_table == nullptr || kv->lens == nullptr) return SIFT_E_NULL;
+  if (!aligned16(kv->key_pos)) return SIFT_E_UNSUPPORTED;
+  int dev = -1;
+  if (hipGetDevice(&dev) != hipSuccess) return SIFT_E_HIP;
+  if (dev != c->device) return SIFT_E_PLAN;
+  a->k = kv->k_pages->data;
+  a->v = kv->v_pages->data;
+  a->table = kv->page_table;
+  a->lens = kv->lens;
+  a->page_lens = kv->page_lens;
+  a->key_pos = kv->key_pos;
+  a->num_seqs = c->num_seqs;
+  a->max_pages = c->max_pages;
+  a->page_shift = log2_of(c->page);
+  a->num_pages = rows / c->page;
+  a->hq = c->hq;
+  a->hkv = c->hkv;
+  return SIFT_OK;
+}
+
+// The new tokens; dtype: the pools'.
+sift_status check_rows(const sift_cache* c, const sift_cache_rows* r, const sift_tensor* q,
+                       int32_t dtype, const sift_score* score, sift::CacheArgs* a) {
+  if (q == nullptr) return SIFT_E_NULL;
+  const int32_t rows = q->tokens;
+  if (rows < 0) return SIFT_E_SHAPE;
+  sift_status st;
+  if ((st = check_tensor(q, rows, c->hq, c->head_dim, dtype)) != SIFT_OK) return st;
+  a->row_ptr = r != nullptr ? r->row_ptr : nullptr;
+  a->row_pos = r != nullptr ? r->row_pos : nullptr;
+  if (a->row_ptr == nullptr &&
+      (rows % c->num_seqs != 0 || rows / c->num_seqs > c->max_rows))
+    return SIFT_E_SHAPE;
+  if (static_cast<int64_t>(rows) * c->hq > int64_t(1) << 26) return SIFT_E_CAPACITY;
+  a->rows = rows;
+  a->max_rows = c->max_rows;
+  a->q = q->data;
+  return sift::make_score(score, c->head_dim, &a->sc);
+}
+
+// Workgroups of the attention: two to a CU (one where its LDS allows no more).
+int32_t attn_groups(const sift_cache* c, bool bf16) {
+  return c->cus * (!bf16 && c->head_dim == 128 ? 1 : 2);
+}
+
+}  // namespace
+
+extern "C" {
+
+sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
+                              int32_t head_dim, int32_t page, int32_t max_pages,
+                              int32_t max_rows, sift_cache** cache_out) {
+  if (cache_out == nullptr) return SIFT_E_NULL;
+  *cache_out = nullptr;
+  if (num_seqs < 1 || num_q_heads < 1 || num_kv_heads < 1 || num_q_heads % num_kv_heads != 0 ||
+      max_pages < 1 || max_rows < 1)
+    return SIFT_E_SHAPE;
+  if (head_dim != 64 && head_dim != 128) return SIFT_E_UNSUPPORTED;
+  if (page != 16 && page != 32 && page != 64 && page != 128) return SIFT_E_UNSUPPORTED;
+  const int64_t g = num_q_heads / num_kv_heads;
+  if (static_cast<int64_t>(max_pages) * page > kMost || max_rows * g > kMost ||
+      num_seqs > kMost || num_kv_heads > kMost / 1024)
+    return SIFT_E_CAPACITY;
+  sift_cache* c = new (std::nothrow) sift_cache();
+  if (c == nullptr) return SIFT_E_HIP;
+  c->num_seqs = num_seqs;
+  c->hq = num_q_heads;
+  c->hkv = num_kv_heads;
+  c->head_dim = head_dim;
+  c->page = page;
+  c->max_pages = max_pages;
+  c->max_rows = max_rows;
+  const auto fail = [c]() {
+    if (c->dev != nullptr) (void)hipFree(c->dev);
+    delete c;
+    return SIFT_E_HIP;
+  };
+  if (hipGetDevice(&c->device) != hipSuccess ||
+      hipDeviceGetAttribute(&c->cus, hipDeviceAttributeMultiprocessorCount, c->device) !=
+          hipSuccess)
+    return fail();
+  const size_t rows = static_cast<size_t>(2 * c->cus) * sift::kCacheSlotRows;
+  const size_t o_bytes = rows * head_dim * sizeof(float);
+  if (hipMalloc(&c->dev, o_bytes + rows * sizeof(float4)) != hipSuccess) return fail();
+  c->part_o = static_cast<float*>(c->dev);
+  c->part_ml = reinterpret_cast<float4*>(static_cast<uint8_t*>(c->dev) + o_bytes);
+  *cache_out = c;
+  return SIFT_OK;
+}
+
+sift_status sift_cache_destroy(sift_cache* cache) {
+  if (cache == nullptr) return SIFT_OK;
+  sift_status st = SIFT_OK;
+  // the last work may still use the scratch
+  if (hipStreamSynchronize(cache->last_stream) != hipSuccess) st = SIFT_E_HIP;
+  if (hipFree(cache->dev) != hipSuccess) st = SIFT_E_HIP;
+  delete cache;
+  return st;
+}
+
+sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
+                                 const sift_cache_rows* new_rows, const sift_tensor* q,
+                                 const sift_tensor* k_new, const sift_tensor* v_new,
+                                 const uint64_t* tree_mask, int32_t mask_words,
+                                 const sift_score* score, sift_tensor* out, float* lse,
+                                 void* stream) {
+  sift::CacheAttnArgs a{};
+  sift_status st;
+  if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
+  const int32_t dtype = kv->k_pages->dtype;
+  if ((st = check_rows(cache, new_rows, q, dtype, score, &a.c)) != SIFT_OK) return st;
+  const int32_t rows = q->tokens, d = cache->head_dim;
+  if ((st = check_tensor(k_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
+  if ((st = check_tensor(v_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
+  if ((st = check_tensor(out, rows, cache->hq, d, dtype)) != SIFT_OK) return st;
+  if (tree_mask != nullptr && mask_words < (cache->max_rows + 63) / 64) return SIFT_E_CAPACITY;
+  if (rows == 0) return SIFT_OK;
+  a.k_new = k_new->data;
+  a.v_new = v_new->data;
+  a.tree_mask = tree_mask;
+  a.mask_words = mask_words;
+  a.out = out->data;
+  a.lse = lse;
+  a.part_o = cache->part_o;
+  a.part_ml = cache->part_ml;
+  const bool bf16 = dtype == SIFT_BF16;
+  a.groups = attn_groups(cache, bf16);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = sift::launch_cache_attn(a, bf16, d, s);
+  cache->last_stream = s;
+  return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
+}
+
+}  // extern "C"

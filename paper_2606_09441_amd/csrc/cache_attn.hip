@@ -1,0 +1,374 @@
+// Attention of every sequence's new tokens (one, a chain, a drafted tree) over
+// its paged cache and over each other.
+//
+// A unit is 32 rows of a (sequence, kv head): row r is new token r / g and query
+// head r % g of the g that share the kv head, so that a key is read once for
+// all of them.  Its keys are tiles of 32, the cached ones first, then the new
+// ones; all cached keys are visible to all rows, of the new ones those of the
+// row's mask.  Few rows and long caches: HBM bounds it, so what counts is even
+// and continuous reading.
+//  * The tiles of all units, four to a step, form one list, cut into equal runs
+//    for a fixed number of workgroups, whatever the lengths (which only the
+//    device knows).  A unit that one workgroup has whole is written by it; of
+//    the others every workgroup leaves its part (not normalised, with reference
+//    max and sums), and a second launch merges them in workgroup order.
+//  * The four wavefronts of a workgroup take the four tiles of a step, each
+//    through LDS of its own (16 KB at bf16, D = 128): no barriers inside a run.
+//    K of the next tile is fetched as soon as K is read, V likewise, so that
+//    each wavefront always has about a tile's half in flight, 128 KB a CU.
+
+#include <algorithm>
+
+#include "cache.h"
+#include "sift_internal.h"
+
+namespace sift {
+namespace {
+
+using namespace cache;
+
+constexpr int kTileKeys = 32;
+constexpr int kStepTiles = 4;  // a step: a tile for each wavefront
+
+struct UnitCost {
+  int32_t g, hkv;
+  __device__ __forceinline__ int blocks(const Seq& s) const {
+    return (s.n * g + kCacheRows - 1) / kCacheRows;
+  }
+  static __device__ __forceinline__ int tiles(const Seq& s) {
+    return (s.len + kTileKeys - 1) / kTileKeys + (s.n + kTileKeys - 1) / kTileKeys;
+  }
+  static __device__ __forceinline__ int steps(const Seq& s) {
+    return (tiles(s) + kStepTiles - 1) / kStepTiles;
+  }
+  __device__ __forceinline__ int64_t operator()(const Seq& s) const {
+    return static_cast<int64_t>(hkv) * blocks(s) * steps(s);
+  }
+};
+
+// The result of one row: sum of weights l, before their rounding le.
+template <typename T>
+__device__ __forceinline__ void store_row(T* dst, const float (&o)[4], float inv) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    *reinterpret_cast<bf16x4*>(dst) =
+        bf16x4{static_cast<__bf16>(o[0] * inv), static_cast<__bf16>(o[1] * inv),
+               static_cast<__bf16>(o[2] * inv), static_cast<__bf16>(o[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+}
+
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
+__device__ __forceinline__ float log_sum(float m, float le) {
+  return le > 0.f ? fmaf(m, kLn2, logf(le)) : le == le ? -INFINITY : le;
+}
+
+// Weight of a part with reference m in a sum with reference top (>= m).
+__device__ __forceinline__ float part_weight(float m, float top) {
+  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);  // no key: zeros, or NaN
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
+  using G = Tile<T, D>;
+  constexpr int kTile = kTileKeys * G::kRow;
+  constexpr int kDmas = 2 * G::kGroupDmas;  // of a K or V tile
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 2 * kTile];
+  __shared__ float part[4][kCacheRows][3];
+  const CacheArgs& a = p.c;
+  const int g = a.hq / a.hkv;
+  const UnitCost cost{g, a.hkv};
+  const int64_t total = total_work(a, cost);
+  const int64_t groups = min(static_cast<int64_t>(p.groups), total);
+  if (blockIdx.x >= groups) return;
+  int64_t x = share(blockIdx.x, total, groups);
+  const int64_t xend = share(blockIdx.x + 1, total, groups);
+
+  const int lane = threadIdx.x & 63;
+  const int wave = uniform(threadIdx.x >> 6);
+  const int l32 = lane & 31, hf = lane >> 5;
+  const int stride = a.hkv * G::kRow;
+  const int lds0 = static_cast<int>(reinterpret_cast<size_t>((lds_u8*)smem));
+  const int kt = lds0 + wave * 2 * kTile, vt = kt + kTile;  // this wavefront's tiles
+  const int kaddr = kt + G::lane_k(l32, hf);
+  const int vaddr = vt + G::lane_v(lane, l32, hf);
+  const float c = score_factor(a.sc);
+
+  Place pl = find_work(a, x, cost);
+  while (x < xend) {
+    // the unit that holds step x
+    const int b = uniform(pl.b);
+    const Seq s = sequence(a, b);
+    const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
+    const int steps = uniform(cost.steps(s)), blocks = uniform(cost.blocks(s));
+    const int unit = uniform(static_cast<int>((x - pl.at) / steps));
+    const int s0 = uniform(static_cast<int>(x - pl.at - static_cast<int64_t>(unit) * steps));
+    const int s1 = uniform(static_cast<int>(min(static_cast<int64_t>(steps), s0 + (xend - x))));
+    const int kvh = unit / blocks, r0 = unit % blocks * kCacheRows;
+    const int ct = (len + kTileKeys - 1) / kTileKeys;  // tiles of cached keys
+    const int tiles = ct + (n + kTileKeys - 1) / kTileKeys;
+
+    const int r = r0 + l32;
+    const bool live = r < n * g;
+    const int node = live ? r / g : 0;
+    const int h = kvh * g + (live ? r % g : 0);
+    QFrag<T, D> q;
+    q.load(static_cast<const T*>(a.q) + (static_cast<int64_t>(row0 + node) * a.hq + h) * D, hf,
+           live);
+    const float slope = a.sc.slopes != nullptr ? a.sc.slopes[h] * kLog2e : 0.f;
+    const int my_pos = a.sc.slopes == nullptr ? 0
+                       : a.row_pos != nullptr ? a.row_pos[row0 + node]
+                                              : len + node;
+
+    struct TileRows {
+      Rows16 r[2];
+    };
+    const auto rows_of = [&](int t) {
+      TileRows x;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = (t - ct) * kTileKeys + 16 * i;
+        x.r[i] = t < ct ? cached_rows(a, b, len, t * kTileKeys + 16 * i)
+                        : Rows16{static_cast<int64_t>(row0) + j, min(max(n - j, 0), 16)};
+      }
+      return x;
+    };
+    const auto fetch = [&](int t, const TileRows& x, auto v) {
+      constexpr bool kV = decltype(v)::value;
+      const void* base = t < ct ? (kV ? a.v : a.k) : (kV ? p.v_new : p.k_new);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        dma_rows<T, D, kV>((kV ? vt : kt) + i * 16 * G::kRow,
+                           rows_rsrc(reinterpret_cast<unsigned long long>(base) +
+                                         (x.r[i].row * a.hkv + kvh) * G::kRow,
+                                     x.r[i].n, stride, G::kRow),
+                           lane, stride);
+    };
+
+    RowState<D> st;
+    st.clear();
+    const int tend = min(tiles, s1 * kStepTiles);
+    int t = s0 * kStepTiles + wave;
+    TileRows rows{};
+    if (t < tend) {
+      rows = rows_of(t);
+      fetch(t, rows, std::false_type{});
+      fetch(t, rows, std::true_type{});
+    }
+    for (; t < tend; t += kStepTiles) {
+      const bool more = t + kStepTiles < tend;
+      // one bit a key: those this row sees
+      uint32_t bits = static_cast<uint32_t>(low_bits(rows.r[0].n)) |
+                      static_cast<uint32_t>(low_bits(rows.r[1].n)) << 16;
+      if (more) rows = rows_of(t + kStepTiles);
+      wait_vm<kDmas>();  // K is there, V may still be on its way
+      f32x16 sc = qk_block<T, D>(kaddr, 0, q);
+      wait_lds();        // K is read
+      if (more) fetch(t + kStepTiles, rows, std::false_type{});
+      const bool fresh = t >= ct;
+      const int j0 = (fresh ? t - ct : t) * kTileKeys;
+      if (fresh) {
+        if (p.tree_mask != nullptr)
+          bits &= static_cast<uint32_t>(
+              p.tree_mask[static_cast<int64_t>(row0 + node) * p.mask_words + (j0 >> 6)] >>
+              (j0 & 32));
+        else
+          bits &= static_cast<uint32_t>(low_bits(node + 1 - j0));
+      }
+      if (a.sc.slopes != nullptr && (fresh ? a.row_pos : a.key_pos) != nullptr) {
+        int dist[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int j = j0 + 4 * hf + key_of(v);
+          const int pos =
+              fresh ? a.row_pos[row0 + min(j, n - 1)]
+                    : a.key_pos[((static_cast<int64_t>(b) * a.hkv + kvh) * a.max_pages
+                                 << a.page_shift) +
+                                min(j, (a.max_pages << a.page_shift) - 1)];
+          dist[v] = my_pos - pos;
+        }
+        score_block_at(a.sc, slope, dist, sc);
+      } else {
+        score_block(a.sc, slope,
+                    static_cast<float>(my_pos - (fresh ? len : 0) - j0 - 4 * hf), sc);
+      }
+      if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(sc, bits >> (4 * hf));
+      st.rescale(half_max(block_max(sc)) * c);
+      weigh_block<T, true>(sc, c, st.base(), st.l, st.le);
+      if (more)
+        wait_vm<kDmas>();  // V is there, the next K may not be
+      else
+        wait_vm<0>();
+      if (fresh) {
+        // rows differ in what they see of V
+        bool bad = false;
+        for (int i = lane; i < kTile / 16; i += 64)
+          bad |= not_finite<T>(
+              *reinterpret_cast<const lds_u32x4*>(static_cast<size_t>(vt + 16 * i)));
+        if (__builtin_amdgcn_ballot_w64(bad)) {
+          add_not_finite<T, D>(vt, kTileKeys, live ? bits : 0u, hf, st.o);
+          for (int i = lane; i < kTile / 16; i += 64) {
+            lds_u32x4* at = reinterpret_cast<lds_u32x4*>(static_cast<size_t>(vt + 16 * i));
+            *at = only_finite<T>(*at);
+          }
+          wait_lds();
+        }
+      }
+      pv_block<T, D>(vaddr, sc, st.o);
+      wait_lds();  // V is read
+      if (more) fetch(t + kStepTiles, rows, std::true_type{});
+    }
+
+    // merge the wavefronts: each leaves its rows in its own tiles' memory, as
+    // fp32 rows whose 16-byte chunks are XORed with the row
+    constexpr int kOutChunks = D / 4;
+    {
+      const float l = half_sum(st.l), le = half_sum(st.le);
+      if (hf == 0) {
+        part[wave][l32][0] = st.m;
+        part[wave][l32][1] = l;
+        part[wave][l32][2] = le;
+      }
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<lds_f32x4*>(static_cast<size_t>(
+              kt + l32 * D * 4 + 16 * ((8 * db + 2 * i + hf) ^ (l32 & (kOutChunks - 1))))) =
+              f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                    st.o[db][4 * i + 3]};
+    }
+    __syncthreads();
+    {
+      const int row = threadIdx.x >> 3;  // 8 threads a row
+      float top = -INFINITY, wt[4], l = 0.f, le = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, part[w][row][0]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        wt[w] = part_weight(part[w][row][0], top);
+        l += part[w][row][1] * wt[w];
+        le += part[w][row][2] * wt[w];
+      }
+      const int rr = r0 + row;
+      if (rr < n * g) {
+        const bool whole = s0 == 0 && s1 == steps;
+        const int64_t at = static_cast<int64_t>(row0 + rr / g) * a.hq + kvh * g + rr % g;
+        const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (s0 == 0)) * kCacheRows + row;
+        if ((threadIdx.x & 7) == 0) {
+          if (!whole)
+            p.part_ml[slot] = float4{top, l, le, 0.f};
+          else if (p.lse != nullptr)
+            p.lse[at] = log_sum(top, le);
+        }
+        const float inv = inverse(l);
+        for (int ch = threadIdx.x & 7; ch < kOutChunks; ch += 8) {
+          float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const f32x4 y = *reinterpret_cast<const lds_f32x4*>(
+                static_cast<size_t>(lds0 + w * 2 * kTile + row * D * 4 +
+                                    16 * (ch ^ (row & (kOutChunks - 1)))));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += y[e] * wt[w];
+          }
+          if (whole)
+            store_row(static_cast<T*>(p.out) + at * D + 4 * ch, o, inv);
+          else
+            *reinterpret_cast<f32x4*>(p.part_o + slot * D + 4 * ch) =
+                f32x4{o[0], o[1], o[2], o[3]};
+        }
+      }
+    }
+    __syncthreads();  // the tiles' memory is free again
+    x += s1 - s0;
+    if (x < xend && x - pl.at >= cost(s)) pl = find_work(a, x, cost);
+  }
+}
+
+// Merge of the parts of one (new token, query head), a wavefront each: lane l
+// takes dims l D / 64 and on.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
+  const CacheArgs& a = p.c;
+  const int g = a.hq / a.hkv;
+  const UnitCost cost{g, a.hkv};
+  const int lane = threadIdx.x & 63;
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (item >= static_cast<int64_t>(a.rows) * a.hq) return;
+  const int token = static_cast<int>(item / a.hq), h = static_cast<int>(item % a.hq);
+  const int64_t total = total_work(a, cost);
+  if (total == 0) return;
+  const int64_t groups = min(static_cast<int64_t>(p.groups), total);
+  // the token's sequence, and its first step
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
+    const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
+    const bool in = b0 + lane < a.num_seqs;
+    const int64_t mine = in ? cost(s) : 0;
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up(upto, d);
+      if (lane >= d) upto += y;
+    }
+    uint64_t has = __ballot(in && token >= s.row0 && token < s.row0 + s.n);
+    for (; has != 0; has &= has - 1) {
+      const int l = __ffsll(static_cast<unsigned long long>(has)) - 1;
+      const int steps = __shfl(cost.steps(s), l), blocks = __shfl(cost.blocks(s), l);
+      const int row0 = __shfl(s.row0, l);
+      const int r = (token - row0) * g + h % g;
+      const int unit = h / g * blocks + r / kCacheRows;
+      const int64_t u0 = before + __shfl(upto - mine, l) + static_cast<int64_t>(unit) * steps;
+      const int64_t first = share_of(u0, total, groups);
+      const int64_t last = share_of(u0 + steps - 1, total, groups);
+      if (first == last) continue;  // written already
+      const int row = r % kCacheRows;
+      const auto slot = [&](int64_t w) { return (2 * w + (w == first)) * kCacheRows + row; };
+      float top = -INFINITY;
+      for (int64_t w = first + lane; w <= last; w += 64) top = fmaxf(top, p.part_ml[slot(w)].x);
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+      float lsum = 0.f, le = 0.f, o[D / 64] = {};
+      for (int64_t w = first; w <= last; ++w) {
+        const float4 ml = p.part_ml[slot(w)];
+        const float wt = part_weight(ml.x, top);
+        lsum += ml.y * wt;
+        le += ml.z * wt;
+        const float* src = p.part_o + slot(w) * D + lane * (D / 64);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) o[e] += src[e] * wt;
+      }
+      const float inv = inverse(lsum);
+      T* dst = static_cast<T*>(p.out) + item * D + lane * (D / 64);
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) dst[e] = static_cast<T>(o[e] * inv);
+      if (p.lse != nullptr && lane == 0) p.lse[item] = log_sum(top, le);
+    }
+    before += __shfl(upto, 63);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream) {
+  if (a.c.rows == 0) return hipSuccess;
+  const int64_t items = static_cast<int64_t>(a.c.rows) * a.c.hq;
+  const int64_t merge = (items + 3) / 4;
+  if (merge >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
+  const auto launch = [&](auto elem, auto dim) {
+    using T = decltype(elem);
+    constexpr int D = decltype(dim)::value;
+    hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), dim3(256), 0, stream, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3(static_cast<unsigned>(merge)), dim3(256),
+                       0, stream, a);
+    return hipGetLastError();
+  };
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (bf16) return head_dim == 128 ? launch(__bf16{}, D128{}) : launch(__bf16{}, D64{});
+  return head_dim == 128 ? launch(float{}, D128{}) : launch(float{}, D64{});
+}
+
+}  // namespace sift

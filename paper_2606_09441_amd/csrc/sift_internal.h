@@ -423,4 +423,45 @@ struct DenseArgs {
 int64_t dense_grid(int32_t num_recs, int32_t hq, int32_t hkv);
 hipError_t launch_attn_dense(const DenseArgs& a, bool bf16, int head_dim, hipStream_t stream);
 
+// The page cache (cache_attn.hip, cache_weights.hip, cache_evict.hip).  Slot i
+// of sequence b is row i % page of page table[b][i / page] of the pool; it
+// holds a key where i < lens[b] and, with page_lens, i % page <
+// page_lens[b][i / page].  Values read from the device are clamped: no table,
+// length or row pointer leads outside the caller's buffers.
+struct CacheArgs {
+  const void* k;             // [num_pages * page][hkv][D]
+  const void* v;
+  const int32_t* table;      // [num_seqs][max_pages]
+  const int32_t* lens;       // [num_seqs]
+  const int32_t* page_lens;  // [num_seqs][max_pages] or nullptr
+  const int32_t* key_pos;    // [num_seqs][hkv][max_pages * page] or nullptr: the slot
+  int32_t num_seqs, max_pages, page_shift, num_pages;
+  int32_t hq, hkv;
+  // the sequences' new tokens, rows row_ptr[b] .. row_ptr[b + 1] - 1 of q
+  const int32_t* row_ptr;    // [num_seqs + 1] or nullptr: rows / num_seqs each
+  const int32_t* row_pos;    // [rows] or nullptr: lens[b] and on
+  int32_t rows, max_rows;
+  const void* q;             // [rows][hq][D]
+  ScoreArgs sc;
+};
+
+struct CacheAttnArgs {
+  CacheArgs c;
+  const void* k_new;         // [rows][hkv][D]
+  const void* v_new;
+  const uint64_t* tree_mask; // [rows][mask_words] or nullptr: a row sees those up to itself
+  int32_t mask_words;
+  void* out;                 // [rows][hq][D]
+  float* lse;                // [rows][hq] or nullptr
+  // partial results of units that more than one workgroup shares: two slots a
+  // workgroup, 32 rows each
+  float* part_o;             // [slots][32][D], not normalised
+  float4* part_ml;           // [slots][32] {reference max, sum, sum before rounding, 0}
+  int32_t groups;            // workgroups of the launch
+};
+
+constexpr int kCacheRows = 32;  // rows (new token, query head of the kv head) of a unit
+constexpr int64_t kCacheSlotRows = 2 * kCacheRows;  // partial rows of a workgroup
+hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream);
+
 }  // namespace sift

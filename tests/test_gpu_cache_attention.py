@@ -1,0 +1,205 @@
+"""GPU tests of the attention over a paged cache (sift_cache_attention) against
+the fp64 oracle, element by element.  Pool rows that hold no key are NaN."""
+
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from cache_helpers import Batch, random_tree, some_empty
+from gpu_helpers import max_abs, say
+
+pytestmark = pytest.mark.gpu
+
+# as in test_gpu_dense.py: the project's bars on N(0, 1) inputs; the log sum's
+# error is that of the scores
+TOL = {"f32": 1e-5, "bf16": 2e-2}
+LSE_TOL = 1e-4
+
+
+def check(x, cap=0.0, bias=False, scale=None, row_ptr=True, name=""):
+    import torch
+    slopes = (2.0 ** (-4.0 * np.arange(1, x.hq + 1) / x.hq)).astype(np.float32) if bias else None
+    lse = torch.full((x.rows, x.hq), 7.0, device=x.q.device)
+    out = torch.full_like(x.q, 7.0)
+    with x.cache() as cache:
+        cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"] if row_ptr else None,
+                        tree_mask=x.mask, row_pos=x.t["row_pos"], scale=scale, cap=cap,
+                        slopes=None if slopes is None else torch.from_numpy(slopes).to(x.q.device),
+                        out=out, lse=lse)
+        torch.cuda.synchronize()
+    ref, ref_lse = x.oracle(scale=scale, cap=cap, slopes=slopes)
+    out, lse = out.float().cpu().numpy(), lse.cpu().numpy()
+    none = np.isneginf(ref_lse)
+    assert np.array_equal(none, np.isneginf(lse))
+    assert not out[none].any()
+    dt = "bf16" if x.q.dtype == torch.bfloat16 else "f32"
+    e, el = max_abs(out, ref), max_abs(lse[~none], ref_lse[~none])
+    say(f"{name} {dt}: {e:.2e}, lse {el:.2e}")
+    assert e <= TOL[dt] and el <= LSE_TOL
+    return out, lse
+
+
+TYPES = [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)]
+LENS = [0, 1, 15, 16, 17, 31, 33, 64, 127, 129, 300, 700]
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_single_tokens(dtype, d, page):
+    check(Batch(LENS, [1] * len(LENS), 8, 2, d, dtype, page), row_ptr=False)
+    check(Batch(LENS, [1] * len(LENS), 8, 2, d, dtype, page, gaps=True), cap=20.0)
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("tree", [None, random_tree, some_empty])
+def test_trees(dtype, d, tree):
+    new = [5, 0, 1, 33, 3, 2, 64, 12, 0, 1, 20, 40]
+    for gaps, moved, cap, bias in [(False, False, 0.0, False), (True, True, 0.0, True),
+                                   (True, False, 30.0, False), (False, True, 20.0, True),
+                                   (False, False, 0.0, True)]:
+        check(Batch(LENS, new, 6, 2, d, dtype, 32, gaps, moved, tree, seed=3), cap, bias,
+              name=f"gaps {gaps} moved {moved} cap {cap} bias {bias}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_new_tokens(dtype):
+    """More than a mask word of them, and a chain longer than the cache."""
+    check(Batch([40, 0, 513], [130, 65, 200], 4, 1, 128, dtype, tree=random_tree, seed=4))
+    check(Batch([40, 0], [150, 90], 4, 4, 64, dtype, seed=5))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 1), (12, 3), (64, 1), (40, 1)])
+def test_head_layouts(hq, hkv):
+    check(Batch([200, 0, 77], [3, 1, 2], hq, hkv, 64, "bf16", seed=6))
+
+
+def test_many_sequences():
+    """More sequences than a wavefront has lanes, many of them without work."""
+    rng = np.random.default_rng(7)
+    lens = rng.integers(0, 90, 150).tolist()
+    new = [int(rng.integers(0, 3)) for _ in lens]
+    check(Batch(lens, new, 4, 2, 64, "bf16", 16, seed=7))
+
+
+def test_long_cache():
+    """Every workgroup shares units with others."""
+    for dtype in ("bf16", "f32"):
+        check(Batch([20000, 7], [1, 1], 4, 1, 128, dtype, 128, seed=8))
+        check(Batch([9000], [21], 8, 2, 64, dtype, 16, tree=random_tree, gaps=True, seed=9), cap=50.0)
+
+
+def test_shared_pages():
+    """Two sequences read the same pages."""
+    x = Batch([100, 100], [2, 2], 4, 2, 128, "bf16", 64, seed=10)
+    x.table[1] = x.table[0]
+    x.t["table"][1] = x.t["table"][0]
+    check(x)
+
+
+def test_rows_left_out():
+    """Rows that row_ptr does not name stay as they are."""
+    import torch
+    x = Batch([50, 60], [4, 4], 4, 2, 64, "bf16", seed=11)
+    out = torch.full_like(x.q, 7.0)
+    with x.cache() as cache:
+        whole = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"])
+        ptr = torch.tensor([0, 4, 6], dtype=torch.int32, device=x.q.device)
+        cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=ptr, out=out)
+    assert torch.equal(out[:6], whole[:6]) and bool((out[6:] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_unseen_new_tokens_do_not_matter(dtype, value):
+    """A drafted token with such values reaches the rows that see it and no other."""
+    x = Batch([70, 0], [9, 40], 4, 2, 128, dtype, tree=random_tree, seed=12)
+    for bad, b in ((3, 0), (9 + 20, 1)):
+        x.v_new[bad, 1, 5:9] = value
+    import torch
+    with x.cache() as cache:
+        out = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"],
+                              tree_mask=x.mask).float().cpu().numpy()
+        x.k_new[3], x.k_new[29] = value, value
+        worse = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"],
+                                tree_mask=x.mask).float().cpu().numpy()
+    torch.cuda.synchronize()
+    x.k_new[3], x.k_new[29] = 0, 0
+    sees = np.concatenate([x.sees[0][:, 3], x.sees[1][:, 20]])
+    with np.errstate(all="ignore"):
+        ref, _ = x.oracle()
+    assert max_abs(worse[~sees], ref[~sees]) <= TOL[dtype]
+    ref_k = Batch([70, 0], [9, 40], 4, 2, 128, dtype, tree=random_tree, seed=12)
+    ref_k.v_new.copy_(x.v_new)
+    with np.errstate(all="ignore"):
+        ref, _ = ref_k.oracle()
+    fine = np.isfinite(ref)
+    assert np.array_equal(fine, np.isfinite(out))
+    assert max_abs(out[fine], ref[fine]) <= TOL[dtype]
+    assert np.array_equal(np.isnan(out), np.isnan(ref))
+
+
+def test_streams_and_repeats():
+    """The same bits on another stream and in a captured graph; a replay follows the
+    tables' present contents."""
+    import torch
+    x = Batch([300, 41], [7, 7], 8, 2, 128, "bf16", tree=random_tree, seed=13)
+    args = (x.q, x.k_new, x.v_new, x.pages())
+    with x.cache() as cache:
+        kw = dict(row_ptr=x.t["row_ptr"], tree_mask=x.mask)
+        first = cache.attention(*args, **kw)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        out = torch.zeros_like(first)
+        with torch.cuda.stream(side):
+            cache.attention(*args, out=out, **kw)
+        side.synchronize()
+        assert torch.equal(out, first)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.attention(*args, out=out, **kw)
+        for n in (300, 200, 0, 300):
+            x.t["lens"][0] = n
+            out.zero_()
+            graph.replay()
+            got = out.clone()
+            assert torch.equal(got, cache.attention(*args, **kw))
+        assert torch.equal(got, first)
+
+
+def test_refusals():
+    import torch
+    from paper_2606_09441_amd import Cache, CachePages, SiftError
+    x = Batch([100, 30], [2, 2], 4, 2, 128, "bf16", seed=14)
+    kv = x.pages()
+
+    def refused(status, fn, *a, **kw):
+        with pytest.raises(SiftError) as e:
+            fn(*a, **kw)
+        assert e.value.status == status
+
+    for status, args in ((2, (0, 4, 2, 128)), (2, (2, 3, 2, 128)), (4, (2, 4, 2, 96)),
+                         (5, (2, 4, 2, 128, 128, 1 << 24))):
+        refused(status, Cache, *args)
+    refused(4, Cache, 2, 4, 2, 128, page=48)
+    refused(2, Cache, 2, 4, 2, 128, max_rows=0)
+    with x.cache() as cache:
+        f = cache.attention
+        refused(2, f, x.q[:3], x.k_new[:3], x.v_new[:3], kv)          # not as many of each
+        refused(2, f, x.q, x.k_new[:3], x.v_new, kv)
+        refused(4, f, x.q, x.k_new, x.v_new.float(), kv)
+        refused(4, f, x.q.float(), x.k_new.float(), x.v_new.float(), kv)
+        refused(4, f, x.q, x.k_new, x.v_new, kv, cap=-2.0)
+        refused(5, f, x.q, x.k_new, x.v_new, kv, row_ptr=x.t["row_ptr"][:2])
+        refused(4, f, x.q, x.k_new, x.v_new, kv, row_ptr=x.t["row_ptr"].long())
+        refused(5, f, x.q, x.k_new, x.v_new, kv, tree_mask=torch.zeros(3, 1, dtype=torch.int64,
+                                                                       device=x.q.device))
+        refused(5, f, x.q, x.k_new, x.v_new, kv, lse=torch.zeros(3, device=x.q.device))
+        small = CachePages(x.k, x.v, x.t["table"][:1].contiguous(), x.t["lens"])
+        refused(5, f, x.q, x.k_new, x.v_new, small)
+        odd = CachePages(x.k[:-1], x.v[:-1], x.t["table"], x.t["lens"])
+        refused(2, f, x.q, x.k_new, x.v_new, odd)
+        other = CachePages(x.k, x.v[:-64], x.t["table"], x.t["lens"])
+        refused(2, f, x.q, x.k_new, x.v_new, other)
+    refused(4, CachePages, x.k, x.v, x.t["table"].long(), x.t["lens"])
+    refused(1, CachePages, x.k, x.v, None, x.t["lens"])
