@@ -145,6 +145,56 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
                                  const sift_score* score, sift_tensor* out, float* lse,
                                  void* stream);
 
+/*
+ * Accumulated attention weights of the cached keys, what an eviction goes by:
+ *   out[b][kv][i] = decay * weights[b][kv][i]
+ *                   + sum over the rows r of b and the query heads h of kv of
+ *                     row_weight[r] * exp(s(r, h, i) - lse[r][h])
+ * with the scores s of the attention call that left lse (same q, score and
+ * tables; its new tokens' own keys are in lse, not here).
+ *   lse          device float [rows][Hq]; a row of -infinity counts for nothing
+ *   row_weight   device float [rows] >= 0, or NULL: 1.  0 leaves a row out (a
+ *                drafted token that was not accepted), whatever it holds.
+ *   weights      device float [num_seqs][Hkv][max_pages * page], or NULL: zeros
+ *   out          the same shape, may be weights.  Slots before lens[b] that hold no
+ *                key get 0, those from lens[b] on are not written.
+ * Sums are fp32, in the order of the rows: the result is the same every time.
+ * Errors: as sift_cache_attention; SIFT_E_UNSUPPORTED for a decay that is not
+ *   finite.
+ */
+sift_status sift_cache_accumulate(sift_cache* cache, const sift_cache_kv* kv,
+                                  const sift_cache_rows* new_rows, const sift_tensor* q,
+                                  const float* lse, const float* row_weight,
+                                  const sift_score* score, const float* weights, float decay,
+                                  float* out, void* stream);
+
+/*
+ * Eviction: every (sequence, kv head) keeps n = min(its keys, budget) keys, its
+ * protected ones first, then those of the largest weights; equal weights (-0 and
+ * 0 among them) go to the lowest slot, NaN counts as less than every number.
+ * Protected: positions before `sinks`, and from next_pos[b] - recent on
+ * (next_pos: device int32 [num_seqs], the position of the next token, or NULL:
+ * lens[b]).  The kept keys end up in slots 0 .. n - 1: those that lie there
+ * stay, of the others the j-th in slot order moves to the j-th free slot, K and
+ * V rows in place.
+ *   budget       >= 1;  sinks, recent >= 0, sinks + recent <= budget
+ *   weights      device float [num_seqs][Hkv][max_pages * page]
+ *   weights_out, pos_out   the same shape (float, int32): the kept keys' weights
+ *                and positions; past them 0 and -1.  pos_out is the key_pos of the
+ *                next calls.
+ *   lens_out     device int32 [num_seqs]: n, the lens of the next calls, which
+ *                take no page_lens: the first slots are all used
+ * weights, key_pos and lens are not changed; the outputs may not overlap them.
+ * The pages of the first `budget` slots must be the sequence's own.
+ * Errors: SIFT_E_NULL, SIFT_E_SHAPE (budget, sinks, recent), SIFT_E_UNSUPPORTED
+ *   (overlap, alignment), SIFT_E_CAPACITY (2^22 (sequence, kv head) pairs or
+ *   more, 2^30 moves or more), SIFT_E_PLAN, SIFT_E_HIP.
+ */
+sift_status sift_cache_evict(sift_cache* cache, const sift_cache_kv* kv, const float* weights,
+                             const int32_t* next_pos, int32_t budget, int32_t sinks,
+                             int32_t recent, float* weights_out, int32_t* pos_out,
+                             int32_t* lens_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -129,6 +129,21 @@ _SERVE_SIGS = {
                                        ctypes.POINTER(SiftTensor), ctypes.c_int32,
                                        ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor), _P,
                                        _P]),
+    "sift_cache_create": (ctypes.c_int, [ctypes.c_int32] * 7 + [ctypes.POINTER(_P)]),
+    "sift_cache_destroy": (ctypes.c_int, [_P]),
+    "sift_cache_attention": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv),
+                                            ctypes.POINTER(SiftCacheRows),
+                                            ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
+                                            ctypes.POINTER(SiftTensor), _P, ctypes.c_int32,
+                                            ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor),
+                                            _P, _P]),
+    "sift_cache_accumulate": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv),
+                                             ctypes.POINTER(SiftCacheRows),
+                                             ctypes.POINTER(SiftTensor), _P, _P,
+                                             ctypes.POINTER(SiftScore), _P, ctypes.c_float, _P,
+                                             _P]),
+    "sift_cache_evict": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv), _P, _P, ctypes.c_int32,
+                                        ctypes.c_int32, ctypes.c_int32, _P, _P, _P, _P]),
 }
 
 # entries of the decoder layer (csrc/layer_api.h), not part of sift.h
@@ -748,3 +763,59 @@ class Cache:
             ctypes.byref(vd), _ptr(tree_mask), words, ctypes.byref(score), ctypes.byref(od),
             _ptr(lse), _stream_ptr(stream)))
         return out
+
+    def _slot_buffer(self, fn, t, name, dtype="float32"):
+        require(fn, t, name, dtype, self.num_seqs * self.hkv * self.slots, self.device)
+
+    def accumulate(self, q, lse, kv, weights=None, decay=1.0, row_ptr=None, row_pos=None,
+                   row_weight=None, scale=None, cap=0.0, slopes=None, out=None, stream=None):
+        """decay * weights plus the attention weight that the new tokens q give to each
+        cached key (sift_cache_accumulate): weights and out float32 [seqs, Hkv,
+        max_pages * page] (weights None: zeros), lse as the attention left it.
+        row_weight float32 [rows] scales a token's part, 0 leaves it out.  out: the
+        weights themselves when None (a new buffer where there are none)."""
+        torch = _torch()
+        fn = "sift_cache_accumulate"
+        rows = self._rows(fn, q, row_ptr, row_pos)
+        require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
+        if row_weight is not None:
+            require(fn, row_weight, "row_weight", "float32", q.shape[0], self.device)
+        if weights is not None:
+            self._slot_buffer(fn, weights, "weights")
+        if out is None:
+            out = weights if weights is not None else torch.zeros(
+                self.num_seqs, self.hkv, self.slots, dtype=torch.float32, device=self.device)
+        self._slot_buffer(fn, out, "out")
+        score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
+        qd = tensor_desc(q)
+        check(fn, lib().sift_cache_accumulate(
+            self._h, self._kv(fn, kv), ctypes.byref(rows), ctypes.byref(qd), _ptr(lse),
+            _ptr(row_weight), ctypes.byref(score), _ptr(weights), decay, _ptr(out),
+            _stream_ptr(stream)))
+        return out
+
+    def evict(self, kv, weights, budget, sinks=0, recent=0, next_pos=None, weights_out=None,
+              pos_out=None, lens_out=None, stream=None):
+        """Keeps `budget` keys of every (sequence, kv head), those of the largest weights
+        beside the protected first `sinks` and last `recent` positions, in its first slots
+        (sift_cache_evict; K and V move in place).  Returns (weights, key_pos, lens) of
+        the cache as it is then: a CachePages of them has no page_lens."""
+        torch = _torch()
+        fn = "sift_cache_evict"
+        self._slot_buffer(fn, weights, "weights")
+        if next_pos is not None:
+            require(fn, next_pos, "next_pos", "int32", self.num_seqs, self.device)
+        shape = (self.num_seqs, self.hkv, self.slots)
+        if weights_out is None:
+            weights_out = torch.empty(shape, dtype=torch.float32, device=self.device)
+        if pos_out is None:
+            pos_out = torch.empty(shape, dtype=torch.int32, device=self.device)
+        if lens_out is None:
+            lens_out = torch.empty(self.num_seqs, dtype=torch.int32, device=self.device)
+        self._slot_buffer(fn, weights_out, "weights_out")
+        self._slot_buffer(fn, pos_out, "pos_out", "int32")
+        require(fn, lens_out, "lens_out", "int32", self.num_seqs, self.device)
+        check(fn, lib().sift_cache_evict(
+            self._h, self._kv(fn, kv), _ptr(weights), _ptr(next_pos), budget, sinks, recent,
+            _ptr(weights_out), _ptr(pos_out), _ptr(lens_out), _stream_ptr(stream)))
+        return weights_out, pos_out, lens_out

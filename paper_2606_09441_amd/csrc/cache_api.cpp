@@ -1,9 +1,11 @@
 // C ABI of the page cache (include/sift_serve.h): the handle with its scratch,
-// and the host checks of its calls.  The kernels are in cache_attn.hip.
+// and the host checks of its calls.  The kernels are in cache_attn.hip,
+// cache_weights.hip and cache_evict.hip.
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <initializer_list>
 #include <limits>
@@ -21,6 +23,8 @@ struct sift_cache {
   void* dev = nullptr;
   float* part_o = nullptr;
   float4* part_ml = nullptr;
+  int32_t* moves = nullptr;      // of the eviction (CacheEvictArgs)
+  int32_t* num_moves = nullptr;
   hipStream_t last_stream = nullptr;  // the stream of the last enqueued work
 };
 
@@ -78,7 +82,7 @@ sift_status check_kv(const sift_cache* c, const sift_cache_kv* kv, sift::CacheAr
 
 // The new tokens; dtype: the pools'.
 sift_status check_rows(const sift_cache* c, const sift_cache_rows* r, const sift_tensor* q,
-                       int32_t dtype, const sift_score* score, sift::CacheArgs* a) {
+                       int32_t dtype, const sift_score* score, double unit, sift::CacheArgs* a) {
   if (q == nullptr) return SIFT_E_NULL;
   const int32_t rows = q->tokens;
   if (rows < 0) return SIFT_E_SHAPE;
@@ -93,7 +97,13 @@ sift_status check_rows(const sift_cache* c, const sift_cache_rows* r, const sift
   a->rows = rows;
   a->max_rows = c->max_rows;
   a->q = q->data;
-  return sift::make_score(score, c->head_dim, &a->sc);
+  return sift::make_score(score, c->head_dim, unit, &a->sc);
+}
+
+// Whether [p, p + n) and [q, q + n) share a byte.
+bool overlap(const void* p, const void* q, size_t n) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return q != nullptr && a < b + n && b < a + n;
 }
 
 // Workgroups of the attention: two to a CU (one where its LDS allows no more).
@@ -139,9 +149,22 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
     return fail();
   const size_t rows = static_cast<size_t>(2 * c->cus) * sift::kCacheSlotRows;
   const size_t o_bytes = rows * head_dim * sizeof(float);
-  if (hipMalloc(&c->dev, o_bytes + rows * sizeof(float4)) != hipSuccess) return fail();
-  c->part_o = static_cast<float*>(c->dev);
-  c->part_ml = reinterpret_cast<float4*>(static_cast<uint8_t*>(c->dev) + o_bytes);
+  const size_t heads = static_cast<size_t>(num_seqs) * num_kv_heads;
+  const size_t moves = heads * max_pages * page;
+  size_t at = 0;
+  const auto place = [&at](size_t n) {
+    const size_t off = at;
+    at += (n + 255) & ~size_t(255);
+    return off;
+  };
+  const size_t o_o = place(o_bytes), o_ml = place(rows * sizeof(float4));
+  const size_t o_moves = place(moves * sizeof(int32_t)), o_num = place(heads * sizeof(int32_t));
+  if (hipMalloc(&c->dev, at) != hipSuccess) return fail();
+  uint8_t* base = static_cast<uint8_t*>(c->dev);
+  c->part_o = reinterpret_cast<float*>(base + o_o);
+  c->part_ml = reinterpret_cast<float4*>(base + o_ml);
+  c->moves = reinterpret_cast<int32_t*>(base + o_moves);
+  c->num_moves = reinterpret_cast<int32_t*>(base + o_num);
   *cache_out = c;
   return SIFT_OK;
 }
@@ -166,7 +189,8 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   sift_status st;
   if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
   const int32_t dtype = kv->k_pages->dtype;
-  if ((st = check_rows(cache, new_rows, q, dtype, score, &a.c)) != SIFT_OK) return st;
+  if ((st = check_rows(cache, new_rows, q, dtype, score, sift::kUnitLog2e, &a.c)) != SIFT_OK)
+    return st;
   const int32_t rows = q->tokens, d = cache->head_dim;
   if ((st = check_tensor(k_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
   if ((st = check_tensor(v_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
@@ -185,6 +209,70 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   a.groups = attn_groups(cache, bf16);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = sift::launch_cache_attn(a, bf16, d, s);
+  cache->last_stream = s;
+  return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
+}
+
+sift_status sift_cache_accumulate(sift_cache* cache, const sift_cache_kv* kv,
+                                  const sift_cache_rows* new_rows, const sift_tensor* q,
+                                  const float* lse, const float* row_weight,
+                                  const sift_score* score, const float* weights, float decay,
+                                  float* out, void* stream) {
+  sift::CacheWeightArgs a{};
+  sift_status st;
+  if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
+  const int32_t dtype = kv->k_pages->dtype;
+  if ((st = check_rows(cache, new_rows, q, dtype, score, 1.0, &a.c)) != SIFT_OK) return st;
+  if (out == nullptr || (lse == nullptr && q->tokens > 0)) return SIFT_E_NULL;
+  if (!std::isfinite(decay)) return SIFT_E_UNSUPPORTED;
+  a.lse = lse;
+  a.row_weight = row_weight;
+  a.weights = weights;
+  a.out = out;
+  a.decay = decay;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e =
+      sift::launch_cache_weights(a, dtype == SIFT_BF16, cache->head_dim, cache->cus, s);
+  cache->last_stream = s;
+  return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
+}
+
+sift_status sift_cache_evict(sift_cache* cache, const sift_cache_kv* kv, const float* weights,
+                             const int32_t* next_pos, int32_t budget, int32_t sinks,
+                             int32_t recent, float* weights_out, int32_t* pos_out,
+                             int32_t* lens_out, void* stream) {
+  sift::CacheEvictArgs a{};
+  sift_status st;
+  if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
+  if (weights == nullptr || weights_out == nullptr || pos_out == nullptr || lens_out == nullptr)
+    return SIFT_E_NULL;
+  if (budget < 1 || sinks < 0 || recent < 0 || static_cast<int64_t>(sinks) + recent > budget)
+    return SIFT_E_SHAPE;
+  const int64_t heads = static_cast<int64_t>(cache->num_seqs) * cache->hkv;
+  const int64_t slots = static_cast<int64_t>(cache->max_pages) * cache->page;
+  const size_t bytes = static_cast<size_t>(heads * slots) * 4;
+  if (overlap(weights_out, weights, bytes) || overlap(weights_out, kv->key_pos, bytes) ||
+      overlap(pos_out, weights, bytes) || overlap(pos_out, kv->key_pos, bytes) ||
+      overlap(pos_out, weights_out, bytes))
+    return SIFT_E_UNSUPPORTED;
+  const size_t small = static_cast<size_t>(cache->num_seqs) * 4;
+  if (overlap(lens_out, kv->lens, small) || overlap(lens_out, next_pos, small))
+    return SIFT_E_UNSUPPORTED;
+  if (heads >= int64_t(1) << 22 || heads * std::min<int64_t>(budget, slots / 2) >= int64_t(1) << 30)
+    return SIFT_E_CAPACITY;
+  a.weights = weights;
+  a.next_pos = next_pos;
+  a.budget = budget;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.weights_out = weights_out;
+  a.pos_out = pos_out;
+  a.lens_out = lens_out;
+  a.moves = cache->moves;
+  a.num_moves = cache->num_moves;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const int row = cache->head_dim * (kv->k_pages->dtype == SIFT_BF16 ? 2 : 4);
+  const hipError_t e = sift::launch_cache_evict(a, row, s);
   cache->last_stream = s;
   return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
 }

@@ -43,6 +43,8 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) float lds_float;
 typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+typedef __attribute__((address_space(3))) int lds_int;
+typedef __attribute__((address_space(3))) i32x4 lds_i32x4;
 
 constexpr int kBufferWord3 = 0x00020000;  // gfx9-family raw buffer resource word 3
 constexpr float kLog2e = 1.4426950408889634f;
@@ -236,7 +238,7 @@ __device__ __forceinline__ void pv_block(int addr, const f32x16& p, f32x16 (&o)[
   }
 }
 
-// cap * log2(e) * tanh(x z0) for any z0.
+// cap * tanh(x z0), in the unit of sc, for any z0.
 __device__ __forceinline__ float cap_any(const ScoreArgs& sc, float z) {
   const float y = z * sc.x;
   const float w = z * z;

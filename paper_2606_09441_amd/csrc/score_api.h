@@ -9,15 +9,17 @@
 
 namespace sift {
 
-// score == nullptr: the default scale alone.
-inline sift_status make_score(const sift_score* score, int32_t head_dim, ScoreArgs* out) {
+constexpr double kUnitLog2e = 1.4426950408889634;
+
+// score == nullptr: the default scale alone.  unit: see ScoreArgs.
+inline sift_status make_score(const sift_score* score, int32_t head_dim, double unit,
+                              ScoreArgs* out) {
   const sift_score s = score != nullptr ? *score : sift_score{0.f, 0.f, nullptr};
   if (!(s.cap >= 0.f) || !std::isfinite(s.cap)) return SIFT_E_UNSUPPORTED;
-  const double log2e = 1.4426950408889634;
   const double scale = s.softmax_scale > 0.f && std::isfinite(s.softmax_scale)
                            ? static_cast<double>(s.softmax_scale)
                            : 1.0 / std::sqrt(static_cast<double>(head_dim));
-  out->c = static_cast<float>(scale * log2e);
+  out->c = static_cast<float>(scale * unit);
   out->x = 0.f;
   out->cap2 = 0.f;
   for (float& a : out->a) a = 0.f;
@@ -25,8 +27,8 @@ inline sift_status make_score(const sift_score* score, int32_t head_dim, ScoreAr
   if (s.cap == 0.f) return SIFT_OK;
   const double x = scale / static_cast<double>(s.cap);
   out->x = static_cast<float>(x);
-  out->cap2 = static_cast<float>(s.cap * log2e);
-  double power = scale * log2e;  // scale log2(e) (scale / cap)^2i
+  out->cap2 = static_cast<float>(s.cap * unit);
+  double power = scale * unit;  // unit scale (scale / cap)^2i
   for (int i = 0; i < 5; ++i, power *= x * x) out->a[i] = static_cast<float>(kTanhPoly[i] * power);
   // a factor that fp32 does not hold, or holds as a denormal, would be a cap of another value
   if (!std::isnormal(out->x) || !std::isnormal(out->cap2)) return SIFT_E_UNSUPPORTED;

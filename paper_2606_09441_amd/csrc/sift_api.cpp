@@ -1221,7 +1221,7 @@ sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_te
     if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return SIFT_E_UNSUPPORTED;
   if (mask < SIFT_MASK_CAUSAL || mask > SIFT_MASK_PREFIX) return SIFT_E_UNSUPPORTED;
   sift::DenseArgs a{};
-  if ((st = sift::make_score(score, in.head_dim, &a.sc)) != SIFT_OK) return st;
+  if ((st = sift::make_score(score, in.head_dim, sift::kUnitLog2e, &a.sc)) != SIFT_OK) return st;
   if ((st = check_device(plan)) != SIFT_OK) return st;
   // a grid holds fewer than 2^32 threads
   if (sift::dense_grid(plan->num_dense, in.num_q_heads, in.num_kv_heads) >= int64_t(1) << 24)

@@ -386,13 +386,13 @@ hipError_t launch_silu_mul(const void* gate, const void* up, int64_t count, void
                            hipStream_t stream);
 
 // Scores of the dense and the cache attention: z = scale * q.k, then
-// cap * tanh(z / cap) where cap > 0, then - slope[head] * |distance|; all in
-// the log2 domain, t = s * log2(e).
+// cap * tanh(z / cap) where cap > 0, then - slope[head] * |distance|; in the
+// unit of log2(e) (the attention, whose weights are powers of 2) or of 1.
 struct ScoreArgs {
-  float c;        // scale * log2(e)
+  float c;        // scale * unit
   float x;        // scale / cap: x z0 is the tanh's argument (z0 = q.k); 0: no cap
-  float cap2;     // cap * log2(e)
-  float a[5];     // t = z0 * poly(z0^2) where |x z0| <= kTanhSmall
+  float cap2;     // cap * unit
+  float a[5];     // unit * s = z0 * poly(z0^2) where |x z0| <= kTanhSmall
   const float* slopes;  // [Hq] or nullptr
 };
 
@@ -463,5 +463,36 @@ struct CacheAttnArgs {
 constexpr int kCacheRows = 32;  // rows (new token, query head of the kv head) of a unit
 constexpr int64_t kCacheSlotRows = 2 * kCacheRows;  // partial rows of a workgroup
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream);
+
+// Accumulated attention weights (cache_weights.hip); c.sc in the natural domain.
+struct CacheWeightArgs {
+  CacheArgs c;
+  const float* lse;          // [rows][hq]
+  const float* row_weight;   // [rows] or nullptr: 1
+  const float* weights;      // [num_seqs][hkv][slots] or nullptr: zeros
+  float* out;                // the same shape
+  float decay;
+  int32_t chunk_rows;        // rows of q that a workgroup holds in LDS, a multiple of 32
+  int32_t groups;            // workgroups of the launch
+};
+// chunk_rows and groups are set by the launch.
+hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int cus,
+                                hipStream_t stream);
+
+// Eviction (cache_evict.hip): a selection per (sequence, kv head), then the
+// moves of the K and V rows that it lists.
+struct CacheEvictArgs {
+  CacheArgs c;
+  const float* weights;      // [num_seqs][hkv][slots]
+  const int32_t* next_pos;   // [num_seqs] or nullptr: lens
+  int32_t budget, sinks, recent;
+  float* weights_out;        // [num_seqs][hkv][slots]
+  int32_t* pos_out;          // the same
+  int32_t* lens_out;         // [num_seqs]
+  int32_t* moves;            // [num_seqs][hkv][slots]: free slots from the front on, the slots
+                             // that move there from slots / 2 on
+  int32_t* num_moves;        // [num_seqs][hkv]
+};
+hipError_t launch_cache_evict(const CacheEvictArgs& a, int row_bytes, hipStream_t stream);
 
 }  // namespace sift
