@@ -77,6 +77,26 @@ __device__ __forceinline__ Place find_work(const CacheArgs& a, int64_t x, Cost c
   return Place{a.num_seqs, before};
 }
 
+// The sequence that new token `token` belongs to (num_seqs: none), and its first
+// step.
+template <typename Cost>
+__device__ __forceinline__ Place find_token(const CacheArgs& a, int token, Cost cost) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
+    const bool in = b0 + lane < a.num_seqs;
+    const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
+    const int64_t mine = in ? cost(s) : 0;
+    const uint64_t has = __ballot(in && token >= s.row0 && token < s.row0 + s.n);
+    if (has != 0) {
+      const int l = __ffsll(static_cast<unsigned long long>(has)) - 1;
+      return Place{b0 + l, before + wave_sum(lane < l ? mine : 0)};
+    }
+    before += wave_sum(mine);
+  }
+  return Place{a.num_seqs, before};
+}
+
 // Steps x of [0, total) go to workgroup share_of(x): workgroup i takes those
 // from share(i) to share(i + 1).  groups <= total: every workgroup has some.
 __device__ __forceinline__ int64_t share(int64_t i, int64_t total, int64_t groups) {

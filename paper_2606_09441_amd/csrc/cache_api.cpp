@@ -93,7 +93,7 @@ sift_status check_rows(const sift_cache* c, const sift_cache_rows* r, const sift
   if (a->row_ptr == nullptr &&
       (rows % c->num_seqs != 0 || rows / c->num_seqs > c->max_rows))
     return SIFT_E_SHAPE;
-  if (static_cast<int64_t>(rows) * c->hq > int64_t(1) << 26) return SIFT_E_CAPACITY;
+  if (static_cast<int64_t>(rows) * c->hq >= int64_t(1) << 24) return SIFT_E_CAPACITY;
   a->rows = rows;
   a->max_rows = c->max_rows;
   a->q = q->data;

@@ -285,67 +285,69 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   }
 }
 
-// Merge of the parts of one (new token, query head), a wavefront each: lane l
-// takes dims l D / 64 and on.
+// Merge of the parts of one (new token, query head), a workgroup each: eight
+// groups of 32 lanes take every eighth part, lane l dims l D / 32 and on.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
   const CacheArgs& a = p.c;
+  constexpr int kDims = D / 32;
+  __shared__ float acc[8][D];
+  __shared__ float part[8][2];
   const int g = a.hq / a.hkv;
   const UnitCost cost{g, a.hkv};
-  const int lane = threadIdx.x & 63;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  if (item >= static_cast<int64_t>(a.rows) * a.hq) return;
+  const int64_t item = blockIdx.x;
   const int token = static_cast<int>(item / a.hq), h = static_cast<int>(item % a.hq);
   const int64_t total = total_work(a, cost);
   if (total == 0) return;
   const int64_t groups = min(static_cast<int64_t>(p.groups), total);
-  // the token's sequence, and its first step
-  int64_t before = 0;
-  for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
-    const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
-    const bool in = b0 + lane < a.num_seqs;
-    const int64_t mine = in ? cost(s) : 0;
-    int64_t upto = mine;
+  const Place pl = find_token(a, token, cost);
+  if (pl.b >= a.num_seqs) return;  // no sequence's
+  const Seq s = sequence(a, pl.b);
+  const int steps = cost.steps(s);
+  const int r = (token - s.row0) * g + h % g;
+  const int64_t u0 =
+      pl.at + static_cast<int64_t>(h / g * cost.blocks(s) + r / kCacheRows) * steps;
+  const int64_t first = share_of(u0, total, groups);
+  const int n = static_cast<int>(share_of(u0 + steps - 1, total, groups) - first) + 1;
+  if (n == 1) return;  // written already
+  // the first part is its workgroup's second, the others their workgroups' first
+  const auto slot = [&](int i) {
+    return (2 * (first + i) + (i == 0)) * kCacheRows + r % kCacheRows;
+  };
+  float top = -INFINITY;
+  for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p.part_ml[slot(i)].x);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
-    }
-    uint64_t has = __ballot(in && token >= s.row0 && token < s.row0 + s.n);
-    for (; has != 0; has &= has - 1) {
-      const int l = __ffsll(static_cast<unsigned long long>(has)) - 1;
-      const int steps = __shfl(cost.steps(s), l), blocks = __shfl(cost.blocks(s), l);
-      const int row0 = __shfl(s.row0, l);
-      const int r = (token - row0) * g + h % g;
-      const int unit = h / g * blocks + r / kCacheRows;
-      const int64_t u0 = before + __shfl(upto - mine, l) + static_cast<int64_t>(unit) * steps;
-      const int64_t first = share_of(u0, total, groups);
-      const int64_t last = share_of(u0 + steps - 1, total, groups);
-      if (first == last) continue;  // written already
-      const int row = r % kCacheRows;
-      const auto slot = [&](int64_t w) { return (2 * w + (w == first)) * kCacheRows + row; };
-      float top = -INFINITY;
-      for (int64_t w = first + lane; w <= last; w += 64) top = fmaxf(top, p.part_ml[slot(w)].x);
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const int grp = threadIdx.x >> 5, l32 = threadIdx.x & 31;
+  float l = 0.f, le = 0.f, o[kDims] = {};
+#pragma unroll 4
+  for (int i = grp; i < n; i += 8) {
+    const float4 ml = p.part_ml[slot(i)];
+    const float* src = p.part_o + slot(i) * D + l32 * kDims;
+    const float wt = part_weight(ml.x, top);
+    l += ml.y * wt;
+    le += ml.z * wt;
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-      float lsum = 0.f, le = 0.f, o[D / 64] = {};
-      for (int64_t w = first; w <= last; ++w) {
-        const float4 ml = p.part_ml[slot(w)];
-        const float wt = part_weight(ml.x, top);
-        lsum += ml.y * wt;
-        le += ml.z * wt;
-        const float* src = p.part_o + slot(w) * D + lane * (D / 64);
-#pragma unroll
-        for (int e = 0; e < D / 64; ++e) o[e] += src[e] * wt;
-      }
-      const float inv = inverse(lsum);
-      T* dst = static_cast<T*>(p.out) + item * D + lane * (D / 64);
-#pragma unroll
-      for (int e = 0; e < D / 64; ++e) dst[e] = static_cast<T>(o[e] * inv);
-      if (p.lse != nullptr && lane == 0) p.lse[item] = log_sum(top, le);
-    }
-    before += __shfl(upto, 63);
+    for (int e = 0; e < kDims; ++e) o[e] += src[e] * wt;
   }
+#pragma unroll
+  for (int e = 0; e < kDims; ++e) acc[grp][l32 * kDims + e] = o[e];
+  if (l32 == 0) {
+    part[grp][0] = l;
+    part[grp][1] = le;
+  }
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  float y = 0.f;
+  l = le = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y += acc[i][threadIdx.x];
+    l += part[i][0];
+    le += part[i][1];
+  }
+  static_cast<T*>(p.out)[item * D + threadIdx.x] = static_cast<T>(y * inverse(l));
+  if (p.lse != nullptr && threadIdx.x == 0) p.lse[item] = log_sum(top, le);
 }
 
 }  // namespace
@@ -353,15 +355,14 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream) {
   if (a.c.rows == 0) return hipSuccess;
   const int64_t items = static_cast<int64_t>(a.c.rows) * a.c.hq;
-  const int64_t merge = (items + 3) / 4;
-  if (merge >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
+  if (items >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
     hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), dim3(256), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3(static_cast<unsigned>(merge)), dim3(256),
+    hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3(static_cast<unsigned>(items)), dim3(256),
                        0, stream, a);
     return hipGetLastError();
   };

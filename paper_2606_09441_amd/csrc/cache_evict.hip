@@ -28,64 +28,110 @@ __device__ __forceinline__ uint32_t rank_of(float w, bool safe) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One workgroup selects for a (sequence, kv head).  The n-th largest rank is
-// found by four 8-bit digits, each a histogram over the slots that share the
-// digits before; equal ranks go to the lowest slots.  Wavefront w then walks the
-// slots of its own sixteenth in order, so that counts before it give every kept
-// and every free slot its number.
+// The weight order of one (sequence, kv head)'s slots.
+struct Ranks {
+  const CacheEvictArgs& p;
+  int64_t at0;
+  int b, len, page, next;
+  __device__ __forceinline__ Ranks(const CacheEvictArgs& args, int head)
+      : p(args), at0(static_cast<int64_t>(head) * (args.c.max_pages << args.c.page_shift)),
+        b(head / args.c.hkv), page(1 << args.c.page_shift) {
+    len = min(max(p.c.lens[b], 0), p.c.max_pages << p.c.page_shift);
+    next = p.next_pos != nullptr ? p.next_pos[b] : len;
+  }
+  __device__ __forceinline__ int pos(int i) const {
+    return p.c.key_pos != nullptr ? p.c.key_pos[at0 + i] : i;
+  }
+  __device__ __forceinline__ bool used(int i) const {
+    return p.c.page_lens == nullptr ||
+           (i & (page - 1)) <
+               p.c.page_lens[static_cast<int64_t>(b) * p.c.max_pages + (i >> p.c.page_shift)];
+  }
+  __device__ __forceinline__ uint32_t rank(int i) const {
+    const int at = pos(i);
+    const bool safe =
+        at < p.sinks || static_cast<int64_t>(at) >= static_cast<int64_t>(next) - p.recent;
+    return used(i) ? rank_of(p.weights[at0 + i], safe) : 0u;
+  }
+};
+
+// Ranks of the slots i0 + 64 e + lane of a wavefront, in registers (kPer > 0: at
+// most that many to a lane), or made again each time they are asked for.
+template <int kPer>
+struct Held {
+  uint32_t r[kPer];
+  __device__ __forceinline__ void load(const Ranks& x, int i0, int i1, int lane) {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = i0 + 64 * e + lane;
+      const uint32_t y = x.rank(min(i, x.len - 1));  // (no branch: all loads in flight at once)
+      r[e] = i < i1 ? y : 0u;
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(const Ranks&, int i0, int i1, int lane, F f) const {
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if (i0 + 64 * e < i1) f(i0 + 64 * e, r[e]);
+  }
+};
+template <>
+struct Held<0> {
+  __device__ __forceinline__ void load(const Ranks&, int, int, int) {}
+  template <typename F>
+  __device__ __forceinline__ void each(const Ranks& x, int i0, int i1, int lane, F f) const {
+    for (int i = i0; i < i1; i += 64) f(i, i + lane < i1 ? x.rank(i + lane) : 0u);
+  }
+};
+
+constexpr int kCopies = 16;  // of the histogram: lanes of one digit rarely meet
+
+// One workgroup selects for a (sequence, kv head); a wavefront takes a sixteenth
+// of the slots, consecutive ones.  The n-th largest rank is found by four 8-bit
+// digits, each a histogram over the slots that share the digits before; equal
+// ranks go to the lowest slots.  Counts of the wavefronts before then give every
+// kept and every free slot its number.  Bound by one CU's reading and LDS
+// atomics; the ranks stay in registers, since a walk over memory costs a round
+// trip for every 1024 slots.
+template <int kPer>
 __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p) {
-  const CacheArgs& a = p.c;
-  __shared__ int hist[256];
+  __shared__ int hist[256 * kCopies];
+  __shared__ int sums[256];
   __shared__ int wave_cnt[kSelWaves][3];
   __shared__ int digit, above;
-  const int b = blockIdx.x / a.hkv;
-  const int slots = a.max_pages << a.page_shift;
-  const int page = 1 << a.page_shift;
-  const int len = min(max(a.lens[b], 0), slots);
-  const int64_t at0 = static_cast<int64_t>(blockIdx.x) * slots;
-  const int next = p.next_pos != nullptr ? p.next_pos[b] : len;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Ranks x(p, blockIdx.x);
+  const int slots = p.c.max_pages << p.c.page_shift;
+  const int len = x.len;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const uint64_t before = (uint64_t(1) << lane) - 1;
+  const int per = (len + kThreads - 1) / kThreads * 64;  // slots of a wavefront
+  const int i0 = min(len, wave * per), i1 = min(len, i0 + per);
+  Held<kPer> held;
+  if (len > 0) held.load(x, i0, i1, lane);
 
-  const auto pos_at = [&](int i) { return a.key_pos != nullptr ? a.key_pos[at0 + i] : i; };
-  const auto rank = [&](int i) -> uint32_t {
-    if (a.page_lens != nullptr &&
-        (i & (page - 1)) >= a.page_lens[static_cast<int64_t>(b) * a.max_pages + (i >> a.page_shift)])
-      return 0u;
-    const int pos = pos_at(i);
-    return rank_of(p.weights[at0 + i],
-                   pos < p.sinks || static_cast<int64_t>(pos) >= static_cast<int64_t>(next) - p.recent);
-  };
-
-  // the digits of the n-th largest rank
-  uint32_t prefix = 0;
+  uint32_t prefix = 0;  // the digits of the n-th largest rank
   int keep = 0, want = 0;
   for (int shift = 24; shift >= 0; shift -= 8) {
-    if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < 256 * kCopies; i += kThreads) hist[i] = 0;
     __syncthreads();
-    int keys = 0;
-    for (int i = threadIdx.x; i < len; i += kThreads) {
-      const uint32_t r = rank(i);
-      keys += r != 0;
-      if (shift == 24 ? r != 0 : (r >> (shift + 8)) == prefix) atomicAdd(&hist[(r >> shift) & 255], 1);
-    }
-    if (shift == 24) {
+    held.each(x, i0, i1, lane, [&](int, uint32_t r) {
+      const bool in = r != 0u && (shift == 24 || (r >> (shift + 8)) == prefix);
+      if (in) atomicAdd(&hist[((r >> shift) & 255) * kCopies + lane % kCopies], 1);
+    });
+    __syncthreads();
+    if (threadIdx.x < 256) {
+      int c = 0;
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) keys += __shfl_xor(keys, d);
-      if (lane == 0) wave_cnt[wave][0] = keys;
+      for (int e = 0; e < kCopies; ++e) c += hist[threadIdx.x * kCopies + (e + lane) % kCopies];
+      sums[threadIdx.x] = c;
     }
     __syncthreads();
-    if (shift == 24) {
-      int all = 0;
-      for (int w = 0; w < kSelWaves; ++w) all += wave_cnt[w][0];
-      keep = want = min(all, p.budget);
-    }
-    // the first digit from the top where the count reaches what is wanted
     if (wave == 0) {
       // lane l holds digits 255 - 4 l .. 252 - 4 l
       int c[4], mine = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        c[e] = hist[255 - 4 * lane - e];
+        c[e] = sums[255 - 4 * lane - e];
         mine += c[e];
       }
       int upto = mine;
@@ -94,6 +140,8 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
         const int y = __shfl_up(upto, d);
         if (lane >= d) upto += y;
       }
+      if (shift == 24) keep = want = min(__shfl(upto, 63), p.budget);
+      // the first digit from the top where the count reaches what is wanted
       int run = upto - mine;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -103,8 +151,10 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
         }
         run += c[e];
       }
+      if (shift == 24 && lane == 0) wave_cnt[0][0] = keep;
     }
     __syncthreads();
+    if (shift == 24) keep = want = wave_cnt[0][0];
     if (want > 0) {
       prefix = prefix << 8 | static_cast<uint32_t>(digit);
       want -= above;
@@ -113,34 +163,32 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
   }
   // kept: ranks above `prefix`, and the first `want` slots of that rank
 
-  const int per = (len + kSelWaves * 64 - 1) / (kSelWaves * 64) * 64;  // slots of a wavefront
-  const int i0 = min(len, wave * per), i1 = min(len, i0 + per);
   int ties = 0;
   if (keep > 0)
-    for (int i = i0 + lane; i < i1; i += 64) ties += rank(i) == prefix;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) ties += __shfl_xor(ties, d);
+    held.each(x, i0, i1, lane, [&](int, uint32_t r) { ties += __popcll(__ballot(r == prefix)); });
   if (lane == 0) wave_cnt[wave][0] = ties;
   __syncthreads();
   int ties_before = 0;
   for (int w = 0; w < wave; ++w) ties_before += wave_cnt[w][0];
 
-  // `each`(slot, in range, kept), in slot order
-  const auto walk = [&](auto each) {
+  // `f`(first slot of 64, mask of the kept ones), in slot order
+  const auto walk = [&](auto f) {
     int seen = ties_before;
-    for (int i = i0 + lane; i - lane < i1; i += 64) {
-      const uint32_t r = i < i1 && keep > 0 ? rank(i) : 0u;
-      const bool tie = r != 0u && r == prefix;
+    held.each(x, i0, i1, lane, [&](int i, uint32_t r) {
+      const bool tie = keep > 0 && r == prefix;  // (prefix is not 0 then: a key's rank)
       const uint64_t mask = __ballot(tie);
-      const int place = seen + __popcll(mask & ((uint64_t(1) << lane) - 1));
-      each(i, i < i1, r > prefix || (tie && place < want));
+      const bool kept =
+          keep > 0 && (r > prefix || (tie && seen + __popcll(mask & before) < want));
       seen += __popcll(mask);
-    }
+      f(i, __ballot(kept));
+    });
   };
+  // of 64 slots from i on: those before slot `keep`, and those that exist
+  const auto low = [&](int i) { return low_bits(keep - i); };
   int moved = 0, free = 0;
-  walk([&](int i, bool in, bool kept) {
-    moved += __popcll(__ballot(in && kept && i >= keep));
-    free += __popcll(__ballot(in && !kept && i < keep));
+  walk([&](int i, uint64_t kept) {
+    moved += __popcll(kept & ~low(i));
+    free += __popcll(~kept & low(i) & low_bits(i1 - i));
   });
   if (lane == 0) {
     wave_cnt[wave][1] = moved;
@@ -156,40 +204,29 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
     }
     all_moved += wave_cnt[w][1];
   }
-  int32_t* holes = p.moves + at0;
+  int32_t* holes = p.moves + x.at0;
   int32_t* from = holes + slots / 2;
-  walk([&](int i, bool in, bool kept) {
-    const uint64_t before = (uint64_t(1) << lane) - 1;
-    const bool goes = in && kept && i >= keep, hole = in && !kept && i < keep;
-    const uint64_t gm = __ballot(goes), hm = __ballot(hole);
-    if (goes) from[moved + __popcll(gm & before)] = i;
-    if (hole) holes[free + __popcll(hm & before)] = i;
-    if (in && kept && i < keep) {
-      p.weights_out[at0 + i] = p.weights[at0 + i];
-      p.pos_out[at0 + i] = pos_at(i);
+  walk([&](int i, uint64_t kept) {
+    const uint64_t goes = kept & ~low(i), hole = ~kept & low(i) & low_bits(i1 - i);
+    if ((goes >> lane) & 1) from[moved + __popcll(goes & before)] = i + lane;
+    if ((hole >> lane) & 1) holes[free + __popcll(hole & before)] = i + lane;
+    if (((kept & low(i)) >> lane) & 1) {
+      p.weights_out[x.at0 + i + lane] = p.weights[x.at0 + i + lane];
+      p.pos_out[x.at0 + i + lane] = x.pos(i + lane);
     }
-    moved += __popcll(gm);
-    free += __popcll(hm);
+    moved += __popcll(goes);
+    free += __popcll(hole);
   });
-  __syncthreads();
-  for (int j = threadIdx.x; j < all_moved; j += kThreads) {
-    const int to = holes[j], i = from[j];
-    p.weights_out[at0 + to] = p.weights[at0 + i];
-    p.pos_out[at0 + to] = pos_at(i);
-  }
-  for (int i = keep + threadIdx.x; i < slots; i += kThreads) {
-    p.weights_out[at0 + i] = 0.f;
-    p.pos_out[at0 + i] = -1;
-  }
   if (threadIdx.x == 0) {
     p.num_moves[blockIdx.x] = all_moved;
-    if (blockIdx.x % a.hkv == 0) p.lens_out[b] = keep;
+    if (blockIdx.x % p.c.hkv == 0) p.lens_out[x.b] = keep;
   }
 }
 
 constexpr int kMoveRows = 64;  // rows of a workgroup
 
-// kRow bytes a row: kRow / 16 lanes each.
+// The moves of a (sequence, kv head), kMoveRows of them a workgroup, kRow / 16
+// lanes a row; the slots past the kept ones are cleared on the side.
 template <int kRow>
 __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int per_head) {
   const CacheArgs& a = p.c;
@@ -198,8 +235,14 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int p
   const int64_t head = blockIdx.x / per_head;
   const int j0 = static_cast<int>(blockIdx.x % per_head) * kMoveRows;
   const int n = p.num_moves[head];
-  if (j0 >= n) return;
   const int b = static_cast<int>(head / a.hkv), kvh = static_cast<int>(head % a.hkv);
+  const int64_t at0 = head * slots;
+  for (int i = p.lens_out[b] + static_cast<int>(blockIdx.x % per_head) * 256 + threadIdx.x;
+       i < slots; i += per_head * 256) {
+    p.weights_out[at0 + i] = 0.f;
+    p.pos_out[at0 + i] = -1;
+  }
+  if (j0 >= n) return;
   const int32_t* holes = p.moves + head * slots;
   const int32_t* from = holes + slots / 2;
   const auto row = [&](int slot) {
@@ -209,7 +252,12 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int p
   };
   const int ch = threadIdx.x % kLanes;
   for (int j = j0 + threadIdx.x / kLanes; j < min(n, j0 + kMoveRows); j += 256 / kLanes) {
-    const int64_t to = row(holes[j]) + 16 * ch, src = row(from[j]) + 16 * ch;
+    const int hole = holes[j], slot = from[j];
+    const int64_t to = row(hole) + 16 * ch, src = row(slot) + 16 * ch;
+    if (ch == 0) {
+      p.weights_out[at0 + hole] = p.weights[at0 + slot];
+      p.pos_out[at0 + hole] = a.key_pos != nullptr ? a.key_pos[at0 + slot] : slot;
+    }
     uint8_t* k = static_cast<uint8_t*>(const_cast<void*>(a.k));
     uint8_t* v = static_cast<uint8_t*>(const_cast<void*>(a.v));
     const u32x4 x = *reinterpret_cast<const u32x4*>(k + src);
@@ -228,8 +276,16 @@ hipError_t launch_cache_evict(const CacheEvictArgs& a, int row_bytes, hipStream_
   const int64_t per = std::max<int64_t>(1, (most + kMoveRows - 1) / kMoveRows);
   // grids of fewer than 2^32 threads
   if (heads >= int64_t(1) << 22 || heads * per >= int64_t(1) << 24) return hipErrorInvalidValue;
-  hipLaunchKernelGGL(cache_select_kernel, dim3(static_cast<unsigned>(heads)), dim3(kThreads), 0,
-                     stream, a);
+  const dim3 sel(static_cast<unsigned>(heads)), threads(kThreads);
+  // slots in registers, 1024 to a unit; beyond 72 of them from memory
+  if (slots <= 4 * kThreads)
+    hipLaunchKernelGGL((cache_select_kernel<4>), sel, threads, 0, stream, a);
+  else if (slots <= 20 * kThreads)
+    hipLaunchKernelGGL((cache_select_kernel<20>), sel, threads, 0, stream, a);
+  else if (slots <= 72 * kThreads)
+    hipLaunchKernelGGL((cache_select_kernel<72>), sel, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL((cache_select_kernel<0>), sel, threads, 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid(static_cast<unsigned>(heads * per)), block(256);
