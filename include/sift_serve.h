@@ -188,7 +188,7 @@ sift_status sift_cache_accumulate(sift_cache* cache, const sift_cache_kv* kv,
  * The pages of the first `budget` slots must be the sequence's own.
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE (budget, sinks, recent), SIFT_E_UNSUPPORTED
  *   (overlap, alignment), SIFT_E_CAPACITY (2^22 (sequence, kv head) pairs or
- *   more, 2^30 moves or more), SIFT_E_PLAN, SIFT_E_HIP.
+ *   more, 2^33 slots of all of them or more), SIFT_E_PLAN, SIFT_E_HIP.
  */
 sift_status sift_cache_evict(sift_cache* cache, const sift_cache_kv* kv, const float* weights,
                              const int32_t* next_pos, int32_t budget, int32_t sinks,

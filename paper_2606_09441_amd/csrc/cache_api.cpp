@@ -25,6 +25,9 @@ struct sift_cache {
   float4* part_ml = nullptr;
   int32_t* moves = nullptr;      // of the eviction (CacheEvictArgs)
   int32_t* num_moves = nullptr;
+  int32_t* hist = nullptr;
+  int4* state = nullptr;
+  int4* counts = nullptr;
   hipStream_t last_stream = nullptr;  // the stream of the last enqueued work
 };
 
@@ -159,12 +162,23 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
   };
   const size_t o_o = place(o_bytes), o_ml = place(rows * sizeof(float4));
   const size_t o_moves = place(moves * sizeof(int32_t)), o_num = place(heads * sizeof(int32_t));
+  const size_t units = static_cast<size_t>(
+      sift::evict_units(static_cast<int64_t>(max_pages) * page));
+  const size_t hist_bytes = heads * sift::kEvictHist * sizeof(int32_t);
+  const size_t o_hist = place(hist_bytes), o_state = place(heads * 3 * sizeof(int4));
+  const size_t o_counts = place(heads * units * sizeof(int4));
   if (hipMalloc(&c->dev, at) != hipSuccess) return fail();
   uint8_t* base = static_cast<uint8_t*>(c->dev);
   c->part_o = reinterpret_cast<float*>(base + o_o);
   c->part_ml = reinterpret_cast<float4*>(base + o_ml);
   c->moves = reinterpret_cast<int32_t*>(base + o_moves);
   c->num_moves = reinterpret_cast<int32_t*>(base + o_num);
+  c->hist = reinterpret_cast<int32_t*>(base + o_hist);
+  c->state = reinterpret_cast<int4*>(base + o_state);
+  c->counts = reinterpret_cast<int4*>(base + o_counts);
+  if (hipMemset(c->hist, 0, hist_bytes) != hipSuccess ||
+      hipStreamSynchronize(nullptr) != hipSuccess)
+    return fail();
   *cache_out = c;
   return SIFT_OK;
 }
@@ -258,8 +272,7 @@ sift_status sift_cache_evict(sift_cache* cache, const sift_cache_kv* kv, const f
   const size_t small = static_cast<size_t>(cache->num_seqs) * 4;
   if (overlap(lens_out, kv->lens, small) || overlap(lens_out, next_pos, small))
     return SIFT_E_UNSUPPORTED;
-  if (heads >= int64_t(1) << 22 || heads * std::min<int64_t>(budget, slots / 2) >= int64_t(1) << 30)
-    return SIFT_E_CAPACITY;
+  if (heads >= int64_t(1) << 22 || heads * slots >= int64_t(1) << 33) return SIFT_E_CAPACITY;
   a.weights = weights;
   a.next_pos = next_pos;
   a.budget = budget;
@@ -270,6 +283,9 @@ sift_status sift_cache_evict(sift_cache* cache, const sift_cache_kv* kv, const f
   a.lens_out = lens_out;
   a.moves = cache->moves;
   a.num_moves = cache->num_moves;
+  a.hist = cache->hist;
+  a.state = cache->state;
+  a.counts = cache->counts;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const int row = cache->head_dim * (kv->k_pages->dtype == SIFT_BF16 ? 2 : 4);
   const hipError_t e = sift::launch_cache_evict(a, row, s);

@@ -7,6 +7,7 @@
 // be.  The order of a cache's slots means nothing; positions move along.
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 #include "sift_internal.h"
@@ -32,12 +33,14 @@ __device__ __forceinline__ uint32_t rank_of(float w, bool safe) {
 struct Ranks {
   const CacheEvictArgs& p;
   int64_t at0;
-  int b, len, page, next;
+  int b, len, page;
+  int late;  // the first position that is protected as recent
   __device__ __forceinline__ Ranks(const CacheEvictArgs& args, int head)
       : p(args), at0(static_cast<int64_t>(head) * (args.c.max_pages << args.c.page_shift)),
         b(head / args.c.hkv), page(1 << args.c.page_shift) {
     len = min(max(p.c.lens[b], 0), p.c.max_pages << p.c.page_shift);
-    next = p.next_pos != nullptr ? p.next_pos[b] : len;
+    const int64_t next = p.next_pos != nullptr ? p.next_pos[b] : len;
+    late = static_cast<int>(max(next - p.recent, static_cast<int64_t>(-0x7fffffff)));
   }
   __device__ __forceinline__ int pos(int i) const {
     return p.c.key_pos != nullptr ? p.c.key_pos[at0 + i] : i;
@@ -49,80 +52,84 @@ struct Ranks {
   }
   __device__ __forceinline__ uint32_t rank(int i) const {
     const int at = pos(i);
-    const bool safe =
-        at < p.sinks || static_cast<int64_t>(at) >= static_cast<int64_t>(next) - p.recent;
-    return used(i) ? rank_of(p.weights[at0 + i], safe) : 0u;
+    return used(i) ? rank_of(p.weights[at0 + i], at < p.sinks || at >= late) : 0u;
   }
 };
 
-// Ranks of the slots i0 + 64 e + lane of a wavefront, in registers (kPer > 0: at
-// most that many to a lane), or made again each time they are asked for.
-template <int kPer>
-struct Held {
-  uint32_t r[kPer];
-  __device__ __forceinline__ void load(const Ranks& x, int i0, int i1, int lane) {
-#pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-      const int i = i0 + 64 * e + lane;
-      const uint32_t y = x.rank(min(i, x.len - 1));  // (no branch: all loads in flight at once)
-      r[e] = i < i1 ? y : 0u;
+// The numbers that a wavefront has got to: ties seen, rows that move, free slots.
+struct Counts {
+  int ties, moved, free;
+};
+
+// Lists what 64 consecutive slots from i on hold, given the masks of the ranks
+// above the n-th and of those equal to it, of which the first `want` are kept.
+struct Places {
+  const CacheEvictArgs& p;
+  const Ranks& x;
+  int keep, want;
+  __device__ __forceinline__ void list(int i, int lane, uint64_t kept, uint64_t tie,
+                                       Counts& c) const {
+    const uint64_t before = (uint64_t(1) << lane) - 1;
+    int32_t* holes = p.moves + x.at0;
+    int32_t* from = holes + (p.c.max_pages << p.c.page_shift) / 2;
+    kept |= __ballot(((tie >> lane) & 1) && c.ties + __popcll(tie & before) < want);
+    c.ties += __popcll(tie);
+    const uint64_t m = low_bits(keep - i), goes = kept & ~m, hole = ~kept & m;
+    if ((goes >> lane) & 1) from[c.moved + __popcll(goes & before)] = i + lane;
+    if ((hole >> lane) & 1) holes[c.free + __popcll(hole & before)] = i + lane;
+    c.moved += __popcll(goes);
+    c.free += __popcll(hole);
+    // what stays, stays; the free slots among these are written with the moves
+    if (i + lane < keep) {
+      p.weights_out[x.at0 + i + lane] = p.weights[x.at0 + i + lane];
+      p.pos_out[x.at0 + i + lane] = x.pos(i + lane);
     }
   }
-  template <typename F>
-  __device__ __forceinline__ void each(const Ranks&, int i0, int i1, int lane, F f) const {
-#pragma unroll
-    for (int e = 0; e < kPer; ++e)
-      if (i0 + 64 * e < i1) f(i0 + 64 * e, r[e]);
-  }
-};
-template <>
-struct Held<0> {
-  __device__ __forceinline__ void load(const Ranks&, int, int, int) {}
-  template <typename F>
-  __device__ __forceinline__ void each(const Ranks& x, int i0, int i1, int lane, F f) const {
-    for (int i = i0; i < i1; i += 64) f(i, i + lane < i1 ? x.rank(i + lane) : 0u);
-  }
 };
 
-constexpr int kCopies = 16;  // of the histogram: lanes of one digit rarely meet
+constexpr int kCopies = 8;       // of the histogram: lanes of one digit rarely meet
+constexpr int kHeld = 8;         // ranks of a lane
+constexpr int kSelectSlots = kHeld * kThreads;  // longest cache of one workgroup
 
-// One workgroup selects for a (sequence, kv head); a wavefront takes a sixteenth
-// of the slots, consecutive ones.  The n-th largest rank is found by four 8-bit
-// digits, each a histogram over the slots that share the digits before; equal
-// ranks go to the lowest slots.  Counts of the wavefronts before then give every
-// kept and every free slot its number.  Bound by one CU's reading and LDS
-// atomics; the ranks stay in registers, since a walk over memory costs a round
-// trip for every 1024 slots.
-template <int kPer>
+// One workgroup selects for a (sequence, kv head) of up to kSelectSlots slots,
+// the ranks in registers; a wavefront has a sixteenth of the slots, consecutive
+// ones.  The n-th largest rank is found by four 8-bit digits, each a histogram
+// over the slots that share the digits before; equal ranks go to the lowest
+// slots.  Counts of the wavefronts before then give every kept and every free
+// slot its number.
 __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p) {
   __shared__ int hist[256 * kCopies];
   __shared__ int sums[256];
-  __shared__ int wave_cnt[kSelWaves][3];
-  __shared__ int digit, above;
+  __shared__ int counts[kSelWaves][4];
+  __shared__ int digit, above, found;
   const Ranks x(p, blockIdx.x);
-  const int slots = p.c.max_pages << p.c.page_shift;
   const int len = x.len;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const uint64_t before = (uint64_t(1) << lane) - 1;
   const int per = (len + kThreads - 1) / kThreads * 64;  // slots of a wavefront
   const int i0 = min(len, wave * per), i1 = min(len, i0 + per);
-  Held<kPer> held;
-  if (len > 0) held.load(x, i0, i1, lane);
+  uint32_t r[kHeld];
+#pragma unroll
+  for (int e = 0; e < kHeld; ++e) {
+    const int i = i0 + 64 * e + lane;
+    r[e] = len > 0 ? x.rank(min(i, len - 1)) : 0u;
+    if (i >= i1) r[e] = 0u;
+  }
 
   uint32_t prefix = 0;  // the digits of the n-th largest rank
   int keep = 0, want = 0;
+#pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = threadIdx.x; i < 256 * kCopies; i += kThreads) hist[i] = 0;
     __syncthreads();
-    held.each(x, i0, i1, lane, [&](int, uint32_t r) {
-      const bool in = r != 0u && (shift == 24 || (r >> (shift + 8)) == prefix);
-      if (in) atomicAdd(&hist[((r >> shift) & 255) * kCopies + lane % kCopies], 1);
-    });
+#pragma unroll
+    for (int e = 0; e < kHeld; ++e)
+      if (r[e] != 0u && (shift == 24 || (r[e] >> (shift + 8)) == prefix))
+        atomicAdd(&hist[((r[e] >> shift) & 255) * kCopies + lane % kCopies], 1);
     __syncthreads();
     if (threadIdx.x < 256) {
       int c = 0;
 #pragma unroll
-      for (int e = 0; e < kCopies; ++e) c += hist[threadIdx.x * kCopies + (e + lane) % kCopies];
+      for (int e = 0; e < kCopies; ++e) c += hist[threadIdx.x * kCopies + (e + lane / 8) % kCopies];
       sums[threadIdx.x] = c;
     }
     __syncthreads();
@@ -135,12 +142,14 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
         mine += c[e];
       }
       int upto = mine;
-#pragma unroll
       for (int d = 1; d < 64; d <<= 1) {
         const int y = __shfl_up(upto, d);
         if (lane >= d) upto += y;
       }
-      if (shift == 24) keep = want = min(__shfl(upto, 63), p.budget);
+      if (shift == 24) {
+        want = min(__shfl(upto, 63), p.budget);
+        if (lane == 0) found = want;
+      }
       // the first digit from the top where the count reaches what is wanted
       int run = upto - mine;
 #pragma unroll
@@ -151,98 +160,252 @@ __global__ __launch_bounds__(kThreads) void cache_select_kernel(CacheEvictArgs p
         }
         run += c[e];
       }
-      if (shift == 24 && lane == 0) wave_cnt[0][0] = keep;
     }
     __syncthreads();
-    if (shift == 24) keep = want = wave_cnt[0][0];
+    if (shift == 24) keep = want = found;
     if (want > 0) {
       prefix = prefix << 8 | static_cast<uint32_t>(digit);
       want -= above;
     }
-    __syncthreads();
   }
   // kept: ranks above `prefix`, and the first `want` slots of that rank
 
-  int ties = 0;
-  if (keep > 0)
-    held.each(x, i0, i1, lane, [&](int, uint32_t r) { ties += __popcll(__ballot(r == prefix)); });
-  if (lane == 0) wave_cnt[wave][0] = ties;
-  __syncthreads();
-  int ties_before = 0;
-  for (int w = 0; w < wave; ++w) ties_before += wave_cnt[w][0];
-
-  // `f`(first slot of 64, mask of the kept ones), in slot order
-  const auto walk = [&](auto f) {
-    int seen = ties_before;
-    held.each(x, i0, i1, lane, [&](int i, uint32_t r) {
-      const bool tie = keep > 0 && r == prefix;  // (prefix is not 0 then: a key's rank)
-      const uint64_t mask = __ballot(tie);
-      const bool kept =
-          keep > 0 && (r > prefix || (tie && seen + __popcll(mask & before) < want));
-      seen += __popcll(mask);
-      f(i, __ballot(kept));
-    });
+  const auto masks = [&](int e, uint64_t& kept, uint64_t& tie) {
+    kept = __ballot(keep > 0 && r[e] > prefix);
+    tie = __ballot(keep > 0 && r[e] == prefix);  // (prefix is a key's rank then, not 0)
   };
-  // of 64 slots from i on: those before slot `keep`, and those that exist
+  // of 64 slots from i on, those before slot `keep`
   const auto low = [&](int i) { return low_bits(keep - i); };
-  int moved = 0, free = 0;
-  walk([&](int i, uint64_t kept) {
-    moved += __popcll(kept & ~low(i));
-    free += __popcll(~kept & low(i) & low_bits(i1 - i));
-  });
-  if (lane == 0) {
-    wave_cnt[wave][1] = moved;
-    wave_cnt[wave][2] = free;
+  int n[4] = {0, 0, 0, 0};  // kept and ties, before slot `keep` and from it on
+#pragma unroll
+  for (int e = 0; e < kHeld; ++e) {
+    uint64_t kept, tie;
+    masks(e, kept, tie);
+    const uint64_t m = low(i0 + 64 * e);
+    n[0] += __popcll(kept & m);
+    n[1] += __popcll(tie & m);
+    n[2] += __popcll(kept & ~m);
+    n[3] += __popcll(tie & ~m);
   }
+  if (lane < 4) counts[wave][lane] = lane == 0 ? n[0] : lane == 1 ? n[1] : lane == 2 ? n[2] : n[3];
   __syncthreads();
-  moved = free = 0;
-  int all_moved = 0;
-  for (int w = 0; w < kSelWaves; ++w) {
-    if (w < wave) {
-      moved += wave_cnt[w][1];
-      free += wave_cnt[w][2];
+  // of the wavefronts before this one and of all: lanes 0 .. 15 add them up
+  int k0 = 0, t0 = 0, k1 = 0, t1 = 0, all_k1 = 0, all_t0 = 0, all_t = 0;
+  if (lane < kSelWaves) {
+    const int c0 = counts[lane][0], c1 = counts[lane][1], c2 = counts[lane][2],
+              c3 = counts[lane][3];
+    if (lane < wave) {
+      k0 = c0;
+      t0 = c1;
+      k1 = c2;
+      t1 = c3;
     }
-    all_moved += wave_cnt[w][1];
+    all_k1 = c2;
+    all_t0 = c1;
+    all_t = c1 + c3;
   }
-  int32_t* holes = p.moves + x.at0;
-  int32_t* from = holes + slots / 2;
-  walk([&](int i, uint64_t kept) {
-    const uint64_t goes = kept & ~low(i), hole = ~kept & low(i) & low_bits(i1 - i);
-    if ((goes >> lane) & 1) from[moved + __popcll(goes & before)] = i + lane;
-    if ((hole >> lane) & 1) holes[free + __popcll(hole & before)] = i + lane;
-    if (((kept & low(i)) >> lane) & 1) {
-      p.weights_out[x.at0 + i + lane] = p.weights[x.at0 + i + lane];
-      p.pos_out[x.at0 + i + lane] = x.pos(i + lane);
+  for (int d = 8; d > 0; d >>= 1) {
+    k0 += __shfl_xor(k0, d);
+    t0 += __shfl_xor(t0, d);
+    k1 += __shfl_xor(k1, d);
+    t1 += __shfl_xor(t1, d);
+    all_k1 += __shfl_xor(all_k1, d);
+    all_t0 += __shfl_xor(all_t0, d);
+    all_t += __shfl_xor(all_t, d);
+  }
+  const Places at{p, x, keep, want};
+  Counts c{uniform(t0 + t1), uniform(k1 + min(want, t0 + t1) - min(want, t0)),
+           uniform(min(i0, keep) - k0 - min(want, t0))};
+#pragma unroll
+  for (int e = 0; e < kHeld; ++e)
+    if (i0 + 64 * e < i1) {
+      uint64_t kept, tie;
+      masks(e, kept, tie);
+      at.list(i0 + 64 * e, lane, kept, tie, c);
     }
-    moved += __popcll(goes);
-    free += __popcll(hole);
-  });
   if (threadIdx.x == 0) {
-    p.num_moves[blockIdx.x] = all_moved;
+    p.num_moves[blockIdx.x] = all_k1 + min(want, all_t) - min(want, all_t0);
     if (blockIdx.x % p.c.hkv == 0) p.lens_out[x.b] = keep;
   }
 }
 
-constexpr int kMoveRows = 64;  // rows of a workgroup
+// The same for long caches, the slots dealt over workgroups of kPart: one CU
+// needs 0.4 us for every instruction of a walk over 64K slots.  Five launches
+// (digits of 10, 11 and 11 bits, counts, lists), each reads the ranks anew; what
+// they hand on lies in the handle's scratch.  The histograms are zero between
+// calls: a stage clears those that no later one reads.
+constexpr int kPart = 2048;
+constexpr int kPickWaves = 4;
+constexpr int kUnitSlots = kPart / kPickWaves;  // of a wavefront, consecutive ones
 
-// The moves of a (sequence, kv head), kMoveRows of them a workgroup, kRow / 16
-// lanes a row; the slots past the kept ones are cleared on the side.
+__device__ __forceinline__ int* hist_of(const CacheEvictArgs& p, int head, int stage) {
+  constexpr int kFrom[3] = {0, 1024, 1024 + 2048};
+  return p.hist + static_cast<int64_t>(head) * kEvictHist + kFrom[stage];
+}
+
+template <int kStage>
+__global__ __launch_bounds__(64 * kPickWaves) void cache_pick_kernel(CacheEvictArgs p, int parts) {
+  __shared__ int bins[kStage < 3 ? 2048 : 1];
+  __shared__ int tot[kPickWaves], found[2];
+  const int head = blockIdx.x / parts, part = blockIdx.x % parts;
+  const Ranks x(p, head);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int i0 = part * kPart + wave * kUnitSlots + lane;
+  uint32_t r[kUnitSlots / 64];
+#pragma unroll
+  for (int e = 0; e < kUnitSlots / 64; ++e) {
+    const int i = i0 + 64 * e;
+    r[e] = x.len > 0 ? x.rank(min(i, x.len - 1)) : 0u;
+    if (i >= x.len) r[e] = 0u;
+  }
+  // {digits so far, keys of that prefix still wanted, keys kept}
+  int4* state = p.state + 3 * static_cast<int64_t>(head);
+  int4 st = kStage >= 2 ? state[kStage == 4 ? 2 : kStage - 2] : int4{0, 0, 0, 0};
+  if constexpr (kStage >= 1 && kStage <= 3) {
+    // this stage's prefix, from the histogram before: thread t holds kMine bins
+    // from the top
+    constexpr int kMine = (kStage == 1 ? 1024 : 2048) / (64 * kPickWaves);
+    const int* h = hist_of(p, head, kStage - 1);
+    const int first = (kStage == 1 ? 1023 : 2047) - kMine * static_cast<int>(threadIdx.x);
+    int c[kMine], mine = 0;
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) {
+      c[e] = h[first - e];
+      mine += c[e];
+    }
+    int upto = mine;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int y = __shfl_up(upto, d);
+      if (lane >= d) upto += y;
+    }
+    if (lane == 63) tot[wave] = upto;
+    __syncthreads();
+    int all = 0, run = upto - mine;
+    for (int w = 0; w < kPickWaves; ++w) {
+      if (w < wave) run += tot[w];
+      all += tot[w];
+    }
+    if (kStage == 1) st = int4{0, min(all, p.budget), min(all, p.budget), 0};
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) {
+      if (st.y > 0 && run < st.y && run + c[e] >= st.y) {
+        found[0] = first - e;
+        found[1] = run;
+      }
+      run += c[e];
+    }
+    __syncthreads();
+    if (st.y > 0) {
+      st.x = static_cast<int>(static_cast<uint32_t>(st.x) << (kStage == 1 ? 10 : 11) |
+                              static_cast<uint32_t>(found[0]));
+      st.y -= found[1];
+    }
+    if (part == 0 && threadIdx.x == 0) state[kStage - 1] = st;
+  }
+  const uint32_t prefix = static_cast<uint32_t>(st.x);
+  if constexpr (kStage < 3) {
+    for (int i = threadIdx.x; i < 2048; i += 64 * kPickWaves) bins[i] = 0;
+    __syncthreads();
+    constexpr int kShift = kStage == 0 ? 22 : kStage == 1 ? 11 : 0;
+#pragma unroll
+    for (int e = 0; e < kUnitSlots / 64; ++e) {
+      const bool in = r[e] != 0u && (kStage == 0 || (r[e] >> (kStage == 1 ? 22 : 11)) == prefix);
+      if (in) atomicAdd(&bins[(r[e] >> kShift) & (kStage == 0 ? 1023 : 2047)], 1);
+    }
+    __syncthreads();
+    int* h = hist_of(p, head, kStage);
+    for (int i = threadIdx.x; i < (kStage == 0 ? 1024 : 2048); i += 64 * kPickWaves)
+      if (bins[i] != 0) atomicAdd(&h[i], bins[i]);
+    return;
+  }
+  const int keep = st.z, want = st.y;
+  const int unit = part * kPickWaves + wave, units = parts * kPickWaves;
+  int4* counts = p.counts + static_cast<int64_t>(head) * units;
+  const auto low = [&](int i) { return low_bits(keep - i); };
+  const auto masks = [&](int e, uint64_t& kept, uint64_t& tie) {
+    kept = __ballot(keep > 0 && r[e] > prefix);
+    tie = __ballot(keep > 0 && r[e] == prefix);  // (prefix is a key's rank then, not 0)
+  };
+  if constexpr (kStage == 3) {
+    int4 n{0, 0, 0, 0};  // kept and ties, before slot `keep` and from it on
+#pragma unroll
+    for (int e = 0; e < kUnitSlots / 64; ++e) {
+      uint64_t kept, tie;
+      masks(e, kept, tie);
+      const uint64_t m = low(i0 - lane + 64 * e);
+      n.x += __popcll(kept & m);
+      n.y += __popcll(tie & m);
+      n.z += __popcll(kept & ~m);
+      n.w += __popcll(tie & ~m);
+    }
+    if (lane == 0) counts[unit] = n;
+    if (part == 0)
+      for (int i = threadIdx.x; i < 1024 + 2048; i += 64 * kPickWaves) hist_of(p, head, 0)[i] = 0;
+  } else {
+    // of the units before this one, and of all
+    int k0 = 0, t0 = 0, k1 = 0, t1 = 0, all_k1 = 0, all_t0 = 0, all_t = 0;
+    for (int u = lane; u < units; u += 64) {
+      const int4 n = counts[u];
+      if (u < unit) {
+        k0 += n.x;
+        t0 += n.y;
+        k1 += n.z;
+        t1 += n.w;
+      }
+      all_k1 += n.z;
+      all_t0 += n.y;
+      all_t += n.y + n.w;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+      k0 += __shfl_xor(k0, d);
+      t0 += __shfl_xor(t0, d);
+      k1 += __shfl_xor(k1, d);
+      t1 += __shfl_xor(t1, d);
+      all_k1 += __shfl_xor(all_k1, d);
+      all_t0 += __shfl_xor(all_t0, d);
+      all_t += __shfl_xor(all_t, d);
+    }
+    // the first `want` ties are kept; those before slot `keep` come first
+    const Places at{p, x, keep, want};
+    const int first = i0 - lane;
+    Counts c{uniform(t0 + t1), uniform(k1 + min(want, t0 + t1) - min(want, t0)),
+             uniform(min(first, keep) - k0 - min(want, t0))};
+#pragma unroll
+    for (int e = 0; e < kUnitSlots / 64; ++e) {
+      uint64_t kept, tie;
+      masks(e, kept, tie);
+      at.list(first + 64 * e, lane, kept, tie, c);
+    }
+    if (part == 0) {
+      for (int i = threadIdx.x; i < 2048; i += 64 * kPickWaves) hist_of(p, head, 2)[i] = 0;
+      if (threadIdx.x == 0) {
+        p.num_moves[head] = all_k1 + min(want, all_t) - min(want, all_t0);
+        if (head % p.c.hkv == 0) p.lens_out[x.b] = keep;
+      }
+    }
+  }
+}
+
+constexpr int kMoveRows = 64;    // moves of a workgroup, where that is not too many of them
+constexpr int kMoveGroups = 8192;
+
+// The moves of a (sequence, kv head) over per_head workgroups, kRow / 16 lanes a
+// row; the slots past the kept ones are cleared on the side.  Bound by HBM.
 template <int kRow>
 __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int per_head) {
   const CacheArgs& a = p.c;
   constexpr int kLanes = kRow / 16;
   const int slots = a.max_pages << a.page_shift;
   const int64_t head = blockIdx.x / per_head;
-  const int j0 = static_cast<int>(blockIdx.x % per_head) * kMoveRows;
+  const int first = static_cast<int>(blockIdx.x % per_head);
   const int n = p.num_moves[head];
   const int b = static_cast<int>(head / a.hkv), kvh = static_cast<int>(head % a.hkv);
   const int64_t at0 = head * slots;
-  for (int i = p.lens_out[b] + static_cast<int>(blockIdx.x % per_head) * 256 + threadIdx.x;
-       i < slots; i += per_head * 256) {
+  for (int i = p.lens_out[b] + first * 256 + threadIdx.x; i < slots; i += per_head * 256) {
     p.weights_out[at0 + i] = 0.f;
     p.pos_out[at0 + i] = -1;
   }
-  if (j0 >= n) return;
   const int32_t* holes = p.moves + head * slots;
   const int32_t* from = holes + slots / 2;
   const auto row = [&](int slot) {
@@ -251,7 +414,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int p
     return (((pg << a.page_shift) + (slot & ((1 << a.page_shift) - 1))) * a.hkv + kvh) * kRow;
   };
   const int ch = threadIdx.x % kLanes;
-  for (int j = j0 + threadIdx.x / kLanes; j < min(n, j0 + kMoveRows); j += 256 / kLanes) {
+  constexpr int kAtOnce = 256 / kLanes;
+  for (int j = first * kAtOnce + threadIdx.x / kLanes; j < n; j += per_head * kAtOnce) {
     const int hole = holes[j], slot = from[j];
     const int64_t to = row(hole) + 16 * ch, src = row(slot) + 16 * ch;
     if (ch == 0) {
@@ -273,21 +437,29 @@ hipError_t launch_cache_evict(const CacheEvictArgs& a, int row_bytes, hipStream_
   const int64_t heads = static_cast<int64_t>(a.c.num_seqs) * a.c.hkv;
   const int64_t slots = static_cast<int64_t>(a.c.max_pages) << a.c.page_shift;
   const int64_t most = std::min<int64_t>(a.budget, slots / 2);  // moves of a head at most
-  const int64_t per = std::max<int64_t>(1, (most + kMoveRows - 1) / kMoveRows);
+  const int64_t per = std::max<int64_t>(
+      1, std::min((most + kMoveRows - 1) / kMoveRows, (kMoveGroups + heads - 1) / heads));
   // grids of fewer than 2^32 threads
-  if (heads >= int64_t(1) << 22 || heads * per >= int64_t(1) << 24) return hipErrorInvalidValue;
-  const dim3 sel(static_cast<unsigned>(heads)), threads(kThreads);
-  // slots in registers, 1024 to a unit; beyond 72 of them from memory
-  if (slots <= 4 * kThreads)
-    hipLaunchKernelGGL((cache_select_kernel<4>), sel, threads, 0, stream, a);
-  else if (slots <= 20 * kThreads)
-    hipLaunchKernelGGL((cache_select_kernel<20>), sel, threads, 0, stream, a);
-  else if (slots <= 72 * kThreads)
-    hipLaunchKernelGGL((cache_select_kernel<72>), sel, threads, 0, stream, a);
-  else
-    hipLaunchKernelGGL((cache_select_kernel<0>), sel, threads, 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (heads >= int64_t(1) << 22 || heads * slots >= int64_t(1) << 33) return hipErrorInvalidValue;
+  hipError_t e;
+  if (slots <= kSelectSlots) {
+    hipLaunchKernelGGL(cache_select_kernel, dim3(static_cast<unsigned>(heads)), dim3(kThreads), 0,
+                       stream, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  } else {
+    const int parts = static_cast<int>((slots + kPart - 1) / kPart);
+    const dim3 grid(static_cast<unsigned>(heads * parts)), block(64 * kPickWaves);
+    const auto stage = [&](auto k) {
+      hipLaunchKernelGGL((cache_pick_kernel<decltype(k)::value>), grid, block, 0, stream, a, parts);
+      return hipGetLastError();
+    };
+    if ((e = stage(std::integral_constant<int, 0>{})) != hipSuccess ||
+        (e = stage(std::integral_constant<int, 1>{})) != hipSuccess ||
+        (e = stage(std::integral_constant<int, 2>{})) != hipSuccess ||
+        (e = stage(std::integral_constant<int, 3>{})) != hipSuccess ||
+        (e = stage(std::integral_constant<int, 4>{})) != hipSuccess)
+      return e;
+  }
   const dim3 grid(static_cast<unsigned>(heads * per)), block(256);
   const int n = static_cast<int>(per);
   if (row_bytes == 128)

@@ -492,7 +492,13 @@ struct CacheEvictArgs {
   int32_t* moves;            // [num_seqs][hkv][slots]: free slots from the front on, the slots
                              // that move there from slots / 2 on
   int32_t* num_moves;        // [num_seqs][hkv]
+  int32_t* hist;             // [num_seqs * hkv][kEvictHist], zero between calls
+  int4* state;               // [num_seqs * hkv][3]
+  int4* counts;              // [num_seqs * hkv][evict_units(slots)]
 };
+constexpr int64_t kEvictHist = 1024 + 2048 + 2048;  // digits of 10, 11 and 11 bits
+// Wavefronts that count a long cache's slots.
+inline int64_t evict_units(int64_t slots) { return (slots + 2047) / 2048 * 4; }
 hipError_t launch_cache_evict(const CacheEvictArgs& a, int row_bytes, hipStream_t stream);
 
 }  // namespace sift
