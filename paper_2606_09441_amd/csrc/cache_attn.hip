@@ -91,6 +91,8 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   const int kt = lds0 + wave * 2 * kTile, vt = kt + kTile;  // this wavefront's tiles
   const int kaddr = kt + G::lane_k(l32, hf);
   const int vaddr = vt + G::lane_v(lane, l32, hf);
+  const int koff = G::template dma_lane<false>(lane, stride);
+  const int voff = G::template dma_lane<true>(lane, stride);
   const float c = score_factor(a.sc);
 
   Place pl = find_work(a, x, cost);
@@ -141,7 +143,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
                            rows_rsrc(reinterpret_cast<unsigned long long>(base) +
                                          (x.r[i].row * a.hkv + kvh) * G::kRow,
                                      x.r[i].n, stride, G::kRow),
-                           lane, stride);
+                           kV ? voff : koff, stride);
     };
 
     RowState<D> st;

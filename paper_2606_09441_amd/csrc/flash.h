@@ -95,11 +95,18 @@ struct Tile {
   }
 
   // Byte offset (from the first of 16 rows of a head, `stride` bytes apart) of
-  // the 16 bytes that this lane brings in DMA instruction j of those rows.
+  // the 16 bytes that this lane brings in DMA instruction j of those rows: the
+  // lane's offset for j = 0, its chunk XORed with the swizzle of row j kDmaRows
+  // (of whose bits the row inside the instruction has none).
   template <bool kV>
-  static __device__ __forceinline__ int dma_off(int lane, int j, int stride) {
-    const int row = j * kDmaRows + lane / kChunks;
+  static __device__ __forceinline__ int dma_lane(int lane, int stride) {
+    const int row = lane / kChunks;
     return row * stride + 16 * ((lane % kChunks) ^ (kV ? swz_v(row) : swz_k(row)));
+  }
+  template <bool kV>
+  static __device__ __forceinline__ int dma_off(int off0, int j, int stride) {
+    const int row = j * kDmaRows;
+    return (off0 ^ (16 * (kV ? swz_v(row) : swz_k(row)))) + row * stride;
   }
 
   // A operand of S^T: chunk 2 s + hf of row l32 of block kb.  lane_k is the
@@ -165,13 +172,13 @@ __device__ __forceinline__ i32x4 rows_rsrc(unsigned long long a, int rows, int s
                uniform(rows > 0 ? (rows - 1) * stride + row : 0), kBufferWord3};
 }
 
-// DMA of 16 rows into LDS at `lds` (wave-uniform byte address).
+// DMA of 16 rows into LDS at `lds` (wave-uniform byte address); off0: dma_lane.
 template <typename T, int D, bool kV>
-__device__ __forceinline__ void dma_rows(int lds, const i32x4& rs, int lane, int stride) {
+__device__ __forceinline__ void dma_rows(int lds, const i32x4& rs, int off0, int stride) {
   using G = Tile<T, D>;
 #pragma unroll
   for (int j = 0; j < G::kGroupDmas; ++j)
-    dma_b128(lds + j * 1024, G::template dma_off<kV>(lane, j, stride), rs);
+    dma_b128(lds + j * 1024, G::template dma_off<kV>(off0, j, stride), rs);
 }
 
 // Q operand: lane holds chunk 2 s + hf of its row, 16 bytes each.
