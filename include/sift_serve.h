@@ -21,7 +21,7 @@ extern "C" {
  * cap is 0), less slopes[h] * |position of the query - position of the key|
  * where slopes are given.
  *   softmax_scale  <= 0 selects 1/sqrt(D)
- *   cap            0 for none; negative or not finite: SIFT_E_UNSUPPORTED
+ *   cap            0 for none; negative, NaN or beyond 1e15: SIFT_E_UNSUPPORTED
  *   slopes         device float [Hq], or NULL; positions are exact up to 2^24
  * A NULL score is the default scale alone.
  */

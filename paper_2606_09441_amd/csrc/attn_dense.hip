@@ -224,10 +224,10 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dense_f32_kernel(De
 
 // bf16, software-pipelined: in step t the scores S(t + 1) = K(t + 1) Q^T are
 // formed on the matrix cores while the VALU makes the weights of S(t), then O
-// += V(t)^T P(t) while it caps S(t + 1) and takes its maxima; K runs a tile
-// ahead of V.  The order inside both halves is laid down by hand.
-//  * kCap: the polynomial of the tanh where no score of the wavefront's tile is
-//    large, the exact form apart where one is.
+// += V(t)^T P(t) while it takes the maxima of S(t + 1); K runs a tile ahead of V.  The order inside both halves is laid down by hand.
+//  * kCap: the tanh as a polynomial of the product where none of the wavefront's
+//    tile is large, folded into the exponent's FMA; the exact form apart where
+//    one is.  The cap keeps the order, so the maxima are those of the products.
 //  * kBias: outside the diagonal the distance is linear in the key, so that the
 //    bias is one more FMA with a constant, folded into the exponent; the tile's
 //    bound stands in for its maximum (its largest product at the smallest
@@ -259,85 +259,91 @@ __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
 
   RowState<D> st;
   st.clear();
-  // tiles that this wavefront computes
-  const int mine = (w.last - w.first + kKeys - 1) / kKeys;
+  // tiles that this wavefront computes: the first ones (with a bias they do not
+  // come in order, and it takes all, some of them masked)
+  const int mine = kBias && w.last > w.first ? w.tiles : (w.last - w.first + kKeys - 1) / kKeys;
   bool cleaned = false;
 
-  // The cap on scores of which none is large, or (1, 0, ..) nothing at all.
-  struct Poly {
-    float a0, a1, a2, a3, a4;
-    __device__ __forceinline__ float operator()(float z) const {
-      const float y = z * z;
-      return z * fmaf(y, fmaf(y, fmaf(y, fmaf(y, a4, a3), a2), a1), a0);
-    }
-  };
-  // A tile's exponents are c s + slope_key key + at, less the reference.
+  // A tile's exponents are cap(z) + slope_key key + at, less the reference.  The
+  // cap is z p(z^2) with these coefficients: the tanh's where no product of the
+  // wavefront's tile is large, (1, 0, ..) where the scores are capped already.
   struct Form {
-    float c, slope_key, at;
+    float p0, p1, p2, p3;  // without kCap: p0 alone, the scale
+    float slope_key, at;
   };
   const int lo = w.r0 + 32 * w.wave;  // this wavefront's rows: lo .. lo + 31
   // Tile t has keys before and after rows of this wavefront.
-  const auto mixed = [&](int t) {
+  const auto around = [&](int t) {
     const int j0 = w.first + t * kKeys;
     return kBias && j0 + kKeys - 1 > lo && j0 < lo + 31;
   };
   const auto masked = [&](int t) { return w.first + (t + 1) * kKeys > w.mine; };
-  const auto form = [&](int t) {
-    Form f{kCap ? 1.f : a.sc.c, 0.f, 0.f};
-    if constexpr (kBias) {
-      const int j0 = w.first + t * kKeys;
-      const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
-      f.slope_key = j0 < lo ? slope : -slope;
-      f.at = -f.slope_key * d;
-      if (mixed(t)) f = Form{1.f, 0.f, 0.f};  // odd_tile has the bias in the scores
-    }
-    return f;
+  const auto capped = [&](const Form& f, float z) {
+    if constexpr (!kCap) return z * f.p0;
+    const float y = z * z;
+    return z * fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
   };
-  // The bound of a tile from its largest score.
-  const auto bound = [&](int t, const Form& f, float mx) {
-    mx = half_max(mx) * f.c;
-    if constexpr (kBias) {
-      // the smallest distance to a key of the tile
-      const int j0 = w.first + t * kKeys;
-      if (f.slope_key > 0.f) mx -= slope * static_cast<float>(w.tok - j0 - (kKeys - 1));
-      if (f.slope_key < 0.f) mx -= slope * static_cast<float>(j0 - w.tok);
-    }
-    return mx;
-  };
-  const auto any_large = [&](const f32x16& s0, const f32x16& s1) {
-    if constexpr (!kCap) return false;
-    float big = 0.f;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) big = fmaxf(big, fmaxf(fabsf(s0[v]), fabsf(s1[v])));
-    return __builtin_amdgcn_ballot_w64(big * a.sc.x > kTanhSmall) != 0;
-  };
-  const auto cap_exactly = [&](f32x16& s0, f32x16& s1) {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      s0[v] = cap_any(a.sc, s0[v]);
-      s1[v] = cap_any(a.sc, s1[v]);
-    }
-  };
-  // The bias of tiles that have keys on both sides of a row, and the mask, on
-  // tile t's capped scores; returns their maximum.
-  const auto odd_tile = [&](int t, f32x16& s0, f32x16& s1) {
+  // Masked scores: -inf, or where z p(z^2) has to stay a number one that no score
+  // comes near (|capped score| <= kMaxCap log2(e)).
+  constexpr float kOut = kCap ? -1e18f : -INFINITY;
+  // Tile t's form, given the largest and the smallest product of each row; the
+  // scores in place where the tile is odd (a large product, keys around the
+  // row, a mask).  Returns the row's bound: its largest product's score at the
+  // smallest distance of the tile.
+  const auto take = [&](int t, f32x16& s0, f32x16& s1, float mx, float mn, Form& f) {
     const int j0 = w.first + t * kKeys;
-    if (mixed(t)) {
-      const float c = kCap ? 1.f : a.sc.c;
-      const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
+    f = Form{kCap ? a.sc.b[0] : a.sc.c, a.sc.b[1], a.sc.b[2], a.sc.b[3], 0.f, 0.f};
+    bool large = false;
+    if constexpr (kCap) {
+      large = __builtin_amdgcn_ballot_w64(fmaxf(mx, -mn) * a.sc.x > kTanhSmallBf16) != 0;
+      if (large) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float e = d - static_cast<float>(key_of(v));
-        s0[v] = fmaf(s0[v], c, -slope * fabsf(e));
-        s1[v] = fmaf(s1[v], c, -slope * fabsf(e - 32.f));
+        for (int v = 0; v < 16; ++v) {
+          s0[v] = cap_any(a.sc, s0[v]);
+          s1[v] = cap_any(a.sc, s1[v]);
+        }
+        mx = cap_any(a.sc, mx);
+        f.p0 = 1.f;
+        f.p1 = f.p2 = f.p3 = 0.f;
       }
     }
-    if (masked(t)) {
+    if (masked(t) || around(t)) {
+      const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
       const uint64_t bits = w.bits(j0);
-      mask_block(s0, static_cast<uint32_t>(bits >> (4 * w.hf)));
-      mask_block(s1, static_cast<uint32_t>(bits >> (32 + 4 * w.hf)));
+      const uint32_t m0 = static_cast<uint32_t>(bits >> (4 * w.hf));
+      const uint32_t m1 = static_cast<uint32_t>(bits >> (32 + 4 * w.hf));
+      mx = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        float x0 = s0[v], x1 = s1[v];
+        if constexpr (kCap || kBias) {
+          x0 = capped(f, x0);
+          x1 = capped(f, x1);
+        }
+        if constexpr (kBias) {
+          x0 = fmaf(-slope, fabsf(d - static_cast<float>(key_of(v))), x0);
+          x1 = fmaf(-slope, fabsf(d - static_cast<float>(key_of(v) + 32)), x1);
+        }
+        const bool in0 = (m0 >> key_of(v)) & 1u, in1 = (m1 >> key_of(v)) & 1u;
+        mx = fmaxf(mx, fmaxf(in0 ? x0 : -INFINITY, in1 ? x1 : -INFINITY));
+        s0[v] = in0 ? x0 : kOut;
+        s1[v] = in1 ? x1 : kOut;
+      }
+      if constexpr (kCap || kBias) {  // all of the exponent is in the scores
+        f.p0 = 1.f;
+        f.p1 = f.p2 = f.p3 = 0.f;
+        return half_max(mx);
+      }
     }
-    return fmaxf(block_max(s0), block_max(s1));
+    mx = half_max(mx);
+    if (mx > -INFINITY) mx = capped(f, mx);
+    if constexpr (kBias) {
+      const float dist = static_cast<float>(w.tok - j0);
+      f.slope_key = j0 < lo ? slope : -slope;
+      f.at = -f.slope_key * (dist - static_cast<float>(4 * w.hf));
+      mx -= slope * (j0 < lo ? dist - static_cast<float>(kKeys - 1) : -dist);
+    }
+    return mx;
   };
 
   // The weight of score e (0 .. 31) of a tile, with its neighbour, into pb.
@@ -345,20 +351,24 @@ __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
   const auto weigh = [&](int e, const f32x16& s0, const f32x16& s1, const Form& f, float base,
                          float& sum, float& le) {
     const int i = e >> 3, v = 8 * (i & 1) + (e & 7);
-    float x0 = i < 2 ? s0[v] : s1[v], x1 = i < 2 ? s0[v + 1] : s1[v + 1];
-    float b0 = -base, b1 = -base;
-    if constexpr (kBias) {
-      const int key = key_of(v) + (i < 2 ? 0 : 32);
-      b0 = fmaf(f.slope_key, static_cast<float>(key), f.at - base);
-      b1 = fmaf(f.slope_key, static_cast<float>(key + 1), f.at - base);
+    float p[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const float z = i < 2 ? s0[v + u] : s1[v + u];
+      float b = -base, pz = f.p0;
+      if constexpr (kBias)
+        b = fmaf(f.slope_key, static_cast<float>(key_of(v + u) + (i < 2 ? 0 : 32)), f.at - base);
+      if constexpr (kCap) {
+        const float y = z * z;
+        pz = fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
+      }
+      p[u] = __builtin_amdgcn_exp2f(fmaf(z, pz, b));
     }
-    const float p0 = __builtin_amdgcn_exp2f(fmaf(x0, f.c, b0));
-    const float p1 = __builtin_amdgcn_exp2f(fmaf(x1, f.c, b1));
-    const bf16x2 pp = bf16x2{static_cast<__bf16>(p0), static_cast<__bf16>(p1)};
+    const bf16x2 pp = bf16x2{static_cast<__bf16>(p[0]), static_cast<__bf16>(p[1])};
     pb[i][e & 7] = pp[0];
     pb[i][(e & 7) + 1] = pp[1];
     sum = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, sum, false);
-    if constexpr (kLse) le += p0 + p1;
+    if constexpr (kLse) le += p[0] + p[1];
   };
 
   // n0, n1 = K Q^T from K slot `slot`, beside the weights of the tile c0, c1
@@ -406,61 +416,61 @@ __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
     }
   };
 
-  // step t: S(t) in c0, c1 with form f; leaves S(t + 1) in n0, n1
+  // Tile of step i.  With a bias from the last row's own tile back, then on: the
+  // reference, which the near keys set, then hardly moves.
+  const int mid = min(w.tiles - 1, (w.r0 + w.rows - 1 - w.first) / kKeys);
+  const auto tile = [&](int i) { return !kBias ? i : i <= mid ? mid - i : i; };
+
+  // step i: its tile's scores in c0, c1 with form f; leaves the next in n0, n1
   Form f;
-  const auto step = [&](int t, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
-    const int par = t & 1;
+  const auto step = [&](int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
+    const int par = i & 1;
     // addresses made anew in every step: kept, each would hold a register
     asm volatile("" : "+v"(kaddr), "+v"(vaddr), "+v"(koff), "+v"(voff));
-    if (t + 1 < w.tiles) stage<T, D, true>(a, w, t + 1, lds0 + (2 + (par ^ 1)) * kTile, voff);
-    if (t + 2 < w.tiles) stage<T, D, false>(a, w, t + 2, lds0 + par * kTile, koff);
-    if (w.mixed(w.first + t * kKeys)) cleaned |= clean_tile<T, D>(lds0 + (2 + par) * kTile);
-    if (t < mine) {
+    if (i + 1 < w.tiles) stage<T, D, true>(a, w, tile(i + 1), lds0 + (2 + (par ^ 1)) * kTile, voff);
+    if (i + 2 < w.tiles) stage<T, D, false>(a, w, tile(i + 2), lds0 + par * kTile, koff);
+    if (w.mixed(w.first + tile(i) * kKeys))
+      cleaned |= clean_tile<T, D>(lds0 + (2 + par) * kTile);
+    if (i < mine) {
       // (past the last tile a body like the others: its scores go nowhere)
-      const bool more = t + 1 < mine;
       qk_and_weigh((par ^ 1) * kTile, n0, n1, c0, c1, f);
-      f = form(t + 1);
-      Poly poly{a.sc.a[0], a.sc.a[1], a.sc.a[2], a.sc.a[3], a.sc.a[4]};
-      if constexpr (kCap) {
-        if (any_large(n0, n1)) {
-          cap_exactly(n0, n1);
-          poly = Poly{1.f, 0.f, 0.f, 0.f, 0.f};
-        }
-      }
-      float mx = -INFINITY;
-      pv_and(par * kTile, [&](int i) {
+      float mx = -INFINITY, mn = INFINITY;
+      pv_and(par * kTile, [&](int e) {
 #pragma unroll
-        for (int u = 0; u < kDone; ++u) {
-          const int e = i * kDone + u;
-          f32x16& n = e < 16 ? n0 : n1;
-          if constexpr (kCap) n[e & 15] = poly(n[e & 15]);
-          mx = fmaxf(mx, n[e & 15]);
+        for (int u = 0; u < kDone; u += 2) {
+          const int v = (e * kDone + u) & 15;
+          const f32x16& n = e * kDone < 16 ? n0 : n1;
+          mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
+          if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
         }
       });
-      if (more && (masked(t + 1) || mixed(t + 1))) mx = odd_tile(t + 1, n0, n1);
-      st.rescale(more ? bound(t + 1, f, mx) : -INFINITY);
+      if (i + 1 < mine) st.rescale(take(tile(i + 1), n0, n1, mx, mn, f));
     }
     wait_vm<0>();
     __syncthreads();
   };
 
-  stage<T, D, false>(a, w, 0, lds0, koff);
-  stage<T, D, true>(a, w, 0, lds0 + 2 * kTile, voff);
-  if (w.tiles > 1) stage<T, D, false>(a, w, 1, lds0 + kTile, koff);
+  stage<T, D, false>(a, w, tile(0), lds0, koff);
+  stage<T, D, true>(a, w, tile(0), lds0 + 2 * kTile, voff);
+  if (w.tiles > 1) stage<T, D, false>(a, w, tile(1), lds0 + kTile, koff);
   wait_vm<0>();
   __syncthreads();
   f32x16 a0{}, a1{}, b0{}, b1{};
   if (mine > 0) {
     a0 = qk_block<T, D>(kaddr, 0, q);
     a1 = qk_block<T, D>(kaddr, 1, q);
-    f = form(0);
-    if constexpr (kCap) cap_exactly(a0, a1);
-    st.rescale(bound(0, f, odd_tile(0, a0, a1)));
+    float mx = -INFINITY, mn = INFINITY;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      mx = fmaxf(fmaxf(mx, a0[v]), a1[v]);
+      mn = fminf(fminf(mn, a0[v]), a1[v]);
+    }
+    st.rescale(take(tile(0), a0, a1, mx, mn, f));
   }
   __syncthreads();  // K slot 0 is refilled by step 0
-  for (int t = 0; t < w.tiles; t += 2) {
-    step(t, a0, a1, b0, b1);
-    if (t + 1 < w.tiles) step(t + 1, b0, b1, a0, a1);
+  for (int i = 0; i < w.tiles; i += 2) {
+    step(i, a0, a1, b0, b1);
+    if (i + 1 < w.tiles) step(i + 1, b0, b1, a0, a1);
   }
   if (cleaned) add_not_finite<T, D>(a, w, st.o);
   finish<T, D, kLse>(a, w, st);

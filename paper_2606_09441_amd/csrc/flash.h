@@ -260,9 +260,13 @@ __device__ __forceinline__ float cap_any(const ScoreArgs& sc, float z) {
 // The cap applied to a block of products, in the log2 domain.  Where none of
 // the wavefront's products is large the polynomial alone serves.
 __device__ __forceinline__ void cap_scores(const ScoreArgs& sc, f32x16& s) {
-  float big = 0.f;
+  float mx = s[0], mn = s[0];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) big = fmaxf(big, fabsf(s[v]));
+  for (int v = 1; v < 15; v += 2) {
+    mx = fmaxf(fmaxf(mx, s[v]), s[v + 1]);
+    mn = fminf(fminf(mn, s[v]), s[v + 1]);
+  }
+  const float big = fmaxf(fmaxf(mx, s[15]), -fminf(mn, s[15]));
   // (a NaN is dropped here, and stays one in the polynomial)
   if (__builtin_amdgcn_ballot_w64(big * sc.x > kTanhSmall)) {
 #pragma unroll

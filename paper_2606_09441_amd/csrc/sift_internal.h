@@ -393,14 +393,21 @@ struct ScoreArgs {
   float x;        // scale / cap: x z0 is the tanh's argument (z0 = q.k); 0: no cap
   float cap2;     // cap * unit
   float a[5];     // unit * s = z0 * poly(z0^2) where |x z0| <= kTanhSmall
+  float b[4];     // the same to bf16's needs where |x z0| <= kTanhSmallBf16
   const float* slopes;  // [Hq] or nullptr
 };
 
-// tanh(y) / y over |y| <= kTanhSmall as a polynomial in y^2 of degree 4:
-// minimax fit of the relative error (1.4e-8), made by reweighted least squares.
+// tanh(y) / y as a polynomial in y^2, minimax fits of the relative error made by
+// reweighted least squares: degree 4 over |y| <= kTanhSmall (1.4e-8), degree 3
+// over |y| <= kTanhSmallBf16 (1.0e-7: a score of 16 is off by 1.6e-6, a weight
+// by as much of it, where rounding it to bf16 takes 4e-3).
 constexpr float kTanhSmall = 0.5f;
 constexpr double kTanhPoly[5] = {0.9999999869, -0.3333306939, 0.1332477931, -0.05298607504,
                                  0.01713500614};
+constexpr float kTanhSmallBf16 = 0.4f;
+constexpr double kTanhPolyBf16[4] = {0.9999999019, -0.3333136246, 0.1327097676, -0.04755360348};
+// Caps beyond this would not show in fp32, and their squares would overflow.
+constexpr float kMaxCap = 1e15f;
 
 // Dense attention (attn_dense.hip).  A record: 128 query rows of a segment,
 // {first row, rows, first key, upto}: row i sees the keys j from the first on
