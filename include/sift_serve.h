@@ -135,7 +135,8 @@ sift_status sift_cache_destroy(sift_cache* cache);
  * influence on it.  Rows that row_ptr leaves out are not written.  Results
  * depend on nothing but the arguments (no atomics).
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, alignment,
- *   cap), SIFT_E_CAPACITY (mask_words; 2^24 rows x heads or more), SIFT_E_PLAN
+ *   cap), SIFT_E_CAPACITY (mask_words; 2^24 rows x heads or more; more
+ *   than 2^31 steps of 128 keys of 32 rows in all), SIFT_E_PLAN
  *   (another device is current), SIFT_E_HIP.
  */
 sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,

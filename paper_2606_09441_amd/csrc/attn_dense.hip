@@ -17,15 +17,13 @@
 
 #include <algorithm>
 
-#include "flash.h"
+#include "flash_pipe.h"
 #include "sift_internal.h"
 
 namespace sift {
 namespace {
 
 using namespace flash;
-
-constexpr int kKeys = 64;   // of a tile
 
 // Workgroup -> record and head, XCD blockIdx % 8 (see dense_grid).
 __device__ __forceinline__ void place(const DenseArgs& a, int& rec, int& h) {
@@ -98,26 +96,6 @@ __device__ __forceinline__ void stage(const DenseArgs& a, const Row& w, int t, i
       off0, stride);
 }
 
-// A V tile at LDS address `tile` whose keys some rows of the record see and others
-// do not: a weight of 0 times an infinity would be a NaN in rows that do not see
-// the key, so the places that are not finite are taken out (and put right at the
-// end, see add_not_finite).  All wavefronts call this; returns whether there
-// were any.
-template <typename T, int D>
-__device__ __forceinline__ bool clean_tile(int tile) {
-  constexpr int kTile = kKeys * Tile<T, D>::kRow;
-  bool bad = false;
-  for (int i = threadIdx.x; i < kTile / 16; i += 256)
-    bad |= not_finite<T>(*reinterpret_cast<const lds_u32x4*>(static_cast<size_t>(tile + 16 * i)));
-  if (!__syncthreads_or(bad)) return false;
-  for (int i = threadIdx.x; i < kTile / 16; i += 256) {
-    lds_u32x4* p = reinterpret_cast<lds_u32x4*>(static_cast<size_t>(tile + 16 * i));
-    *p = only_finite<T>(*p);
-  }
-  __syncthreads();
-  return true;
-}
-
 // Adds what clean_tile took out to the rows that see it.
 template <typename T, int D>
 __device__ __forceinline__ void add_not_finite(const DenseArgs& a, const Row& w,
@@ -125,15 +103,7 @@ __device__ __forceinline__ void add_not_finite(const DenseArgs& a, const Row& w,
   const T* v = static_cast<const T*>(a.v) + static_cast<int64_t>(w.kvh) * D + 4 * w.hf;
 #pragma unroll 1
   for (int j = w.first + (w.all - w.first) / kKeys * kKeys; j < w.kend; ++j) {
-    const T* row = v + static_cast<int64_t>(j) * a.hkv * D;
-    const bool sees = j < w.upto || j <= w.tok;
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = static_cast<float>(row[32 * db + key_of(i)]);
-        if (sees && !(fabsf(x) < INFINITY)) o[db][i] += x;
-      }
+    add_not_finite_row<T, D>(v + static_cast<int64_t>(j) * a.hkv * D, j < w.upto || j <= w.tok, o);
   }
 }
 
@@ -222,26 +192,63 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dense_f32_kernel(De
   finish<T, D, kLse>(a, w, st);
 }
 
-// bf16, software-pipelined: in step t the scores S(t + 1) = K(t + 1) Q^T are
-// formed on the matrix cores while the VALU makes the weights of S(t), then O
-// += V(t)^T P(t) while it takes the maxima of S(t + 1); K runs a tile ahead of V.  The order inside both halves is laid down by hand.
-//  * kCap: the tanh as a polynomial of the product where none of the wavefront's
-//    tile is large, folded into the exponent's FMA; the exact form apart where
-//    one is.  The cap keeps the order, so the maxima are those of the products.
-//  * kBias: outside the diagonal the distance is linear in the key, so that the
-//    bias is one more FMA with a constant, folded into the exponent; the tile's
-//    bound stands in for its maximum (its largest product at the smallest
-//    distance), which only has to be near and not below.
+// The record's tiles as the pipeline takes them (flash_pipe.h).  kBias: outside the
+// diagonal the distance is linear in the key, so that the bias is one more FMA with
+// a constant, folded into the exponent; the tile's bound then is its largest
+// product at the smallest distance, which only has to be near and not below.
+template <int D, bool kCap, bool kBias>
+struct DenseTiles {
+  using T = __bf16;
+  const DenseArgs& a;
+  const Row& w;
+  float slope;
+  int steps, mine;
+  int lo;   // this wavefront's rows: lo .. lo + 31
+  int mid;  // the last row's own tile
+  bool cleaned = false;
+  __device__ __forceinline__ DenseTiles(const DenseArgs& args, const Row& row)
+      : a(args), w(row), slope(kBias ? args.sc.slopes[row.h] * kLog2e : 0.f), steps(row.tiles),
+        lo(row.r0 + 32 * row.wave) {
+    // (with a bias the tiles do not come in order, and every wavefront takes all,
+    // some of them masked)
+    mine = kBias && w.last > w.first ? steps : (w.last - w.first + kKeys - 1) / kKeys;
+    mid = min(steps - 1, (w.r0 + w.rows - 1 - w.first) / kKeys);
+  }
+  // Tile of step i.  With a bias from the last row's own back, then on: the
+  // reference, which the near keys set, then hardly moves.
+  __device__ __forceinline__ int tile(int i) const { return !kBias ? i : i <= mid ? mid - i : i; }
+  template <bool kV>
+  __device__ __forceinline__ void fetch(int i, int lds, int off0) const {
+    stage<T, D, kV>(a, w, tile(i), lds, off0);
+  }
+  __device__ __forceinline__ void clean(int i, int lds) {
+    if (w.mixed(w.first + tile(i) * kKeys)) cleaned |= clean_tile<T, D>(lds);
+  }
+  __device__ __forceinline__ float take(int i, f32x16& s0, f32x16& s1, float mx, float mn,
+                                        Form& f) const {
+    const int j0 = w.first + tile(i) * kKeys;
+    const bool masked = j0 + kKeys > w.mine;
+    const bool around = kBias && j0 + kKeys - 1 > lo && j0 < lo + 31;  // a row inside the tile
+    const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
+    mx = take_tile<kCap, kBias>(
+        a.sc, s0, s1, mx, mn, masked || around, w.bits(j0), w.hf, slope,
+        [&](int key) { return fabsf(d - static_cast<float>(key)); }, f);
+    if constexpr (kBias) {
+      if (!masked && !around) {
+        const float dist = static_cast<float>(w.tok - j0);
+        f.slope_key = j0 < lo ? slope : -slope;
+        f.at = -f.slope_key * d;
+        mx -= slope * (j0 < lo ? dist - static_cast<float>(kKeys - 1) : -dist);
+      }
+    }
+    return mx;
+  }
+};
+
 template <int D, bool kCap, bool kBias, bool kLse>
 __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
   using T = __bf16;
-  using G = Tile<T, D>;
-  constexpr int kTile = kKeys * G::kRow;
-  constexpr int kSteps = G::kSteps;         // of QK^T: 16 dims each
-  constexpr int kEach = 32 / kSteps;        // scores of S(t) that go with one
-  constexpr int kPv = 4 * (D / 32);         // matrix instructions of PV
-  constexpr int kDone = 32 / kPv;           // scores of S(t + 1) that go with one
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * kTile];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * kKeys * Tile<T, D>::kRow];
   int rec, h;
   place(a, rec, h);
   if (rec >= a.num_recs) return;
@@ -249,230 +256,11 @@ __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
   w.load(a, rec, h);
   QFrag<T, D> q;
   q.load(static_cast<const T*>(a.q) + (static_cast<int64_t>(w.tok) * a.hq + w.h) * D, w.hf, w.live);
-  const int lds0 = static_cast<int>(reinterpret_cast<size_t>((lds_u8*)smem));
-  int kaddr = lds0 + G::lane_k(w.l32, w.hf);
-  int vaddr = lds0 + 2 * kTile + G::lane_v(w.lane, w.l32, w.hf);
-  int koff = G::template dma_lane<false>(w.lane, a.hkv * G::kRow);
-  int voff = G::template dma_lane<true>(w.lane, a.hkv * G::kRow);
-  const float slope = kBias ? a.sc.slopes[w.h] * kLog2e : 0.f;
-  const bf16x2 ones = bf16x2{static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
-
   RowState<D> st;
   st.clear();
-  // tiles that this wavefront computes: the first ones (with a bias they do not
-  // come in order, and it takes all, some of them masked)
-  const int mine = kBias && w.last > w.first ? w.tiles : (w.last - w.first + kKeys - 1) / kKeys;
-  bool cleaned = false;
-
-  // A tile's exponents are cap(z) + slope_key key + at, less the reference.  The
-  // cap is z p(z^2) with these coefficients: the tanh's where no product of the
-  // wavefront's tile is large, (1, 0, ..) where the scores are capped already.
-  struct Form {
-    float p0, p1, p2, p3;  // without kCap: p0 alone, the scale
-    float slope_key, at;
-  };
-  const int lo = w.r0 + 32 * w.wave;  // this wavefront's rows: lo .. lo + 31
-  // Tile t has keys before and after rows of this wavefront.
-  const auto around = [&](int t) {
-    const int j0 = w.first + t * kKeys;
-    return kBias && j0 + kKeys - 1 > lo && j0 < lo + 31;
-  };
-  const auto masked = [&](int t) { return w.first + (t + 1) * kKeys > w.mine; };
-  const auto capped = [&](const Form& f, float z) {
-    if constexpr (!kCap) return z * f.p0;
-    const float y = z * z;
-    return z * fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
-  };
-  // Masked scores: -inf, or where z p(z^2) has to stay a number one that no score
-  // comes near (|capped score| <= kMaxCap log2(e)).
-  constexpr float kOut = kCap ? -1e18f : -INFINITY;
-  // Tile t's form, given the largest and the smallest product of each row; the
-  // scores in place where the tile is odd (a large product, keys around the
-  // row, a mask).  Returns the row's bound: its largest product's score at the
-  // smallest distance of the tile.
-  const auto take = [&](int t, f32x16& s0, f32x16& s1, float mx, float mn, Form& f) {
-    const int j0 = w.first + t * kKeys;
-    f = Form{kCap ? a.sc.b[0] : a.sc.c, a.sc.b[1], a.sc.b[2], a.sc.b[3], 0.f, 0.f};
-    bool large = false;
-    if constexpr (kCap) {
-      large = __builtin_amdgcn_ballot_w64(fmaxf(mx, -mn) * a.sc.x > kTanhSmallBf16) != 0;
-      if (large) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          s0[v] = cap_any(a.sc, s0[v]);
-          s1[v] = cap_any(a.sc, s1[v]);
-        }
-        mx = cap_any(a.sc, mx);
-        f.p0 = 1.f;
-        f.p1 = f.p2 = f.p3 = 0.f;
-      }
-    }
-    if (masked(t) || around(t)) {
-      const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
-      const uint64_t bits = w.bits(j0);
-      const uint32_t m0 = static_cast<uint32_t>(bits >> (4 * w.hf));
-      const uint32_t m1 = static_cast<uint32_t>(bits >> (32 + 4 * w.hf));
-      mx = -INFINITY;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        float x0 = s0[v], x1 = s1[v];
-        if constexpr (kCap || kBias) {
-          x0 = capped(f, x0);
-          x1 = capped(f, x1);
-        }
-        if constexpr (kBias) {
-          x0 = fmaf(-slope, fabsf(d - static_cast<float>(key_of(v))), x0);
-          x1 = fmaf(-slope, fabsf(d - static_cast<float>(key_of(v) + 32)), x1);
-        }
-        const bool in0 = (m0 >> key_of(v)) & 1u, in1 = (m1 >> key_of(v)) & 1u;
-        mx = fmaxf(mx, fmaxf(in0 ? x0 : -INFINITY, in1 ? x1 : -INFINITY));
-        s0[v] = in0 ? x0 : kOut;
-        s1[v] = in1 ? x1 : kOut;
-      }
-      if constexpr (kCap || kBias) {  // all of the exponent is in the scores
-        f.p0 = 1.f;
-        f.p1 = f.p2 = f.p3 = 0.f;
-        return half_max(mx);
-      }
-    }
-    mx = half_max(mx);
-    if (mx > -INFINITY) mx = capped(f, mx);
-    if constexpr (kBias) {
-      const float dist = static_cast<float>(w.tok - j0);
-      f.slope_key = j0 < lo ? slope : -slope;
-      f.at = -f.slope_key * (dist - static_cast<float>(4 * w.hf));
-      mx -= slope * (j0 < lo ? dist - static_cast<float>(kKeys - 1) : -dist);
-    }
-    return mx;
-  };
-
-  // The weight of score e (0 .. 31) of a tile, with its neighbour, into pb.
-  bf16x8 pb[4];
-  const auto weigh = [&](int e, const f32x16& s0, const f32x16& s1, const Form& f, float base,
-                         float& sum, float& le) {
-    const int i = e >> 3, v = 8 * (i & 1) + (e & 7);
-    float p[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const float z = i < 2 ? s0[v + u] : s1[v + u];
-      float b = -base, pz = f.p0;
-      if constexpr (kBias)
-        b = fmaf(f.slope_key, static_cast<float>(key_of(v + u) + (i < 2 ? 0 : 32)), f.at - base);
-      if constexpr (kCap) {
-        const float y = z * z;
-        pz = fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
-      }
-      p[u] = __builtin_amdgcn_exp2f(fmaf(z, pz, b));
-    }
-    const bf16x2 pp = bf16x2{static_cast<__bf16>(p[0]), static_cast<__bf16>(p[1])};
-    pb[i][e & 7] = pp[0];
-    pb[i][(e & 7) + 1] = pp[1];
-    sum = __builtin_amdgcn_fdot2_f32_bf16(pp, ones, sum, false);
-    if constexpr (kLse) le += p[0] + p[1];
-  };
-
-  // n0, n1 = K Q^T from K slot `slot`, beside the weights of the tile c0, c1
-  const auto qk_and_weigh = [&](int slot, f32x16& n0, f32x16& n1, const f32x16& c0,
-                                const f32x16& c1, const Form& f) {
-    const float base = st.base();
-    float sum = 0.f, le = 0.f;
-    u32x4 x[3][2];
-#pragma unroll
-    for (int s = 0; s < 3; ++s) {
-      x[s][0] = G::k_frag(kaddr + slot, 0, s);
-      x[s][1] = G::k_frag(kaddr + slot, 1, s);
-    }
-    n0 = n1 = f32x16{};
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      n0 = dot_step<T>(x[s % 3][0], q.x[s], n0);
-      n1 = dot_step<T>(x[s % 3][1], q.x[s], n1);
-#pragma unroll
-      for (int u = 0; u < kEach; u += 2) weigh(s * kEach + u, c0, c1, f, base, sum, le);
-      if (s + 3 < kSteps) {
-        x[s % 3][0] = G::k_frag(kaddr + slot, 0, s + 3);
-        x[s % 3][1] = G::k_frag(kaddr + slot, 1, s + 3);
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    st.l += sum;
-    st.le += le;
-  };
-  // O += V^T P^T from V slot `slot`; with(i) goes beside matrix instruction i
-  const auto pv_and = [&](int slot, auto with) {
-    constexpr int kAhead = 3;
-    bf16x8 x[kAhead];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) x[i] = G::v_frag(vaddr + slot, i % (D / 32), i / (D / 32));
-#pragma unroll
-    for (int i = 0; i < kPv; ++i) {
-      const int db = i % (D / 32);
-      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i % kAhead], pb[i / (D / 32)], st.o[db],
-                                                        0, 0, 0);
-      with(i);
-      const int j = i + kAhead;
-      if (j < kPv) x[j % kAhead] = G::v_frag(vaddr + slot, j % (D / 32), j / (D / 32));
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
-
-  // Tile of step i.  With a bias from the last row's own tile back, then on: the
-  // reference, which the near keys set, then hardly moves.
-  const int mid = min(w.tiles - 1, (w.r0 + w.rows - 1 - w.first) / kKeys);
-  const auto tile = [&](int i) { return !kBias ? i : i <= mid ? mid - i : i; };
-
-  // step i: its tile's scores in c0, c1 with form f; leaves the next in n0, n1
-  Form f;
-  const auto step = [&](int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
-    const int par = i & 1;
-    // addresses made anew in every step: kept, each would hold a register
-    asm volatile("" : "+v"(kaddr), "+v"(vaddr), "+v"(koff), "+v"(voff));
-    if (i + 1 < w.tiles) stage<T, D, true>(a, w, tile(i + 1), lds0 + (2 + (par ^ 1)) * kTile, voff);
-    if (i + 2 < w.tiles) stage<T, D, false>(a, w, tile(i + 2), lds0 + par * kTile, koff);
-    if (w.mixed(w.first + tile(i) * kKeys))
-      cleaned |= clean_tile<T, D>(lds0 + (2 + par) * kTile);
-    if (i < mine) {
-      // (past the last tile a body like the others: its scores go nowhere)
-      qk_and_weigh((par ^ 1) * kTile, n0, n1, c0, c1, f);
-      float mx = -INFINITY, mn = INFINITY;
-      pv_and(par * kTile, [&](int e) {
-#pragma unroll
-        for (int u = 0; u < kDone; u += 2) {
-          const int v = (e * kDone + u) & 15;
-          const f32x16& n = e * kDone < 16 ? n0 : n1;
-          mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
-          if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
-        }
-      });
-      if (i + 1 < mine) st.rescale(take(tile(i + 1), n0, n1, mx, mn, f));
-    }
-    wait_vm<0>();
-    __syncthreads();
-  };
-
-  stage<T, D, false>(a, w, tile(0), lds0, koff);
-  stage<T, D, true>(a, w, tile(0), lds0 + 2 * kTile, voff);
-  if (w.tiles > 1) stage<T, D, false>(a, w, tile(1), lds0 + kTile, koff);
-  wait_vm<0>();
-  __syncthreads();
-  f32x16 a0{}, a1{}, b0{}, b1{};
-  if (mine > 0) {
-    a0 = qk_block<T, D>(kaddr, 0, q);
-    a1 = qk_block<T, D>(kaddr, 1, q);
-    float mx = -INFINITY, mn = INFINITY;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      mx = fmaxf(fmaxf(mx, a0[v]), a1[v]);
-      mn = fminf(fminf(mn, a0[v]), a1[v]);
-    }
-    st.rescale(take(tile(0), a0, a1, mx, mn, f));
-  }
-  __syncthreads();  // K slot 0 is refilled by step 0
-  for (int i = 0; i < w.tiles; i += 2) {
-    step(i, a0, a1, b0, b1);
-    if (i + 1 < w.tiles) step(i + 1, b0, b1, a0, a1);
-  }
-  if (cleaned) add_not_finite<T, D>(a, w, st.o);
+  DenseTiles<D, kCap, kBias> src(a, w);
+  run_pipe<D, kCap, kBias, kLse>(src, q, st, smem, w.lane, a.hkv * Tile<T, D>::kRow);
+  if (src.cleaned) add_not_finite<T, D>(a, w, st.o);
   finish<T, D, kLse>(a, w, st);
 }
 

@@ -36,43 +36,44 @@ __device__ __forceinline__ Seq sequence(const CacheArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
+__device__ __forceinline__ int wave_sum(int x) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+  return uniform(x);
 }
 
-// The work of all sequences, `cost(Seq)` steps each, one after another.
+// The work of all sequences, cost(Seq) steps each, one after another: fewer than
+// 2^31 (checked by the host).  All uniform.
 struct Place {
-  int32_t b;     // sequence that holds step x, num_seqs past the end
-  int64_t at;    // the sequence's first step
+  int32_t b;   // sequence that holds a step, num_seqs past the end
+  int32_t at;  // the sequence's first step
 };
 
 template <typename Cost>
-__device__ __forceinline__ int64_t total_work(const CacheArgs& a, Cost cost) {
-  int64_t sum = 0;
+__device__ __forceinline__ int total_work(const CacheArgs& a, Cost cost) {
+  int sum = 0;
   for (int b = threadIdx.x & 63; b < a.num_seqs; b += 64) sum += cost(sequence(a, b));
   return wave_sum(sum);
 }
 
 template <typename Cost>
-__device__ __forceinline__ Place find_work(const CacheArgs& a, int64_t x, Cost cost) {
+__device__ __forceinline__ Place find_work(const CacheArgs& a, int x, Cost cost) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  int before = 0;
   for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
-    const int64_t mine = b0 + lane < a.num_seqs ? cost(sequence(a, b0 + lane)) : 0;
-    int64_t upto = mine;  // inclusive scan
+    const int mine = b0 + lane < a.num_seqs ? cost(sequence(a, b0 + lane)) : 0;
+    int upto = mine;  // inclusive scan
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up(upto, d);
+      const int y = __shfl_up(upto, d);
       if (lane >= d) upto += y;
     }
     const uint64_t past = __ballot(before + upto > x);
     if (past != 0) {
       const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      return Place{b0 + l, before + __shfl(upto - mine, l)};
+      return Place{b0 + l, uniform(before + __shfl(upto - mine, l))};
     }
-    before += __shfl(upto, 63);
+    before += uniform(__shfl(upto, 63));
   }
   return Place{a.num_seqs, before};
 }
@@ -82,11 +83,11 @@ __device__ __forceinline__ Place find_work(const CacheArgs& a, int64_t x, Cost c
 template <typename Cost>
 __device__ __forceinline__ Place find_token(const CacheArgs& a, int token, Cost cost) {
   const int lane = threadIdx.x & 63;
-  int64_t before = 0;
+  int before = 0;
   for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
     const bool in = b0 + lane < a.num_seqs;
     const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
-    const int64_t mine = in ? cost(s) : 0;
+    const int mine = in ? cost(s) : 0;
     const uint64_t has = __ballot(in && token >= s.row0 && token < s.row0 + s.n);
     if (has != 0) {
       const int l = __ffsll(static_cast<unsigned long long>(has)) - 1;
@@ -97,13 +98,82 @@ __device__ __forceinline__ Place find_token(const CacheArgs& a, int token, Cost 
   return Place{a.num_seqs, before};
 }
 
-// Steps x of [0, total) go to workgroup share_of(x): workgroup i takes those
-// from share(i) to share(i + 1).  groups <= total: every workgroup has some.
-__device__ __forceinline__ int64_t share(int64_t i, int64_t total, int64_t groups) {
-  return i * total / groups;
+// An even split of `total` steps over the workgroups of a launch, or over as many
+// as there are steps: workgroup i takes those from at(i) to at(i + 1).
+struct Split {
+  int total, groups, each, more;  // total = groups * each + more
+  __device__ __forceinline__ Split(int total_, int launched)
+      : total(total_), groups(min(total_, launched)) {
+    each = groups > 0 ? quotient(total, groups) : 0;
+    more = total - each * groups;
+  }
+  static __device__ __forceinline__ int quotient(int x, int y) {
+    return uniform(static_cast<int>(static_cast<unsigned>(x) / static_cast<unsigned>(y)));
+  }
+  // the first `more` workgroups take one step more
+  __device__ __forceinline__ int at(int i) const { return i * each + min(i, more); }
+  __device__ __forceinline__ int of(int x) const {
+    const int big = more * (each + 1);  // steps of the first ones
+    return uniform(x < big ? quotient(x, each + 1) : more + quotient(x - big, each));
+  }
+};
+
+// The units of an attention: kRows rows (new token, query head) of a (sequence, kv
+// head) over all its keys, in steps.
+struct Narrow {  // four 32-key tiles a step
+  static constexpr int kRows = 32;
+  static constexpr int kTileKeys = 32, kStepTiles = 4;
+};
+struct Wide {    // a 64-key tile a step
+  static constexpr int kRows = 128;
+  static constexpr int kTileKeys = 64, kStepTiles = 1;
+};
+template <typename U>
+struct UnitCost {
+  int32_t g, hkv;
+  __device__ __forceinline__ int blocks(const Seq& s) const {
+    return (s.n * g + U::kRows - 1) / U::kRows;
+  }
+  static __device__ __forceinline__ int cached_tiles(const Seq& s) {
+    return (s.len + U::kTileKeys - 1) / U::kTileKeys;
+  }
+  static __device__ __forceinline__ int tiles(const Seq& s) {
+    return cached_tiles(s) + (s.n + U::kTileKeys - 1) / U::kTileKeys;
+  }
+  static __device__ __forceinline__ int steps(const Seq& s) {
+    return (tiles(s) + U::kStepTiles - 1) / U::kStepTiles;
+  }
+  __device__ __forceinline__ int operator()(const Seq& s) const {
+    return hkv * blocks(s) * steps(s);
+  }
+};
+
+// A workgroup's place in the list of steps.  Workgroups go round-robin over the
+// XCDs: where all have work, those of an XCD take neighbouring shares, so that
+// units of the same keys meet in its L2.
+__device__ __forceinline__ int group_of(const Split& split) {
+  if (split.groups < static_cast<int>(gridDim.x) || split.groups % kNumXcd != 0) return blockIdx.x;
+  return blockIdx.x % kNumXcd * (split.groups / kNumXcd) + blockIdx.x / kNumXcd;
 }
-__device__ __forceinline__ int64_t share_of(int64_t x, int64_t total, int64_t groups) {
-  return ((x + 1) * groups - 1) / total;
+
+// The result of a row: four of its dims, and its log sum; l, le: the sums of its
+// weights as they were multiplied, and before their rounding.
+template <typename T>
+__device__ __forceinline__ void store_row(T* dst, const float (&o)[4], float inv) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    *reinterpret_cast<bf16x4*>(dst) =
+        bf16x4{static_cast<__bf16>(o[0] * inv), static_cast<__bf16>(o[1] * inv),
+               static_cast<__bf16>(o[2] * inv), static_cast<__bf16>(o[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+}
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
+__device__ __forceinline__ float log_sum(float m, float le) {
+  return le > 0.f ? fmaf(m, kLn2, logf(le)) : le == le ? -INFINITY : le;
+}
+// Weight of a part with reference m in a sum with reference top (>= m).
+__device__ __forceinline__ float part_weight(float m, float top) {
+  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);  // no key: zeros, or NaN
 }
 
 // 16 rows of keys: where, and how many are valid.

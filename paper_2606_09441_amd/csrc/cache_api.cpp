@@ -150,7 +150,9 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
       hipDeviceGetAttribute(&c->cus, hipDeviceAttributeMultiprocessorCount, c->device) !=
           hipSuccess)
     return fail();
-  const size_t rows = static_cast<size_t>(2 * c->cus) * sift::kCacheSlotRows;
+  const bool wide = sift::cache_attn_wide(true, max_rows * g);
+  const size_t rows = static_cast<size_t>(2 * 2 * c->cus) *
+                      (wide ? sift::kCacheWideRows : sift::kCacheRows);
   const size_t o_bytes = rows * head_dim * sizeof(float);
   const size_t heads = static_cast<size_t>(num_seqs) * num_kv_heads;
   const size_t moves = heads * max_pages * page;
@@ -210,6 +212,7 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   if ((st = check_tensor(v_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
   if ((st = check_tensor(out, rows, cache->hq, d, dtype)) != SIFT_OK) return st;
   if (tree_mask != nullptr && mask_words < (cache->max_rows + 63) / 64) return SIFT_E_CAPACITY;
+  if (sift::cache_attn_steps(a.c) >= int64_t(1) << 31) return SIFT_E_CAPACITY;
   if (rows == 0) return SIFT_OK;
   a.k_new = k_new->data;
   a.v_new = v_new->data;
@@ -239,6 +242,7 @@ sift_status sift_cache_accumulate(sift_cache* cache, const sift_cache_kv* kv,
   if ((st = check_rows(cache, new_rows, q, dtype, score, 1.0, &a.c)) != SIFT_OK) return st;
   if (out == nullptr || (lse == nullptr && q->tokens > 0)) return SIFT_E_NULL;
   if (!std::isfinite(decay)) return SIFT_E_UNSUPPORTED;
+  if (sift::cache_weights_steps(a.c) >= int64_t(1) << 31) return SIFT_E_CAPACITY;
   a.lse = lse;
   a.row_weight = row_weight;
   a.weights = weights;

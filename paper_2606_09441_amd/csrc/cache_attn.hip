@@ -27,45 +27,9 @@ namespace {
 
 using namespace cache;
 
-constexpr int kTileKeys = 32;
-constexpr int kStepTiles = 4;  // a step: a tile for each wavefront
-
-struct UnitCost {
-  int32_t g, hkv;
-  __device__ __forceinline__ int blocks(const Seq& s) const {
-    return (s.n * g + kCacheRows - 1) / kCacheRows;
-  }
-  static __device__ __forceinline__ int tiles(const Seq& s) {
-    return (s.len + kTileKeys - 1) / kTileKeys + (s.n + kTileKeys - 1) / kTileKeys;
-  }
-  static __device__ __forceinline__ int steps(const Seq& s) {
-    return (tiles(s) + kStepTiles - 1) / kStepTiles;
-  }
-  __device__ __forceinline__ int64_t operator()(const Seq& s) const {
-    return static_cast<int64_t>(hkv) * blocks(s) * steps(s);
-  }
-};
-
-// The result of one row: sum of weights l, before their rounding le.
-template <typename T>
-__device__ __forceinline__ void store_row(T* dst, const float (&o)[4], float inv) {
-  if constexpr (std::is_same<T, __bf16>::value)
-    *reinterpret_cast<bf16x4*>(dst) =
-        bf16x4{static_cast<__bf16>(o[0] * inv), static_cast<__bf16>(o[1] * inv),
-               static_cast<__bf16>(o[2] * inv), static_cast<__bf16>(o[3] * inv)};
-  else
-    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-}
-
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
-__device__ __forceinline__ float log_sum(float m, float le) {
-  return le > 0.f ? fmaf(m, kLn2, logf(le)) : le == le ? -INFINITY : le;
-}
-
-// Weight of a part with reference m in a sum with reference top (>= m).
-__device__ __forceinline__ float part_weight(float m, float top) {
-  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);  // no key: zeros, or NaN
-}
+constexpr int kTileKeys = Narrow::kTileKeys;
+constexpr int kStepTiles = Narrow::kStepTiles;  // a tile for each wavefront
+constexpr int kRows = Narrow::kRows;
 
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
@@ -73,15 +37,15 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   constexpr int kTile = kTileKeys * G::kRow;
   constexpr int kDmas = 2 * G::kGroupDmas;  // of a K or V tile
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 2 * kTile];
-  __shared__ float part[4][kCacheRows][3];
+  __shared__ float part[4][kRows][3];
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
-  const UnitCost cost{g, a.hkv};
-  const int64_t total = total_work(a, cost);
-  const int64_t groups = min(static_cast<int64_t>(p.groups), total);
-  if (blockIdx.x >= groups) return;
-  int64_t x = share(blockIdx.x, total, groups);
-  const int64_t xend = share(blockIdx.x + 1, total, groups);
+  const UnitCost<Narrow> cost{g, a.hkv};
+  const Split split(total_work(a, cost), p.groups);
+  const int group = group_of(split);
+  if (group >= split.groups) return;
+  int x = split.at(group);
+  const int xend = split.at(group + 1);
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
@@ -96,18 +60,18 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   const float c = score_factor(a.sc);
 
   Place pl = find_work(a, x, cost);
-  while (x < xend) {
+  while (x < xend && pl.b < a.num_seqs) {
     // the unit that holds step x
-    const int b = uniform(pl.b);
+    const int b = pl.b;
     const Seq s = sequence(a, b);
     const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
     const int steps = uniform(cost.steps(s)), blocks = uniform(cost.blocks(s));
-    const int unit = uniform(static_cast<int>((x - pl.at) / steps));
-    const int s0 = uniform(static_cast<int>(x - pl.at - static_cast<int64_t>(unit) * steps));
-    const int s1 = uniform(static_cast<int>(min(static_cast<int64_t>(steps), s0 + (xend - x))));
-    const int kvh = unit / blocks, r0 = unit % blocks * kCacheRows;
-    const int ct = (len + kTileKeys - 1) / kTileKeys;  // tiles of cached keys
-    const int tiles = ct + (n + kTileKeys - 1) / kTileKeys;
+    const int unit = Split::quotient(x - pl.at, steps);
+    const int s0 = x - pl.at - unit * steps;
+    const int s1 = min(steps, s0 + (xend - x));
+    const int kvh = unit / blocks, r0 = unit % blocks * kRows;
+    const int ct = cost.cached_tiles(s);
+    const int tiles = cost.tiles(s);
 
     const int r = r0 + l32;
     const bool live = r < n * g;
@@ -255,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
       if (rr < n * g) {
         const bool whole = s0 == 0 && s1 == steps;
         const int64_t at = static_cast<int64_t>(row0 + rr / g) * a.hq + kvh * g + rr % g;
-        const int64_t slot = (2 * static_cast<int64_t>(blockIdx.x) + (s0 == 0)) * kCacheRows + row;
+        const int64_t slot = (2 * static_cast<int64_t>(group) + (s0 == 0)) * kRows + row;
         if ((threadIdx.x & 7) == 0) {
           if (!whole)
             p.part_ml[slot] = float4{top, l, le, 0.f};
@@ -289,32 +253,30 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
 
 // Merge of the parts of one (new token, query head), a workgroup each: eight
 // groups of 32 lanes take every eighth part, lane l dims l D / 32 and on.
-template <typename T, int D>
+template <typename U, typename T, int D>
 __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
   const CacheArgs& a = p.c;
   constexpr int kDims = D / 32;
   __shared__ float acc[8][D];
   __shared__ float part[8][2];
   const int g = a.hq / a.hkv;
-  const UnitCost cost{g, a.hkv};
+  const UnitCost<U> cost{g, a.hkv};
   const int64_t item = blockIdx.x;
   const int token = static_cast<int>(item / a.hq), h = static_cast<int>(item % a.hq);
-  const int64_t total = total_work(a, cost);
-  if (total == 0) return;
-  const int64_t groups = min(static_cast<int64_t>(p.groups), total);
+  const Split split(total_work(a, cost), p.groups);
+  if (split.total == 0) return;
   const Place pl = find_token(a, token, cost);
   if (pl.b >= a.num_seqs) return;  // no sequence's
   const Seq s = sequence(a, pl.b);
-  const int steps = cost.steps(s);
+  const int steps = uniform(cost.steps(s));
   const int r = (token - s.row0) * g + h % g;
-  const int64_t u0 =
-      pl.at + static_cast<int64_t>(h / g * cost.blocks(s) + r / kCacheRows) * steps;
-  const int64_t first = share_of(u0, total, groups);
-  const int n = static_cast<int>(share_of(u0 + steps - 1, total, groups) - first) + 1;
+  const int u0 = uniform(pl.at + (h / g * cost.blocks(s) + r / U::kRows) * steps);
+  const int first = split.of(u0);
+  const int n = split.of(u0 + steps - 1) - first + 1;
   if (n == 1) return;  // written already
   // the first part is its workgroup's second, the others their workgroups' first
   const auto slot = [&](int i) {
-    return (2 * (first + i) + (i == 0)) * kCacheRows + r % kCacheRows;
+    return (2 * static_cast<int64_t>(first + i) + (i == 0)) * U::kRows + r % U::kRows;
   };
   float top = -INFINITY;
   for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p.part_ml[slot(i)].x);
@@ -354,18 +316,45 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
 
 }  // namespace
 
+// Rows of a kv head beyond which bf16 goes by the wide units, whose 128 rows share
+// what the workgroup reads and whose matrix work is pipelined.
+constexpr int64_t kNarrowMost = 64;
+
+bool cache_attn_wide(bool bf16, int64_t rows_of_kv) { return bf16 && rows_of_kv > kNarrowMost; }
+
+int64_t cache_attn_steps(const CacheArgs& a) {
+  // of the narrow units: the wide ones are a quarter as many, of twice the steps
+  const int64_t units =
+      a.hkv * (static_cast<int64_t>(a.rows) * (a.hq / a.hkv) / kRows + a.num_seqs);
+  const int64_t keys = (static_cast<int64_t>(a.max_pages) << a.page_shift) +
+                       std::min(a.rows, a.max_rows) + 2 * kTileKeys;
+  return units * (keys / (kTileKeys * kStepTiles) + 1);
+}
+
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream) {
   if (a.c.rows == 0) return hipSuccess;
   const int64_t items = static_cast<int64_t>(a.c.rows) * a.c.hq;
   if (items >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
+  const int64_t most = static_cast<int64_t>(std::min(a.c.rows, a.c.max_rows)) * (a.c.hq / a.c.hkv);
+  const bool wide = cache_attn_wide(bf16, most);
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
-    hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), dim3(256), 0, stream, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cache_merge_kernel<T, D>), dim3(static_cast<unsigned>(items)), dim3(256),
-                       0, stream, a);
+    const dim3 grid(static_cast<unsigned>(items)), block(256);
+    if constexpr (Tile<T, D>::kBf16) {
+      if (wide) {
+        const hipError_t e = launch_cache_wide(a, D, stream);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL((cache_merge_kernel<Wide, T, D>), grid, block, 0, stream, a);
+        return hipGetLastError();
+      }
+    }
+    {
+      hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), block, 0, stream, a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a);
+    }
     return hipGetLastError();
   };
   using D64 = std::integral_constant<int, 64>;

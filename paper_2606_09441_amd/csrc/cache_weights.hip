@@ -32,9 +32,7 @@ struct KeyCost {
   static __device__ __forceinline__ int steps(const Seq& s) {
     return (s.len + kStepKeys - 1) / kStepKeys;
   }
-  __device__ __forceinline__ int64_t operator()(const Seq& s) const {
-    return static_cast<int64_t>(hkv) * steps(s);
-  }
+  __device__ __forceinline__ int operator()(const Seq& s) const { return hkv * steps(s); }
 };
 
 template <typename T, int D>
@@ -45,11 +43,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
   const KeyCost cost{a.hkv};
-  const int64_t total = total_work(a, cost);
-  const int64_t groups = min(static_cast<int64_t>(p.groups), total);
-  if (blockIdx.x >= groups) return;
-  int64_t x = share(blockIdx.x, total, groups);
-  const int64_t xend = share(blockIdx.x + 1, total, groups);
+  const Split split(total_work(a, cost), p.groups);
+  const int group = group_of(split);
+  if (group >= split.groups) return;
+  int x = split.at(group);
+  const int xend = split.at(group + 1);
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
@@ -62,14 +60,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
   const bool bias = a.sc.slopes != nullptr;
 
   Place pl = find_work(a, x, cost);
-  while (x < xend) {
-    const int b = uniform(pl.b);
+  while (x < xend && pl.b < a.num_seqs) {
+    const int b = pl.b;
     const Seq s = sequence(a, b);
     const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
     const int steps = uniform(cost.steps(s));
-    const int kvh = uniform(static_cast<int>((x - pl.at) / steps));
-    const int s0 = uniform(static_cast<int>(x - pl.at - static_cast<int64_t>(kvh) * steps));
-    const int s1 = uniform(static_cast<int>(min(static_cast<int64_t>(steps), s0 + (xend - x))));
+    const int kvh = Split::quotient(x - pl.at, steps);
+    const int s0 = x - pl.at - kvh * steps;
+    const int s1 = min(steps, s0 + (xend - x));
     const int64_t at0 = (static_cast<int64_t>(b) * a.hkv + kvh) * slots;
     const int rows = n * g;
 
@@ -185,6 +183,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
 }
 
 }  // namespace
+
+int64_t cache_weights_steps(const CacheArgs& a) {
+  return static_cast<int64_t>(a.num_seqs) * a.hkv *
+         (((static_cast<int64_t>(a.max_pages) << a.page_shift) + kStepKeys - 1) / kStepKeys);
+}
 
 hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int cus,
                                 hipStream_t stream) {

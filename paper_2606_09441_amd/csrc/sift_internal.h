@@ -461,14 +461,20 @@ struct CacheAttnArgs {
   void* out;                 // [rows][hq][D]
   float* lse;                // [rows][hq] or nullptr
   // partial results of units that more than one workgroup shares: two slots a
-  // workgroup, 32 rows each
-  float* part_o;             // [slots][32][D], not normalised
-  float4* part_ml;           // [slots][32] {reference max, sum, sum before rounding, 0}
+  // workgroup, of a unit's rows each
+  float* part_o;             // [slots][rows][D], not normalised
+  float4* part_ml;           // [slots][rows] {reference max, sum, sum before rounding, 0}
   int32_t groups;            // workgroups of the launch
 };
 
-constexpr int kCacheRows = 32;  // rows (new token, query head of the kv head) of a unit
-constexpr int64_t kCacheSlotRows = 2 * kCacheRows;  // partial rows of a workgroup
+// Rows (new token, query head of the kv head) of a unit: 32, or where there are
+// many (cache_attn_wide) 128.
+constexpr int kCacheRows = 32, kCacheWideRows = 128;
+// rows_of_kv: the most rows of a (sequence, kv head).  A launch's list of steps
+// (cache_attn_steps bounds it) has to be shorter than 2^31.
+bool cache_attn_wide(bool bf16, int64_t rows_of_kv);
+int64_t cache_attn_steps(const CacheArgs& a);
+hipError_t launch_cache_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream);
 
 // Accumulated attention weights (cache_weights.hip); c.sc in the natural domain.
@@ -482,7 +488,8 @@ struct CacheWeightArgs {
   int32_t chunk_rows;        // rows of q that a workgroup holds in LDS, a multiple of 32
   int32_t groups;            // workgroups of the launch
 };
-// chunk_rows and groups are set by the launch.
+// chunk_rows and groups are set by the launch; its list of steps too is bounded.
+int64_t cache_weights_steps(const CacheArgs& a);
 hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int cus,
                                 hipStream_t stream);
 
