@@ -5,10 +5,15 @@
 //
 // S = Q K^T with the rows on M and the keys on N, so that a lane holds one key's
 // scores for 16 rows of a block of 32 and their sum is in-lane but for one
-// exchange.  A wavefront keeps 32 keys in registers, read straight from the
-// pages, and walks the row blocks of Q, which the workgroup holds in LDS; the
-// next 32 keys are on their way meanwhile.  K is read once (for every chunk_rows
-// rows) and a key's sum is made by one lane in row order: no atomics.
+// exchange.  A wavefront keeps 32 keys in registers and walks the row blocks of Q,
+// which the workgroup holds in LDS; while the VALU makes the weights of a block
+// the matrix cores form the scores of the next.  K is read once (for every
+// chunk_rows rows) and a key's sum is made by one lane in row order: no atomics.
+//  * Few rows (one block or two): HBM bounds it.  K comes by DMA through LDS of
+//    the wavefront's own, whole lines at a time, the next tile as soon as the
+//    present one is in registers.
+//  * Many rows: their Q takes that LDS, the VALU (four instructions and an
+//    exponential a score) bounds it, and K goes straight to registers.
 //
 // The exponent is formed as scale * q.k - lse in the natural domain and only
 // then multiplied by log2(e): the two are large and nearly equal for the keys
@@ -26,6 +31,8 @@ using namespace cache;
 
 constexpr int kWaves = 8;
 constexpr int kStepKeys = 32 * kWaves;  // a step: 32 keys of each wavefront
+constexpr int kMostBlocks = 32;         // of 32 rows in LDS
+constexpr int kFewRows = 64;            // up to which K comes through LDS
 
 struct KeyCost {
   int32_t hkv;
@@ -35,11 +42,14 @@ struct KeyCost {
   __device__ __forceinline__ int operator()(const Seq& s) const { return hkv * steps(s); }
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeightArgs p) {
+template <typename T, int D, bool kDma>
+__global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) void cache_weights_kernel(CacheWeightArgs p) {
   using G = Tile<T, D>;
-  // chunk_rows rows of Q, swizzled as K tiles are, then {lse, slope, position} of each
+  constexpr int kTile = 32 * G::kRow;
+  // chunk_rows rows of Q, swizzled as K tiles are, then {lse, slope, position} of
+  // each, then (kDma) a K tile of each wavefront
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
+  __shared__ int dead[kMostBlocks];  // whether a block has rows that count for nothing
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
   const KeyCost cost{a.hkv};
@@ -53,11 +63,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
   const int wave = uniform(threadIdx.x >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
   const int slots = a.max_pages << a.page_shift;
+  const int stride = a.hkv * G::kRow;
   const int lds0 = static_cast<int>(reinterpret_cast<size_t>((lds_u8*)smem));
   const int qaddr = lds0 + G::lane_k(l32, hf);
-  const int lse0 = lds0 + p.chunk_rows * G::kRow;  // three float arrays of chunk_rows
+  const int lse0 = lds0 + p.chunk_rows * G::kRow;  // three arrays of chunk_rows
   const int slope0 = lse0 + 4 * p.chunk_rows, pos0 = slope0 + 4 * p.chunk_rows;
+  const int kt = lds0 + (p.chunk_rows * (G::kRow + 12) + 1023) / 1024 * 1024 + wave * kTile;
+  const int kaddr = kt + G::lane_k(l32, hf);
+  const int koff = G::template dma_lane<false>(lane, stride);
   const bool bias = a.sc.slopes != nullptr;
+  const float c = a.sc.x != 0.f ? 1.f : a.sc.c;
 
   Place pl = find_work(a, x, cost);
   while (x < xend && pl.b < a.num_seqs) {
@@ -75,16 +90,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
       const int cn = min(rows - c0, p.chunk_rows);
       const int blocks = (cn + 31) / 32;
       __syncthreads();  // the last chunk is read
-      for (int e = threadIdx.x; e < blocks * 32 * G::kChunks; e += 64 * kWaves) {
-        const int i = e / G::kChunks, ch = e % G::kChunks, r = c0 + i;
-        u32x4 y = u32x4{0u, 0u, 0u, 0u};
-        if (i < cn)
-          y = *reinterpret_cast<const u32x4*>(
-              static_cast<const uint8_t*>(a.q) +
-              (static_cast<int64_t>(row0 + r / g) * a.hq + kvh * g + r % g) * G::kRow + 16 * ch);
-        *reinterpret_cast<lds_u32x4*>(
-            static_cast<size_t>(lds0 + i * G::kRow + 16 * (ch ^ G::swz_k(i)))) = y;
-      }
+      if (threadIdx.x < kMostBlocks) dead[threadIdx.x] = 0;
+      __syncthreads();
       for (int i = threadIdx.x; i < blocks * 32; i += 64 * kWaves) {
         const int r = c0 + i, tok = row0 + r / g, h = kvh * g + r % g;
         // a row without weight or keys, or none: +inf, its weights are 0
@@ -99,82 +106,191 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_weights_kernel(CacheWeig
             pos = a.row_pos != nullptr ? a.row_pos[tok] : len + r / g;
           }
         }
+        if (l == INFINITY) dead[i / 32] = 1;
         *reinterpret_cast<lds_float*>(static_cast<size_t>(lse0 + 4 * i)) = l;
         *reinterpret_cast<lds_float*>(static_cast<size_t>(slope0 + 4 * i)) = slope;
         *reinterpret_cast<lds_int*>(static_cast<size_t>(pos0 + 4 * i)) = pos;
       }
       __syncthreads();
+      for (int e = threadIdx.x; e < blocks * 32 * G::kChunks; e += 64 * kWaves) {
+        const int i = e / G::kChunks, ch = e % G::kChunks, r = c0 + i;
+        u32x4 y = u32x4{0u, 0u, 0u, 0u};
+        if (*reinterpret_cast<const lds_float*>(static_cast<size_t>(lse0 + 4 * i)) != INFINITY)
+          y = *reinterpret_cast<const u32x4*>(
+              static_cast<const uint8_t*>(a.q) +
+              (static_cast<int64_t>(row0 + r / g) * a.hq + kvh * g + r % g) * G::kRow + 16 * ch);
+        *reinterpret_cast<lds_u32x4*>(
+            static_cast<size_t>(lds0 + i * G::kRow + 16 * (ch ^ G::swz_k(i)))) = y;
+      }
+      __syncthreads();
+      const uint32_t dead_blocks =
+          static_cast<uint32_t>(__ballot(lane < kMostBlocks && dead[lane % kMostBlocks] != 0));
 
-      // this lane's key of tile t: row l32
-      const auto key_at = [&](int t, bool& valid) {
-        const int slot = t * 32 + 16 * (l32 >> 4);
-        const Rows16 lo = cached_rows(a, b, len, t * 32), hi = cached_rows(a, b, len, t * 32 + 16);
-        const Rows16 r = l32 < 16 ? lo : hi;
-        valid = slot < slots && (l32 & 15) < r.n;
-        return static_cast<const uint8_t*>(a.k) + ((r.row + (l32 & 15)) * a.hkv + kvh) * G::kRow +
-               16 * hf;
+      // A tile's keys: to LDS (kDma) or to registers, with what else a lane needs of
+      // its key (lane l32).
+      struct Key {
+        float old;
+        int pos;
+        bool valid;
       };
-      u32x4 kf[G::kSteps], kn[G::kSteps];
-      bool valid = false, valid_next = false;
-      const auto load = [&](int t, u32x4(&dst)[G::kSteps], bool& ok) {
-        const uint8_t* src = key_at(t, ok);
-#pragma unroll
-        for (int i = 0; i < G::kSteps; ++i) {
-          dst[i] = u32x4{0u, 0u, 0u, 0u};
-          if (ok) dst[i] = *reinterpret_cast<const u32x4*>(src + 32 * i);
-        }
-      };
-      const int tend = min((len + 31) / 32, s1 * kWaves);
-      int t = s0 * kWaves + wave;
-      if (t < tend) load(t, kf, valid);
-      for (; t < tend; t += kWaves) {
-        if (t + kWaves < tend) load(t + kWaves, kn, valid_next);
+      const auto fetch = [&](int t, u32x4(&dst)[G::kSteps], Key& k) {
+        const Rows16 r0 = cached_rows(a, b, len, t * 32), r1 = cached_rows(a, b, len, t * 32 + 16);
         const int slot = t * 32 + l32;
-        float old = 0.f;
+        const Rows16 r = l32 < 16 ? r0 : r1;
+        k.valid = (l32 & 15) < r.n;
+        if constexpr (kDma) {
+          dma_rows<T, D, false>(kt, rows_rsrc(reinterpret_cast<unsigned long long>(a.k) +
+                                                  (r0.row * a.hkv + kvh) * G::kRow,
+                                              r0.n, stride, G::kRow), koff, stride);
+          dma_rows<T, D, false>(kt + 16 * G::kRow,
+                                rows_rsrc(reinterpret_cast<unsigned long long>(a.k) +
+                                              (r1.row * a.hkv + kvh) * G::kRow,
+                                          r1.n, stride, G::kRow), koff, stride);
+        } else {
+          const uint8_t* src = static_cast<const uint8_t*>(a.k) +
+                               ((r.row + (l32 & 15)) * a.hkv + kvh) * G::kRow + 16 * hf;
+#pragma unroll
+          for (int i = 0; i < G::kSteps; ++i) {
+            dst[i] = u32x4{0u, 0u, 0u, 0u};
+            if (k.valid) dst[i] = *reinterpret_cast<const u32x4*>(src + 32 * i);
+          }
+        }
+        k.old = 0.f;
         if (slot < len && hf == 0) {
           if (c0 > 0)
-            old = p.out[at0 + slot];
+            k.old = p.out[at0 + slot];
           else if (p.weights != nullptr && p.decay != 0.f)
-            old = p.decay * p.weights[at0 + slot];
+            k.old = p.decay * p.weights[at0 + slot];
         }
-        int kpos = slot;
-        if (bias && a.key_pos != nullptr) kpos = a.key_pos[at0 + min(slot, slots - 1)];
-        float sum = 0.f;
-        for (int rb = 0; rb < blocks; ++rb) {
+        k.pos = bias && a.key_pos != nullptr ? a.key_pos[at0 + min(slot, slots - 1)] : slot;
+      };
+
+      u32x4 kf[G::kSteps], kn[G::kSteps];
+      Key key{0.f, 0, false}, next{0.f, 0, false};
+      const int tend = min((len + 31) / 32, s1 * kWaves);
+      int t = s0 * kWaves + wave;
+      if (t < tend) fetch(t, kDma ? kn : kf, kDma ? next : key);
+      for (; t < tend; t += kWaves) {
+        if constexpr (kDma) {
+          wait_vm<0>();
+          key = next;
+#pragma unroll
+          for (int i = 0; i < G::kSteps; ++i) kf[i] = G::k_frag(kaddr, 0, i);
+          wait_lds();  // the tile is in registers
+        }
+        if (t + kWaves < tend) fetch(t + kWaves, kn, next);
+
+        // Scores of row block rb, transformed; lane's key, registers' rows.
+        const auto transform = [&](int rb, f32x16& sc) {
+          if (a.sc.x != 0.f) cap_scores(a.sc, sc);
+          if (bias) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int off = 4 * (32 * rb + 8 * j + 4 * hf);
+              const f32x4 sl =
+                  *reinterpret_cast<const lds_f32x4*>(static_cast<size_t>(slope0 + off));
+              const i32x4 ps = *reinterpret_cast<const lds_i32x4*>(static_cast<size_t>(pos0 + off));
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                sc[4 * j + e] = fmaf(sc[4 * j + e], c,
+                                     -sl[e] * fabsf(static_cast<float>(ps[e] - key.pos)));
+            }
+          }
+        };
+        const float cc = bias ? 1.f : c;
+        const auto row_lse = [&](int rb, f32x4(&l)[4]) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            l[j] = *reinterpret_cast<const lds_f32x4*>(
+                static_cast<size_t>(lse0 + 4 * (32 * rb + 8 * j + 4 * hf)));
+        };
+        const auto weight = [&](const f32x16& sc, const f32x4(&l)[4], int v) {
+          return __builtin_amdgcn_exp2f(fmaf(sc[v], cc, -l[v >> 2][v & 3]) * kLog2e);
+        };
+        // The sum of a block's weights, rows that count for nothing left out,
+        // whatever the key holds.
+        const auto careful = [&](const f32x16& sc, const f32x4(&l)[4]) {
+          float part[2] = {0.f, 0.f};
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float w = weight(sc, l, v);
+            part[v & 1] += l[v >> 2][v & 3] < INFINITY ? w : 0.f;
+          }
+          return part[0] + part[1];
+        };
+        const auto scores = [&](int rb) {
           f32x16 sc = f32x16{};
 #pragma unroll
           for (int i = 0; i < G::kSteps; ++i)
             sc = dot_step<T>(G::k_frag(qaddr + rb * 32 * G::kRow, 0, i), kf[i], sc);
-          const int left = cn - 32 * rb;
-          if (a.sc.x != 0.f) cap_scores(a.sc, sc);
-          const float c = a.sc.x != 0.f ? 1.f : a.sc.c;
-          float part = 0.f;
+          return sc;
+        };
+        float sum = 0.f;
+        if constexpr (kDma) {
+          for (int rb = 0; rb < blocks; ++rb) {
+            f32x4 l[4];
+            row_lse(rb, l);
+            f32x16 sc = scores(rb);
+            transform(rb, sc);
+            sum += careful(sc, l);
+          }
+        } else {
+          // block rb's weights beside block rb + 1's scores; the fragments three
+          // steps ahead and the log sums a block ahead, across the blocks (past the
+          // last one the first again, for nothing)
+          const auto block_at = [&](int rb) {
+            return qaddr + (rb < blocks ? rb : 0) * 32 * G::kRow;
+          };
+          constexpr int kAhead = 3, kEach = 16 / G::kSteps > 0 ? 16 / G::kSteps : 1;
+          u32x4 f[kAhead];
+          const auto body = [&](int rb, f32x16& cur, f32x4(&l)[4], f32x16& nxt, f32x4(&ln)[4]) {
+            row_lse(rb + 1 < blocks ? rb + 1 : 0, ln);
+            if ((dead_blocks >> rb) & 1) {
+              sum += careful(cur, l);
+              nxt = scores(rb + 1 < blocks ? rb + 1 : 0);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (8 * j >= left) break;  // the block's rows end before
-            const int off = 4 * (32 * rb + 8 * j + 4 * hf);
-            const f32x4 l = *reinterpret_cast<const lds_f32x4*>(static_cast<size_t>(lse0 + off));
-            f32x4 sl = f32x4{0.f, 0.f, 0.f, 0.f};
-            i32x4 ps = i32x4{0, 0, 0, 0};
-            if (bias) {
-              sl = *reinterpret_cast<const lds_f32x4*>(static_cast<size_t>(slope0 + off));
-              ps = *reinterpret_cast<const lds_i32x4*>(static_cast<size_t>(pos0 + off));
+              for (int i = 0; i < kAhead; ++i) f[i] = G::k_frag(block_at(rb + 2), 0, i);
+            } else {
+              float part[2] = {0.f, 0.f};
+              const int q1 = block_at(rb + 1), q2 = block_at(rb + 2);
+              u32x4 h[kAhead] = {f[0], f[1], f[2]};
+              nxt = f32x16{};
+#pragma unroll
+              for (int i = 0; i < G::kSteps; ++i) {
+                nxt = dot_step<T>(h[i % kAhead], kf[i], nxt);
+                const int j = i + kAhead;
+                h[i % kAhead] = j < G::kSteps ? G::k_frag(q1, 0, j) : G::k_frag(q2, 0, j - G::kSteps);
+#pragma unroll
+                for (int u = 0; u < kEach; ++u) part[u & 1] += weight(cur, l, i * kEach + u);
+                __builtin_amdgcn_sched_barrier(0);
+              }
+#pragma unroll
+              for (int i = 0; i < kAhead; ++i) f[i] = h[(G::kSteps + i) % kAhead];
+              sum += part[0] + part[1];
             }
+            transform(rb + 1 < blocks ? rb + 1 : 0, nxt);
+          };
+          if (blocks > 0) {
+            f32x16 s0_ = scores(0), s1_;
+            f32x4 l0[4], l1[4];
+            row_lse(0, l0);
+            transform(0, s0_);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float y = fmaf(sc[4 * j + e], c, -l[e]);
-              if (bias) y = fmaf(-sl[e], fabsf(static_cast<float>(ps[e] - kpos)), y);
-              const float w = __builtin_amdgcn_exp2f(y * kLog2e);
-              part += l[e] < INFINITY ? w : 0.f;
+            for (int i = 0; i < kAhead; ++i) f[i] = G::k_frag(block_at(1), 0, i);
+            for (int rb = 0; rb < blocks; rb += 2) {
+              body(rb, s0_, l0, s1_, l1);
+              if (rb + 1 < blocks) body(rb + 1, s1_, l1, s0_, l0);
             }
           }
-          sum += part;
         }
         sum = half_sum(sum);
-        if (slot < len && hf == 0) p.out[at0 + slot] = valid ? old + sum : 0.f;
+        const int slot = t * 32 + l32;
+        if (slot < len && hf == 0) p.out[at0 + slot] = key.valid ? key.old + sum : 0.f;
+        if constexpr (!kDma) {
 #pragma unroll
-        for (int i = 0; i < G::kSteps; ++i) kf[i] = kn[i];
-        valid = valid_next;
+          for (int i = 0; i < G::kSteps; ++i) kf[i] = kn[i];
+          key = next;
+        }
       }
     }
     x += s1 - s0;
@@ -196,13 +312,20 @@ hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int 
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
     constexpr int kRowLds = Tile<T, D>::kRow + 12;
-    constexpr int kFit = 144 * 1024 / kRowLds / 32 * 32;  // rows that 144 KB hold
+    constexpr int kKeyLds = kWaves * 32 * Tile<T, D>::kRow + 1024;
+    constexpr int kFit = std::min(144 * 1024 / kRowLds, 32 * kMostBlocks) / 32 * 32;
     const int64_t need = std::max<int64_t>(32, (most + 31) / 32 * 32);
     a.chunk_rows = static_cast<int32_t>(std::min<int64_t>(need, kFit));
-    const int lds = a.chunk_rows * kRowLds;
-    a.groups = cus * (lds <= 72 * 1024 ? 2 : 1);
-    hipLaunchKernelGGL((cache_weights_kernel<T, D>), dim3(a.groups), dim3(64 * kWaves), lds,
-                       stream, a);
+    int lds = a.chunk_rows * kRowLds;
+    const bool dma = need <= kFewRows && lds + kKeyLds <= 158 * 1024;
+    if (dma) lds += kKeyLds;
+    a.groups = cus * (lds <= 79 * 1024 ? 2 : 1);
+    if (dma)
+      hipLaunchKernelGGL((cache_weights_kernel<T, D, true>), dim3(a.groups), dim3(64 * kWaves), lds,
+                         stream, a);
+    else
+      hipLaunchKernelGGL((cache_weights_kernel<T, D, false>), dim3(a.groups), dim3(64 * kWaves),
+                         lds, stream, a);
     return hipGetLastError();
   };
   using D64 = std::integral_constant<int, 64>;
