@@ -192,9 +192,15 @@ def check(fn: str, status: int) -> None:
 # ----------------------------------------------------------------------------
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def tensor_desc(t) -> SiftTensor:
@@ -268,9 +274,13 @@ def layout_struct(seg_offsets, prompt_seg_ptr):
 
 
 def _stream_ptr(stream):
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
     torch = _torch()
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object
+    if raw is not None:
+        return ctypes.c_void_p(raw(torch.cuda.current_device()))
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 def _ptr(t):

@@ -42,6 +42,10 @@ __device__ __forceinline__ int wave_sum(int x) {
   return uniform(x);
 }
 
+__device__ __forceinline__ int lane_value(int x, int lane) {
+  return __builtin_amdgcn_readlane(x, lane);
+}
+
 // The work of all sequences, cost(Seq) steps each, one after another: fewer than
 // 2^31 (checked by the host).  All uniform.
 struct Place {
@@ -50,53 +54,77 @@ struct Place {
 };
 
 template <typename Cost>
-__device__ __forceinline__ int total_work(const CacheArgs& a, Cost cost) {
-  int sum = 0;
-  for (int b = threadIdx.x & 63; b < a.num_seqs; b += 64) sum += cost(sequence(a, b));
-  return wave_sum(sum);
-}
-
-template <typename Cost>
-__device__ __forceinline__ Place find_work(const CacheArgs& a, int x, Cost cost) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
-    const int mine = b0 + lane < a.num_seqs ? cost(sequence(a, b0 + lane)) : 0;
-    int upto = mine;  // inclusive scan
+struct Work {
+  const CacheArgs& a;
+  const Cost cost;
+  // of sequence `lane`, the first 64: their sizes, and their steps with those before
+  Seq mine;
+  int upto;
+  int first, total;  // steps of the first 64, and of all
+  __device__ __forceinline__ Work(const CacheArgs& args, Cost c) : a(args), cost(c) {
+    const int lane = threadIdx.x & 63;
+    mine = sequence(a, min(lane, a.num_seqs - 1));
+    upto = scan(lane < a.num_seqs ? cost(mine) : 0);
+    first = total = lane_value(upto, 63);
+    if (a.num_seqs <= 64) return;
+    int sum = 0;
+    for (int b = 64 + lane; b < a.num_seqs; b += 64) sum += cost(sequence(a, b));
+    total += wave_sum(sum);
+  }
+  static __device__ __forceinline__ int scan(int x) {  // inclusive
+    const int lane = threadIdx.x & 63;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(upto, d);
-      if (lane >= d) upto += y;
+      const int y = __shfl_up(x, d);
+      if (lane >= d) x += y;
     }
-    const uint64_t past = __ballot(before + upto > x);
-    if (past != 0) {
-      const int l = __ffsll(static_cast<unsigned long long>(past)) - 1;
-      return Place{b0 + l, uniform(before + __shfl(upto - mine, l))};
-    }
-    before += uniform(__shfl(upto, 63));
+    return x;
   }
-  return Place{a.num_seqs, before};
-}
-
-// The sequence that new token `token` belongs to (num_seqs: none), and its first
-// step.
-template <typename Cost>
-__device__ __forceinline__ Place find_token(const CacheArgs& a, int token, Cost cost) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  for (int b0 = 0; b0 < a.num_seqs; b0 += 64) {
-    const bool in = b0 + lane < a.num_seqs;
-    const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
-    const int mine = in ? cost(s) : 0;
-    const uint64_t has = __ballot(in && token >= s.row0 && token < s.row0 + s.n);
-    if (has != 0) {
-      const int l = __ffsll(static_cast<unsigned long long>(has)) - 1;
-      return Place{b0 + l, before + wave_sum(lane < l ? mine : 0)};
-    }
-    before += wave_sum(mine);
+  static __device__ __forceinline__ Place among(int b0, int before, int upto, int x) {
+    const int l =
+        __ffsll(static_cast<unsigned long long>(__ballot(before + upto > x))) - 1;  // there is one
+    return Place{b0 + l, before + (l > 0 ? lane_value(upto, l - 1) : 0)};
   }
-  return Place{a.num_seqs, before};
-}
+  // The place of step x.
+  __device__ __forceinline__ Place find(int x) const {
+    if (x < first) return among(0, 0, upto, x);
+    const int lane = threadIdx.x & 63;
+    int before = first;
+    for (int b0 = 64; b0 < a.num_seqs; b0 += 64) {
+      const int u = scan(b0 + lane < a.num_seqs ? cost(sequence(a, b0 + lane)) : 0);
+      const int all = lane_value(u, 63);
+      if (x < before + all) return among(b0, before, u, x);
+      before += all;
+    }
+    return Place{a.num_seqs, before};
+  }
+  // The sequence that new token `token` belongs to, and its first step.
+  __device__ __forceinline__ Place find_token(int token) const {
+    const int lane = threadIdx.x & 63;
+    const auto has = [&](const Seq& s, bool in) {
+      return __ballot(in && token >= s.row0 && token < s.row0 + s.n);
+    };
+    uint64_t m = has(mine, lane < a.num_seqs);
+    int before = 0, u = upto, b0 = 0;
+    while (m == 0) {
+      before += lane_value(u, 63);
+      b0 += 64;
+      if (b0 >= a.num_seqs) return Place{a.num_seqs, before};
+      const Seq s = sequence(a, min(b0 + lane, a.num_seqs - 1));
+      const bool in = b0 + lane < a.num_seqs;
+      u = scan(in ? cost(s) : 0);
+      m = has(s, in);
+    }
+    const int l = __ffsll(static_cast<unsigned long long>(m)) - 1;
+    return Place{b0 + l, before + (l > 0 ? lane_value(u, l - 1) : 0)};
+  }
+  __device__ __forceinline__ Seq seq(int b) const {
+    if (b < 64) return Seq{lane_value(mine.len, b), lane_value(mine.row0, b), lane_value(mine.n, b)};
+    if (b >= a.num_seqs) return Seq{0, 0, 0};
+    const Seq s = sequence(a, b);
+    return Seq{uniform(s.len), uniform(s.row0), uniform(s.n)};
+  }
+};
 
 // An even split of `total` steps over the workgroups of a launch, or over as many
 // as there are steps: workgroup i takes those from at(i) to at(i + 1).

@@ -41,11 +41,19 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
   const UnitCost<Narrow> cost{g, a.hkv};
-  const Split split(total_work(a, cost), p.groups);
-  const int group = group_of(split);
-  if (group >= split.groups) return;
-  int x = split.at(group);
-  const int xend = split.at(group + 1);
+  int group, x, xend;
+  Place pl;
+  Seq s;
+  {
+    const Work work(a, cost);
+    const Split split(work.total, p.groups);
+    group = group_of(split);
+    if (group >= split.groups) return;
+    x = split.at(group);
+    xend = split.at(group + 1);
+    pl = work.find(x);
+    s = work.seq(pl.b);
+  }
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
@@ -59,12 +67,10 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
   const int voff = G::template dma_lane<true>(lane, stride);
   const float c = score_factor(a.sc);
 
-  Place pl = find_work(a, x, cost);
   while (x < xend && pl.b < a.num_seqs) {
     // the unit that holds step x
     const int b = pl.b;
-    const Seq s = sequence(a, b);
-    const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
+    const int len = s.len, n = s.n, row0 = s.row0;
     const int steps = uniform(cost.steps(s)), blocks = uniform(cost.blocks(s));
     const int unit = Split::quotient(x - pl.at, steps);
     const int s0 = x - pl.at - unit * steps;
@@ -247,7 +253,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
     }
     __syncthreads();  // the tiles' memory is free again
     x += s1 - s0;
-    if (x < xend && x - pl.at >= cost(s)) pl = find_work(a, x, cost);
+    if (x < xend && x - pl.at >= cost(s)) {
+      const Work work(a, cost);
+      pl = work.find(x);
+      s = work.seq(pl.b);
+    }
   }
 }
 
@@ -263,11 +273,12 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
   const UnitCost<U> cost{g, a.hkv};
   const int64_t item = blockIdx.x;
   const int token = static_cast<int>(item / a.hq), h = static_cast<int>(item % a.hq);
-  const Split split(total_work(a, cost), p.groups);
+  const Work work(a, cost);
+  const Split split(work.total, p.groups);
   if (split.total == 0) return;
-  const Place pl = find_token(a, token, cost);
+  const Place pl = work.find_token(token);
   if (pl.b >= a.num_seqs) return;  // no sequence's
-  const Seq s = sequence(a, pl.b);
+  const Seq s = work.seq(pl.b);
   const int steps = uniform(cost.steps(s));
   const int r = (token - s.row0) * g + h % g;
   const int u0 = uniform(pl.at + (h / g * cost.blocks(s) + r / U::kRows) * steps);

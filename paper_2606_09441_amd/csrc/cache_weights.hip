@@ -53,11 +53,19 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
   const KeyCost cost{a.hkv};
-  const Split split(total_work(a, cost), p.groups);
-  const int group = group_of(split);
-  if (group >= split.groups) return;
-  int x = split.at(group);
-  const int xend = split.at(group + 1);
+  int group, x, xend;
+  Place pl;
+  Seq s;
+  {
+    const Work work(a, cost);
+    const Split split(work.total, p.groups);
+    group = group_of(split);
+    if (group >= split.groups) return;
+    x = split.at(group);
+    xend = split.at(group + 1);
+    pl = work.find(x);
+    s = work.seq(pl.b);
+  }
 
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
@@ -74,11 +82,9 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
   const bool bias = a.sc.slopes != nullptr;
   const float c = a.sc.x != 0.f ? 1.f : a.sc.c;
 
-  Place pl = find_work(a, x, cost);
   while (x < xend && pl.b < a.num_seqs) {
     const int b = pl.b;
-    const Seq s = sequence(a, b);
-    const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
+    const int len = s.len, n = s.n, row0 = s.row0;
     const int steps = uniform(cost.steps(s));
     const int kvh = Split::quotient(x - pl.at, steps);
     const int s0 = x - pl.at - kvh * steps;
@@ -89,42 +95,6 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
     for (int c0 = 0; c0 == 0 || c0 < rows; c0 += p.chunk_rows) {
       const int cn = min(rows - c0, p.chunk_rows);
       const int blocks = (cn + 31) / 32;
-      __syncthreads();  // the last chunk is read
-      if (threadIdx.x < kMostBlocks) dead[threadIdx.x] = 0;
-      __syncthreads();
-      for (int i = threadIdx.x; i < blocks * 32; i += 64 * kWaves) {
-        const int r = c0 + i, tok = row0 + r / g, h = kvh * g + r % g;
-        // a row without weight or keys, or none: +inf, its weights are 0
-        float l = INFINITY, slope = 0.f;
-        int pos = 0;
-        if (i < cn) {
-          const float f = p.row_weight != nullptr ? p.row_weight[tok] : 1.f;
-          const float y = p.lse[static_cast<int64_t>(tok) * a.hq + h];
-          if (f != 0.f && y != -INFINITY) l = f == 1.f ? y : y - logf(f);
-          if (bias) {
-            slope = a.sc.slopes[h];
-            pos = a.row_pos != nullptr ? a.row_pos[tok] : len + r / g;
-          }
-        }
-        if (l == INFINITY) dead[i / 32] = 1;
-        *reinterpret_cast<lds_float*>(static_cast<size_t>(lse0 + 4 * i)) = l;
-        *reinterpret_cast<lds_float*>(static_cast<size_t>(slope0 + 4 * i)) = slope;
-        *reinterpret_cast<lds_int*>(static_cast<size_t>(pos0 + 4 * i)) = pos;
-      }
-      __syncthreads();
-      for (int e = threadIdx.x; e < blocks * 32 * G::kChunks; e += 64 * kWaves) {
-        const int i = e / G::kChunks, ch = e % G::kChunks, r = c0 + i;
-        u32x4 y = u32x4{0u, 0u, 0u, 0u};
-        if (*reinterpret_cast<const lds_float*>(static_cast<size_t>(lse0 + 4 * i)) != INFINITY)
-          y = *reinterpret_cast<const u32x4*>(
-              static_cast<const uint8_t*>(a.q) +
-              (static_cast<int64_t>(row0 + r / g) * a.hq + kvh * g + r % g) * G::kRow + 16 * ch);
-        *reinterpret_cast<lds_u32x4*>(
-            static_cast<size_t>(lds0 + i * G::kRow + 16 * (ch ^ G::swz_k(i)))) = y;
-      }
-      __syncthreads();
-      const uint32_t dead_blocks =
-          static_cast<uint32_t>(__ballot(lane < kMostBlocks && dead[lane % kMostBlocks] != 0));
 
       // A tile's keys: to LDS (kDma) or to registers, with what else a lane needs of
       // its key (lane l32).
@@ -170,6 +140,44 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
       const int tend = min((len + 31) / 32, s1 * kWaves);
       int t = s0 * kWaves + wave;
       if (t < tend) fetch(t, kDma ? kn : kf, kDma ? next : key);
+
+      __syncthreads();  // the last chunk is read
+      if (threadIdx.x < kMostBlocks) dead[threadIdx.x] = 0;
+      __syncthreads();
+      for (int i = threadIdx.x; i < blocks * 32; i += 64 * kWaves) {
+        const int r = c0 + i, tok = row0 + r / g, h = kvh * g + r % g;
+        // a row without weight or keys, or none: +inf, its weights are 0
+        float l = INFINITY, slope = 0.f;
+        int pos = 0;
+        if (i < cn) {
+          const float f = p.row_weight != nullptr ? p.row_weight[tok] : 1.f;
+          const float y = p.lse[static_cast<int64_t>(tok) * a.hq + h];
+          if (f != 0.f && y != -INFINITY) l = f == 1.f ? y : y - logf(f);
+          if (bias) {
+            slope = a.sc.slopes[h];
+            pos = a.row_pos != nullptr ? a.row_pos[tok] : len + r / g;
+          }
+        }
+        if (l == INFINITY) dead[i / 32] = 1;
+        *reinterpret_cast<lds_float*>(static_cast<size_t>(lse0 + 4 * i)) = l;
+        *reinterpret_cast<lds_float*>(static_cast<size_t>(slope0 + 4 * i)) = slope;
+        *reinterpret_cast<lds_int*>(static_cast<size_t>(pos0 + 4 * i)) = pos;
+      }
+      __syncthreads();
+      for (int e = threadIdx.x; e < blocks * 32 * G::kChunks; e += 64 * kWaves) {
+        const int i = e / G::kChunks, ch = e % G::kChunks, r = c0 + i;
+        u32x4 y = u32x4{0u, 0u, 0u, 0u};
+        if (*reinterpret_cast<const lds_float*>(static_cast<size_t>(lse0 + 4 * i)) != INFINITY)
+          y = *reinterpret_cast<const u32x4*>(
+              static_cast<const uint8_t*>(a.q) +
+              (static_cast<int64_t>(row0 + r / g) * a.hq + kvh * g + r % g) * G::kRow + 16 * ch);
+        *reinterpret_cast<lds_u32x4*>(
+            static_cast<size_t>(lds0 + i * G::kRow + 16 * (ch ^ G::swz_k(i)))) = y;
+      }
+      __syncthreads();
+      const uint32_t dead_blocks =
+          static_cast<uint32_t>(__ballot(lane < kMostBlocks && dead[lane % kMostBlocks] != 0));
+
       for (; t < tend; t += kWaves) {
         if constexpr (kDma) {
           wait_vm<0>();
@@ -182,7 +190,7 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
 
         // Scores of row block rb, transformed; lane's key, registers' rows.
         const auto transform = [&](int rb, f32x16& sc) {
-          if (a.sc.x != 0.f) cap_scores(a.sc, sc);
+          if (a.sc.x != 0.f) cap_scores(a.sc, sc, 4 * min(4, (cn - 32 * rb + 7) / 8));
           if (bias) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -209,12 +217,16 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
         };
         // The sum of a block's weights, rows that count for nothing left out,
         // whatever the key holds.
-        const auto careful = [&](const f32x16& sc, const f32x4(&l)[4]) {
+        const auto careful = [&](int rb, const f32x16& sc, const f32x4(&l)[4]) {
           float part[2] = {0.f, 0.f};
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const float w = weight(sc, l, v);
-            part[v & 1] += l[v >> 2][v & 3] < INFINITY ? w : 0.f;
+          for (int j = 0; j < 4; ++j) {
+            if (32 * rb + 8 * j >= cn) break;  // the block's rows end before
+#pragma unroll
+            for (int v = 4 * j; v < 4 * j + 4; ++v) {
+              const float w = weight(sc, l, v);
+              part[v & 1] += l[j][v & 3] < INFINITY ? w : 0.f;
+            }
           }
           return part[0] + part[1];
         };
@@ -232,7 +244,7 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
             row_lse(rb, l);
             f32x16 sc = scores(rb);
             transform(rb, sc);
-            sum += careful(sc, l);
+            sum += careful(rb, sc, l);
           }
         } else {
           // block rb's weights beside block rb + 1's scores; the fragments three
@@ -246,7 +258,7 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
           const auto body = [&](int rb, f32x16& cur, f32x4(&l)[4], f32x16& nxt, f32x4(&ln)[4]) {
             row_lse(rb + 1 < blocks ? rb + 1 : 0, ln);
             if ((dead_blocks >> rb) & 1) {
-              sum += careful(cur, l);
+              sum += careful(rb, cur, l);
               nxt = scores(rb + 1 < blocks ? rb + 1 : 0);
 #pragma unroll
               for (int i = 0; i < kAhead; ++i) f[i] = G::k_frag(block_at(rb + 2), 0, i);
@@ -294,7 +306,11 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
       }
     }
     x += s1 - s0;
-    if (x < xend && x - pl.at >= cost(s)) pl = find_work(a, x, cost);
+    if (x < xend && x - pl.at >= cost(s)) {
+      const Work work(a, cost);
+      pl = work.find(x);
+      s = work.seq(pl.b);
+    }
   }
 }
 

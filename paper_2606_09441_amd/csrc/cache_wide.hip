@@ -106,26 +106,32 @@ __global__ __launch_bounds__(256, 2) void cache_wide_kernel(CacheAttnArgs p) {
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
   const UnitCost<Wide> cost{g, a.hkv};
-  const Split split(total_work(a, cost), p.groups);
-  const int group = group_of(split);
-  if (group >= split.groups) return;
-  int x = split.at(group);
-  const int xend = split.at(group + 1);
+  int group, x, xend;
+  Place pl;
+  Seq s;
+  {
+    const Work work(a, cost);
+    const Split split(work.total, p.groups);
+    group = group_of(split);
+    if (group >= split.groups) return;
+    x = split.at(group);
+    xend = split.at(group + 1);
+    pl = work.find(x);
+    s = work.seq(pl.b);
+  }
   const int lane = threadIdx.x & 63;
   const int wave = uniform(threadIdx.x >> 6);
   const int l32 = lane & 31, hf = lane >> 5;
 
-  Place pl = find_work(a, x, cost);
   while (x < xend && pl.b < a.num_seqs) {
     const int b = pl.b;
-    const Seq s = sequence(a, b);
     const int steps = uniform(cost.steps(s)), blocks = uniform(cost.blocks(s));
     const int unit = Split::quotient(x - pl.at, steps);
     const int s0 = x - pl.at - unit * steps;
     const int s1 = min(steps, s0 + (xend - x));
     const int kvh = unit / blocks, r0 = unit % blocks * Wide::kRows;
     const int r = r0 + 32 * wave + l32;
-    const int len = uniform(s.len), n = uniform(s.n), row0 = uniform(s.row0);
+    const int len = s.len, n = s.n, row0 = s.row0;
     const bool live = r < n * g;
     const int token = live ? r / g : 0;
     const int h = kvh * g + (live ? r % g : 0);
@@ -186,7 +192,11 @@ __global__ __launch_bounds__(256, 2) void cache_wide_kernel(CacheAttnArgs p) {
         }
     }
     x += s1 - s0;
-    if (x < xend && x - pl.at >= cost(s)) pl = find_work(a, x, cost);
+    if (x < xend && x - pl.at >= cost(s)) {
+      const Work work(a, cost);
+      pl = work.find(x);
+      s = work.seq(pl.b);
+    }
   }
 }
 

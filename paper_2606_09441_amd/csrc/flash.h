@@ -258,8 +258,9 @@ __device__ __forceinline__ float cap_any(const ScoreArgs& sc, float z) {
 }
 
 // The cap applied to a block of products, in the log2 domain.  Where none of
-// the wavefront's products is large the polynomial alone serves.
-__device__ __forceinline__ void cap_scores(const ScoreArgs& sc, f32x16& s) {
+// the wavefront's products is large the polynomial alone serves.  Only the first
+// `count` (a multiple of 4) matter.
+__device__ __forceinline__ void cap_scores(const ScoreArgs& sc, f32x16& s, int count = 16) {
   float mx = s[0], mn = s[0];
 #pragma unroll
   for (int v = 1; v < 15; v += 2) {
@@ -273,9 +274,13 @@ __device__ __forceinline__ void cap_scores(const ScoreArgs& sc, f32x16& s) {
     for (int v = 0; v < 16; ++v) s[v] = cap_any(sc, s[v]);
   } else {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const float w = s[v] * s[v];
-      s[v] *= fmaf(w, fmaf(w, fmaf(w, fmaf(w, sc.a[4], sc.a[3]), sc.a[2]), sc.a[1]), sc.a[0]);
+    for (int j = 0; j < 16; j += 4) {
+      if (j >= count) break;
+#pragma unroll
+      for (int v = j; v < j + 4; ++v) {
+        const float w = s[v] * s[v];
+        s[v] *= fmaf(w, fmaf(w, fmaf(w, fmaf(w, sc.a[4], sc.a[3]), sc.a[2]), sc.a[1]), sc.a[0]);
+      }
     }
   }
 }
