@@ -110,26 +110,20 @@ __device__ __forceinline__ void add_not_finite(const DenseArgs& a, const Row& w,
 template <typename T, int D, bool kLse>
 __device__ __forceinline__ void finish(const DenseArgs& a, const Row& w, const RowState<D>& st) {
   if (!w.live) return;
-  const float l = half_sum(st.l);
-  const float inv = l > 0.f ? 1.f / l : l == l ? 0.f : l;
+  const float inv = inverse(half_sum(st.l));
   const int64_t at = static_cast<int64_t>(w.tok) * a.hq + w.h;
   if constexpr (kLse) {
     const float le = half_sum(st.le);
-    if (w.hf == 0) a.lse[at] = le > 0.f ? fmaf(st.m, kLn2, logf(le)) : le == le ? -INFINITY : le;
+    if (w.hf == 0) a.lse[at] = log_sum(st.m, le);
   }
   T* dst = static_cast<T*>(a.out) + at * D + 4 * w.hf;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f32x4 y = f32x4{st.o[db][4 * i] * inv, st.o[db][4 * i + 1] * inv,
-                            st.o[db][4 * i + 2] * inv, st.o[db][4 * i + 3] * inv};
-      if constexpr (Tile<T, D>::kBf16)
-        *reinterpret_cast<bf16x4*>(dst + 32 * db + 8 * i) =
-            bf16x4{static_cast<__bf16>(y[0]), static_cast<__bf16>(y[1]), static_cast<__bf16>(y[2]),
-                   static_cast<__bf16>(y[3])};
-      else
-        *reinterpret_cast<f32x4*>(dst + 32 * db + 8 * i) = y;
+      const float o[4] = {st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
+                          st.o[db][4 * i + 3]};
+      store_row(dst + 32 * db + 8 * i, o, inv);
     }
 }
 
@@ -264,7 +258,106 @@ __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
   finish<T, D, kLse>(a, w, st);
 }
 
+// Few records: 32 rows a workgroup (blockIdx.y of the record's four), whose keys its
+// wavefronts share out, 32 at a time through LDS of their own, as in cache_attn.hip:
+// sixteen times the wavefronts, each with a quarter of the steps.
+template <typename T, int D>
+__global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void attn_dense_small_kernel(DenseArgs a) {
+  using G = Tile<T, D>;
+  constexpr int kOwn = 32;  // keys of a wavefront's tile
+  constexpr int kTile = kOwn * G::kRow;
+  constexpr int kDmas = 2 * G::kGroupDmas;  // of a K or V tile
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 2 * kTile];
+  __shared__ float part[4][32][3];
+  int rec, h;
+  place(a, rec, h);
+  if (rec >= a.num_recs) return;
+  const int4 r = a.recs[rec];
+  const int r0 = uniform(r.x) + 32 * static_cast<int>(blockIdx.y);
+  const int rows = min(32, uniform(r.x) + uniform(r.y) - r0);
+  if (rows <= 0) return;
+  h = uniform(h);
+  const int first = uniform(r.z);
+  // keys that all rows of the record see: up to the record's own first (causal),
+  // which is before this workgroup's
+  const bool prefix = uniform(r.w) > uniform(r.x);
+  const int upto = prefix ? uniform(r.w) : r0;
+  const int kend = max(r0 + rows, upto);
+  const int kvh = h / (a.hq / a.hkv);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int l32 = lane & 31, hf = lane >> 5;
+  const int tok = r0 + l32;
+  const bool live = l32 < rows;
+  const int stride = a.hkv * G::kRow;
+  QFrag<T, D> q;
+  q.load(static_cast<const T*>(a.q) + (static_cast<int64_t>(tok) * a.hq + h) * D, hf, live);
+  const int lds0 = static_cast<int>(reinterpret_cast<size_t>((lds_u8*)smem));
+  const int kt = lds0 + wave * 2 * kTile, vt = kt + kTile;
+  const int kaddr = kt + G::lane_k(l32, hf), vaddr = vt + G::lane_v(lane, l32, hf);
+  const int koff = G::template dma_lane<false>(lane, stride);
+  const int voff = G::template dma_lane<true>(lane, stride);
+  const float slope = a.sc.slopes != nullptr ? a.sc.slopes[h] * kLog2e : 0.f;
+  const float c = score_factor(a.sc);
+  const int tiles = (kend - first + kOwn - 1) / kOwn;
+  const auto fetch = [&](int t, auto v) {
+    constexpr bool kV = decltype(v)::value;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int k0 = first + t * kOwn + 16 * i;
+      dma_rows<T, D, kV>((kV ? vt : kt) + i * 16 * G::kRow,
+                         rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
+                                       (static_cast<int64_t>(k0) * a.hkv + kvh) * G::kRow,
+                                   min(16, kend - k0), stride, G::kRow),
+                         kV ? voff : koff, stride);
+    }
+  };
+  RowState<D> st;
+  st.clear();
+  int t = wave;
+  if (t < tiles) {
+    fetch(t, std::false_type{});
+    fetch(t, std::true_type{});
+  }
+  for (; t < tiles; t += 4) {
+    const bool more = t + 4 < tiles;
+    wait_vm<kDmas>();  // K is there, V may still be on its way
+    f32x16 s = qk_block<T, D>(kaddr, 0, q);
+    wait_lds();        // K is read
+    if (more) fetch(t + 4, std::false_type{});
+    const int j0 = first + t * kOwn;
+    const uint32_t bits =
+        live ? static_cast<uint32_t>(low_bits(max(upto, tok + 1) - j0)) : 0u;
+    score_block(a.sc, slope, static_cast<float>(tok - j0 - 4 * hf), s);
+    if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(s, bits >> (4 * hf));
+    st.rescale(half_max(block_max(s)) * c);
+    weigh_block<T, true>(s, c, st.base(), st.l, st.le);
+    if (more)
+      wait_vm<kDmas>();  // V is there, the next K may not be
+    else
+      wait_vm<0>();
+    if (j0 + kOwn > max(upto, r0 + 1) && upto < kend)
+      mend_own_tile<T, D>(vt, bits, lane, st.o);
+    pv_block<T, D>(vaddr, s, st.o);
+    wait_lds();        // V is read
+    if (more) fetch(t + 4, std::true_type{});
+  }
+  merge_waves<D>(st, kt, lds0, 2 * kTile, part, wave, l32, hf,
+                 [&](int row, int dim, const float(&o)[4], float top, float l, float le) {
+                   if (row >= rows) return;
+                   const int64_t at = static_cast<int64_t>(r0 + row) * a.hq + h;
+                   store_row(static_cast<T*>(a.out) + at * D + dim, o, inverse(l));
+                   if (dim == 0 && a.lse != nullptr) a.lse[at] = log_sum(top, le);
+                 });
+}
+
 }  // namespace
+
+// Workgroups of 128 rows up to which those of 32 rows run instead: the card is not
+// full, so what counts is how long one takes.  us of 128 / 32 rows (causal, bf16 D =
+// 128, then fp32 D = 64): 6 workgroups 11.8 / 8.1, 25.8 / 11.6; 136: 45 / 30, 156 /
+// 77; 264: 86 / 73, 315 / 205; but 224 of a short prompt 19.3 / 20.0, 544: 59 / 82,
+// 216 / 194.
+constexpr int64_t kDenseFew = 256;
 
 int64_t dense_grid(int32_t num_recs, int32_t hq, int32_t hkv) {
   const int64_t n = num_recs;
@@ -278,6 +371,7 @@ hipError_t launch_attn_dense(const DenseArgs& a, bool bf16, int head_dim, hipStr
   if (grid == 0) return hipSuccess;
   if (grid >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
   const dim3 g(static_cast<unsigned>(grid)), b(256);
+  const bool small = grid <= kDenseFew;
   using F = std::false_type;
   using Y = std::true_type;
   const auto launch = [&](auto dim) {
@@ -293,7 +387,13 @@ hipError_t launch_attn_dense(const DenseArgs& a, bool bf16, int head_dim, hipStr
       else
         with(cap, bias, F{});
     };
-    if (!bf16) {
+    if (small) {
+      const dim3 sub(g.x, kDenseRows / 32);
+      if (bf16)
+        hipLaunchKernelGGL((attn_dense_small_kernel<__bf16, D>), sub, b, 0, stream, a);
+      else
+        hipLaunchKernelGGL((attn_dense_small_kernel<float, D>), sub, b, 0, stream, a);
+    } else if (!bf16) {
       if (a.lse != nullptr)
         hipLaunchKernelGGL((attn_dense_f32_kernel<D, true>), g, b, 0, stream, a);
       else

@@ -184,26 +184,6 @@ __device__ __forceinline__ int group_of(const Split& split) {
   return blockIdx.x % kNumXcd * (split.groups / kNumXcd) + blockIdx.x / kNumXcd;
 }
 
-// The result of a row: four of its dims, and its log sum; l, le: the sums of its
-// weights as they were multiplied, and before their rounding.
-template <typename T>
-__device__ __forceinline__ void store_row(T* dst, const float (&o)[4], float inv) {
-  if constexpr (std::is_same<T, __bf16>::value)
-    *reinterpret_cast<bf16x4*>(dst) =
-        bf16x4{static_cast<__bf16>(o[0] * inv), static_cast<__bf16>(o[1] * inv),
-               static_cast<__bf16>(o[2] * inv), static_cast<__bf16>(o[3] * inv)};
-  else
-    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-}
-__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
-__device__ __forceinline__ float log_sum(float m, float le) {
-  return le > 0.f ? fmaf(m, kLn2, logf(le)) : le == le ? -INFINITY : le;
-}
-// Weight of a part with reference m in a sum with reference top (>= m).
-__device__ __forceinline__ float part_weight(float m, float top) {
-  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);  // no key: zeros, or NaN
-}
-
 // 16 rows of keys: where, and how many are valid.
 struct Rows16 {
   int64_t row;  // of the pool, or of the new tokens

@@ -32,7 +32,7 @@ constexpr int kStepTiles = Narrow::kStepTiles;  // a tile for each wavefront
 constexpr int kRows = Narrow::kRows;
 
 template <typename T, int D>
-__global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
+__global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void cache_attn_kernel(CacheAttnArgs p) {
   using G = Tile<T, D>;
   constexpr int kTile = kTileKeys * G::kRow;
   constexpr int kDmas = 2 * G::kGroupDmas;  // of a K or V tile
@@ -170,88 +170,30 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(CacheAttnArgs p) {
         wait_vm<kDmas>();  // V is there, the next K may not be
       else
         wait_vm<0>();
-      if (fresh) {
-        // rows differ in what they see of V
-        bool bad = false;
-        for (int i = lane; i < kTile / 16; i += 64)
-          bad |= not_finite<T>(
-              *reinterpret_cast<const lds_u32x4*>(static_cast<size_t>(vt + 16 * i)));
-        if (__builtin_amdgcn_ballot_w64(bad)) {
-          add_not_finite<T, D>(vt, kTileKeys, live ? bits : 0u, hf, st.o);
-          for (int i = lane; i < kTile / 16; i += 64) {
-            lds_u32x4* at = reinterpret_cast<lds_u32x4*>(static_cast<size_t>(vt + 16 * i));
-            *at = only_finite<T>(*at);
-          }
-          wait_lds();
-        }
-      }
+      if (fresh) mend_own_tile<T, D>(vt, live ? bits : 0u, lane, st.o);
       pv_block<T, D>(vaddr, sc, st.o);
       wait_lds();  // V is read
       if (more) fetch(t + kStepTiles, rows, std::true_type{});
     }
 
-    // merge the wavefronts: each leaves its rows in its own tiles' memory, as
-    // fp32 rows whose 16-byte chunks are XORed with the row
-    constexpr int kOutChunks = D / 4;
-    {
-      const float l = half_sum(st.l), le = half_sum(st.le);
-      if (hf == 0) {
-        part[wave][l32][0] = st.m;
-        part[wave][l32][1] = l;
-        part[wave][l32][2] = le;
-      }
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<lds_f32x4*>(static_cast<size_t>(
-              kt + l32 * D * 4 + 16 * ((8 * db + 2 * i + hf) ^ (l32 & (kOutChunks - 1))))) =
-              f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2],
-                    st.o[db][4 * i + 3]};
-    }
-    __syncthreads();
-    {
-      const int row = threadIdx.x >> 3;  // 8 threads a row
-      float top = -INFINITY, wt[4], l = 0.f, le = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) top = fmaxf(top, part[w][row][0]);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        wt[w] = part_weight(part[w][row][0], top);
-        l += part[w][row][1] * wt[w];
-        le += part[w][row][2] * wt[w];
-      }
-      const int rr = r0 + row;
-      if (rr < n * g) {
-        const bool whole = s0 == 0 && s1 == steps;
-        const int64_t at = static_cast<int64_t>(row0 + rr / g) * a.hq + kvh * g + rr % g;
-        const int64_t slot = (2 * static_cast<int64_t>(group) + (s0 == 0)) * kRows + row;
-        if ((threadIdx.x & 7) == 0) {
-          if (!whole)
-            p.part_ml[slot] = float4{top, l, le, 0.f};
-          else if (p.lse != nullptr)
-            p.lse[at] = log_sum(top, le);
-        }
-        const float inv = inverse(l);
-        for (int ch = threadIdx.x & 7; ch < kOutChunks; ch += 8) {
-          float o[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const f32x4 y = *reinterpret_cast<const lds_f32x4*>(
-                static_cast<size_t>(lds0 + w * 2 * kTile + row * D * 4 +
-                                    16 * (ch ^ (row & (kOutChunks - 1)))));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] += y[e] * wt[w];
-          }
-          if (whole)
-            store_row(static_cast<T*>(p.out) + at * D + 4 * ch, o, inv);
-          else
-            *reinterpret_cast<f32x4*>(p.part_o + slot * D + 4 * ch) =
-                f32x4{o[0], o[1], o[2], o[3]};
-        }
-      }
-    }
-    __syncthreads();  // the tiles' memory is free again
+    const bool whole = s0 == 0 && s1 == steps;
+    merge_waves<D>(st, kt, lds0, 2 * kTile, part, wave, l32, hf,
+                   [&](int row, int dim, const float(&o)[4], float top, float l, float le) {
+                     const int rr = r0 + row;
+                     if (rr >= n * g) return;
+                     const int64_t at =
+                         static_cast<int64_t>(row0 + rr / g) * a.hq + kvh * g + rr % g;
+                     const int64_t slot =
+                         (2 * static_cast<int64_t>(group) + (s0 == 0)) * kRows + row;
+                     if (whole) {
+                       store_row(static_cast<T*>(p.out) + at * D + dim, o, inverse(l));
+                       if (dim == 0 && p.lse != nullptr) p.lse[at] = log_sum(top, le);
+                     } else {
+                       *reinterpret_cast<f32x4*>(p.part_o + slot * D + dim) =
+                           f32x4{o[0], o[1], o[2], o[3]};
+                       if (dim == 0) p.part_ml[slot] = float4{top, l, le, 0.f};
+                     }
+                   });
     x += s1 - s0;
     if (x < xend && x - pl.at >= cost(s)) {
       const Work work(a, cost);

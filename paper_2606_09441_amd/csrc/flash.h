@@ -426,6 +426,74 @@ struct RowState {
   }
 };
 
+// The result of a row: four of its dims, and its log sum; l, le: the sums of its
+// weights as they were multiplied, and before their rounding.
+template <typename T>
+__device__ __forceinline__ void store_row(T* dst, const float (&o)[4], float inv) {
+  if constexpr (std::is_same<T, __bf16>::value)
+    *reinterpret_cast<bf16x4*>(dst) =
+        bf16x4{static_cast<__bf16>(o[0] * inv), static_cast<__bf16>(o[1] * inv),
+               static_cast<__bf16>(o[2] * inv), static_cast<__bf16>(o[3] * inv)};
+  else
+    *reinterpret_cast<f32x4*>(dst) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+}
+__device__ __forceinline__ float inverse(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
+__device__ __forceinline__ float log_sum(float m, float le) {
+  return le > 0.f ? fmaf(m, kLn2, logf(le)) : le == le ? -INFINITY : le;
+}
+// Weight of a part with reference m in a sum with reference top (>= m).
+__device__ __forceinline__ float part_weight(float m, float top) {
+  return m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);  // no key: zeros, or NaN
+}
+
+// Merge of four wavefronts that took different keys of the same 32 rows.  Each
+// leaves its rows at its own LDS address `mine` (`apart` bytes after the one before,
+// the first at lds0) as fp32 rows whose 16-byte chunks are XORed with the row; then
+// eight threads a row call f(row, first dim, sums of four dims, reference, l, le).
+// All wavefronts call this; the LDS is free again when it returns.
+template <int D, typename F>
+__device__ __forceinline__ void merge_waves(const RowState<D>& st, int mine, int lds0, int apart,
+                                            float (&part)[4][32][3], int wave, int l32, int hf,
+                                            F f) {
+  constexpr int kChunks = D / 4;
+  const float l = half_sum(st.l), le = half_sum(st.le);
+  if (hf == 0) {
+    part[wave][l32][0] = st.m;
+    part[wave][l32][1] = l;
+    part[wave][l32][2] = le;
+  }
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<lds_f32x4*>(static_cast<size_t>(
+          mine + l32 * D * 4 + 16 * ((8 * db + 2 * i + hf) ^ (l32 & (kChunks - 1))))) =
+          f32x4{st.o[db][4 * i], st.o[db][4 * i + 1], st.o[db][4 * i + 2], st.o[db][4 * i + 3]};
+  __syncthreads();
+  const int row = threadIdx.x >> 3;
+  float top = -INFINITY, wt[4], sl = 0.f, sle = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) top = fmaxf(top, part[w][row][0]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    wt[w] = part_weight(part[w][row][0], top);
+    sl += part[w][row][1] * wt[w];
+    sle += part[w][row][2] * wt[w];
+  }
+  for (int ch = threadIdx.x & 7; ch < kChunks; ch += 8) {
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const f32x4 y = *reinterpret_cast<const lds_f32x4*>(static_cast<size_t>(
+          lds0 + w * apart + row * D * 4 + 16 * (ch ^ (row & (kChunks - 1)))));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += y[e] * wt[w];
+    }
+    f(row, 4 * ch, o, top, sl, sle);
+  }
+  __syncthreads();
+}
+
 // V of a tile whose keys are visible to some rows and not to others: a weight
 // of 0 times an infinity would be a NaN in rows that do not see the key.  The
 // places that are not finite are taken out of the matrix product (`clean`)
@@ -446,6 +514,23 @@ __device__ __forceinline__ void add_not_finite(int tile, int keys, uint64_t bits
           if (b == db && bad && sees) o[b][v] += x;
       }
   }
+}
+
+// The same for a wavefront's own tile of 32 keys at LDS address `tile`.
+template <typename T, int D>
+__device__ __forceinline__ void mend_own_tile(int tile, uint32_t bits, int lane,
+                                              f32x16 (&o)[D / 32]) {
+  constexpr int kTile = 32 * Tile<T, D>::kRow;
+  bool bad = false;
+  for (int i = lane; i < kTile / 16; i += 64)
+    bad |= not_finite<T>(*reinterpret_cast<const lds_u32x4*>(static_cast<size_t>(tile + 16 * i)));
+  if (!__builtin_amdgcn_ballot_w64(bad)) return;
+  add_not_finite<T, D>(tile, 32, bits, lane >> 5, o);
+  for (int i = lane; i < kTile / 16; i += 64) {
+    lds_u32x4* at = reinterpret_cast<lds_u32x4*>(static_cast<size_t>(tile + 16 * i));
+    *at = only_finite<T>(*at);
+  }
+  wait_lds();
 }
 
 }  // namespace flash
