@@ -56,8 +56,9 @@ typedef enum sift_mask {
  * The plan's lists are neither read nor changed.  bf16: the weights are
  * rounded to bf16 for their product with V, as in the sparse attention, the
  * sums are fp32.
+ * out and lse overlap no input.
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (mask, cap, dtypes,
- *   alignment), SIFT_E_PLAN (another device is current), SIFT_E_CAPACITY (2^24
+ *   alignment, more than 2^17 kv heads), SIFT_E_PLAN (another device is current), SIFT_E_CAPACITY (2^24
  *   workgroups of 128 rows of a head or more), SIFT_E_HIP.
  */
 sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_tensor* k,
@@ -107,7 +108,8 @@ typedef struct sift_cache sift_cache;
  *   max_pages  pages of a sequence at most, >= 1
  *   max_rows   new tokens of a sequence in one call at most, >= 1
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (D, page),
- *   SIFT_E_CAPACITY (slots or rows x heads beyond 2^31 - 256), SIFT_E_HIP.
+ *   SIFT_E_CAPACITY (slots or rows x heads beyond 2^31 - 256, more than 2^17 kv
+ *   heads), SIFT_E_HIP.
  */
 sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads,
                               int32_t head_dim, int32_t page, int32_t max_pages,

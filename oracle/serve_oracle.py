@@ -57,7 +57,7 @@ def dense_visible(seg_offsets, prompt_seg_ptr, mask):
 
 
 def dense(q, k, v, seg_offsets, prompt_seg_ptr, mask, scale=None, cap=0.0, slopes=None):
-    """(out [n, Hq, D], lse [n, Hq]) of the dense attention."""
+    """(out [n, Hq, D], lse [n, Hq]) of the dense attention, row by row."""
     n, hq, d = q.shape
     g = hq // k.shape[1]
     scale = d ** -0.5 if scale is None else scale
@@ -68,6 +68,29 @@ def dense(q, k, v, seg_offsets, prompt_seg_ptr, mask, scale=None, cap=0.0, slope
         for h in range(hq):
             out[i, h], lse[i, h] = attend(q[i, h], k[j, h // g], v[j, h // g], scale, cap,
                                           0.0 if slopes is None else slopes[h], i - j)
+    return out, lse
+
+
+def dense_by_head(q, k, v, seg_offsets, prompt_seg_ptr, mask, scale=None, cap=0.0, slopes=None):
+    """The same, a head's whole score matrix at a time (finite inputs)."""
+    q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
+    n, hq, d = q.shape
+    g = hq // k.shape[1]
+    scale = d ** -0.5 if scale is None else scale
+    sees = dense_visible(seg_offsets, prompt_seg_ptr, mask)
+    far = np.abs(np.arange(n)[:, None] - np.arange(n)[None])
+    out, lse = np.zeros((n, hq, d)), np.zeros((n, hq))
+    for h in range(hq):
+        s = q[:, h] @ k[:, h // g].T * scale
+        if cap:
+            s = cap * np.tanh(s / cap)
+        if slopes is not None:
+            s = s - float(slopes[h]) * far
+        s = np.where(sees, s, -np.inf)
+        m = s.max(1, keepdims=True)
+        w = np.exp(s - m)
+        out[:, h] = w @ v[:, h // g] / w.sum(1, keepdims=True)
+        lse[:, h] = m[:, 0] + np.log(w.sum(1))
     return out, lse
 
 

@@ -417,7 +417,6 @@ class Plan:
         "document" or "prefix"; scores capped by cap * tanh(s / cap) (cap > 0) and
         biased by -slopes[h] * distance (float32 [Hq]).  lse: float32 [tokens, Hq]
         buffer that receives the rows' log sum exp."""
-        torch = _torch()
         fn = "sift_plan_dense"
         if mask not in MASKS:
             raise SiftError(fn, 4, f"mask must be one of {sorted(MASKS)}")
@@ -426,12 +425,29 @@ class Plan:
             require(fn, lse, "lse", "float32", self.info["num_tokens"] * self.info["num_q_heads"],
                     self.device)
         if out is None:
-            out = torch.empty_like(q)
+            out = _empty(q.shape, q.dtype, q.device, stream)
+        _on(fn, self.device, q=q, k=k, v=v, out=out)
         qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
         check(fn, lib().sift_plan_dense(
             self._h, ctypes.byref(qd), ctypes.byref(kd), ctypes.byref(vd), MASKS[mask],
             ctypes.byref(score), ctypes.byref(od), _ptr(lse), _stream_ptr(stream)))
         return out
+
+
+def _empty(shape, dtype, device, stream):
+    """A buffer for a call to write, of the pool of the stream that it runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _on(fn, device, **tensors) -> None:
+    """All of these tensors on `device`."""
+    for name, t in tensors.items():
+        if getattr(t, "device", None) != device:
+            raise SiftError(fn, 7, f"{name} is not on {device}")
 
 
 def score_struct(fn, scale, cap, slopes, num_q_heads, device) -> SiftScore:
@@ -753,7 +769,6 @@ class Cache:
         many of each); tree_mask int64 [rows, words] holds each row's visible new
         tokens as bits (None: those up to itself); row_pos int32 [rows].  lse: float32
         [rows, Hq] buffer that receives the rows' log sum exp."""
-        torch = _torch()
         fn = "sift_cache_attention"
         rows = self._rows(fn, q, row_ptr, row_pos)
         words = 0
@@ -766,7 +781,8 @@ class Cache:
         if lse is not None:
             require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
         if out is None:
-            out = torch.empty_like(q)
+            out = _empty(q.shape, q.dtype, q.device, stream)
+        _on(fn, self.device, q=q, k_new=k_new, v_new=v_new, out=out)
         qd, kd, vd, od = tensor_desc(q), tensor_desc(k_new), tensor_desc(v_new), tensor_desc(out)
         check(fn, lib().sift_cache_attention(
             self._h, self._kv(fn, kv), ctypes.byref(rows), ctypes.byref(qd), ctypes.byref(kd),
@@ -793,8 +809,12 @@ class Cache:
         if weights is not None:
             self._slot_buffer(fn, weights, "weights")
         if out is None:
-            out = weights if weights is not None else torch.zeros(
-                self.num_seqs, self.hkv, self.slots, dtype=torch.float32, device=self.device)
+            out = weights
+        if out is None:
+            out = _empty((self.num_seqs, self.hkv, self.slots), torch.float32, self.device, stream)
+            with torch.cuda.stream(stream):  # (None: the current one)
+                out.zero_()
+        _on(fn, self.device, q=q)
         self._slot_buffer(fn, out, "out")
         score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
         qd = tensor_desc(q)
@@ -817,11 +837,11 @@ class Cache:
             require(fn, next_pos, "next_pos", "int32", self.num_seqs, self.device)
         shape = (self.num_seqs, self.hkv, self.slots)
         if weights_out is None:
-            weights_out = torch.empty(shape, dtype=torch.float32, device=self.device)
+            weights_out = _empty(shape, torch.float32, self.device, stream)
         if pos_out is None:
-            pos_out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            pos_out = _empty(shape, torch.int32, self.device, stream)
         if lens_out is None:
-            lens_out = torch.empty(self.num_seqs, dtype=torch.int32, device=self.device)
+            lens_out = _empty((self.num_seqs,), torch.int32, self.device, stream)
         self._slot_buffer(fn, weights_out, "weights_out")
         self._slot_buffer(fn, pos_out, "pos_out", "int32")
         require(fn, lens_out, "lens_out", "int32", self.num_seqs, self.device)

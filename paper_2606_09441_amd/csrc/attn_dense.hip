@@ -170,15 +170,26 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dense_f32_kernel(De
     f32x16 s0 = qk_block<T, D>(kaddr + slot, 0, q);
     f32x16 s1 = qk_block<T, D>(kaddr + slot, 1, q);
     const float dist = static_cast<float>(w.tok - j0 - 4 * w.hf);
-    score_block(a.sc, slope, dist, s0);
-    score_block(a.sc, slope, dist - 32.f, s1);
+    if (a.sc.x != 0.f) {
+      cap_scores(a.sc, s0);
+      cap_scores(a.sc, s1);
+    }
     if (j0 + kKeys > w.mine) {
       mask_block(s0, static_cast<uint32_t>(bits >> (4 * w.hf)));
       mask_block(s1, static_cast<uint32_t>(bits >> (32 + 4 * w.hf)));
     }
-    st.rescale(half_max(fmaxf(block_max(s0), block_max(s1))) * c);
-    weigh_block<T, kLse>(s0, c, st.base(), st.l, st.le);
-    weigh_block<T, kLse>(s1, c, st.base(), st.l, st.le);
+    float off = 0.f;
+    if (a.sc.slopes != nullptr) {
+      const auto far0 = [&](int v) { return fabsf(dist - static_cast<float>(key_of(v))); };
+      const auto far1 = [&](int v) { return fabsf(dist - static_cast<float>(32 + key_of(v))); };
+      off = half_max(fmaxf(largest_bias(s0, slope, far0), largest_bias(s1, slope, far1)));
+      if (off == -INFINITY) off = 0.f;
+      add_bias(a.sc, s0, slope, off, far0);
+      add_bias(a.sc, s1, slope, off, far1);
+    }
+    st.rescale(fmaf(half_max(fmaxf(block_max(s0), block_max(s1))), c, off));
+    weigh_block<T, kLse>(s0, c, st.base() - off, st.l, st.le);
+    weigh_block<T, kLse>(s1, c, st.base() - off, st.l, st.le);
     pv_block<T, D>(vaddr + slot, s0, st.o);
     pv_block<T, D>(vaddr + slot + 32 * G::kRow, s1, st.o);
   }
@@ -189,7 +200,7 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_dense_f32_kernel(De
 // The record's tiles as the pipeline takes them (flash_pipe.h).  kBias: outside the
 // diagonal the distance is linear in the key, so that the bias is one more FMA with
 // a constant, folded into the exponent; the tile's bound then is its largest
-// product at the smallest distance, which only has to be near and not below.
+// product with its largest bias, which only has to be near and not below.
 template <int D, bool kCap, bool kBias>
 struct DenseTiles {
   using T = __bf16;
@@ -231,8 +242,9 @@ struct DenseTiles {
       if (!masked && !around) {
         const float dist = static_cast<float>(w.tok - j0);
         f.slope_key = j0 < lo ? slope : -slope;
-        f.at = -f.slope_key * d;
-        mx -= slope * (j0 < lo ? dist - static_cast<float>(kKeys - 1) : -dist);
+        f.d = d;
+        // the distances run from |dist| to |dist - 63|; slopes may be negative
+        mx += fmaxf(-slope * fabsf(dist), -slope * fabsf(dist - static_cast<float>(kKeys - 1)));
       }
     }
     return mx;
@@ -327,10 +339,18 @@ __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void attn_dense_s
     const int j0 = first + t * kOwn;
     const uint32_t bits =
         live ? static_cast<uint32_t>(low_bits(max(upto, tok + 1) - j0)) : 0u;
-    score_block(a.sc, slope, static_cast<float>(tok - j0 - 4 * hf), s);
+    if (a.sc.x != 0.f) cap_scores(a.sc, s);
     if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(s, bits >> (4 * hf));
-    st.rescale(half_max(block_max(s)) * c);
-    weigh_block<T, true>(s, c, st.base(), st.l, st.le);
+    float off = 0.f;
+    if (a.sc.slopes != nullptr) {
+      const float dist = static_cast<float>(tok - j0 - 4 * hf);
+      const auto far = [&](int v) { return fabsf(dist - static_cast<float>(key_of(v))); };
+      off = half_max(largest_bias(s, slope, far));
+      if (off == -INFINITY) off = 0.f;
+      add_bias(a.sc, s, slope, off, far);
+    }
+    st.rescale(fmaf(half_max(block_max(s)), c, off));
+    weigh_block<T, true>(s, c, st.base() - off, st.l, st.le);
     if (more)
       wait_vm<kDmas>();  // V is there, the next K may not be
     else

@@ -201,15 +201,5 @@ __device__ __forceinline__ Rows16 cached_rows(const CacheArgs& a, int b, int len
   return Rows16{(static_cast<int64_t>(page) << a.page_shift) + in, min(max(n, 0), 16)};
 }
 
-// Scores of a block whose keys' positions are not consecutive.
-__device__ __forceinline__ void score_block_at(const ScoreArgs& sc, float slope,
-                                               const int (&dist)[16], f32x16& s) {
-  if (sc.x != 0.f) cap_scores(sc, s);
-  const float c = sc.x != 0.f ? 1.f : sc.c;
-#pragma unroll
-  for (int v = 0; v < 16; ++v)
-    s[v] = fmaf(s[v], c, -slope * fabsf(static_cast<float>(dist[v])));
-}
-
 }  // namespace cache
 }  // namespace sift

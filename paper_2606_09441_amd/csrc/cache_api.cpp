@@ -130,7 +130,7 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
   if (page != 16 && page != 32 && page != 64 && page != 128) return SIFT_E_UNSUPPORTED;
   const int64_t g = num_q_heads / num_kv_heads;
   if (static_cast<int64_t>(max_pages) * page > kMost || max_rows * g > kMost ||
-      num_seqs > kMost || num_kv_heads > kMost / 1024)
+      num_seqs > kMost || num_kv_heads > sift::kMostKvHeads)
     return SIFT_E_CAPACITY;
   sift_cache* c = new (std::nothrow) sift_cache();
   if (c == nullptr) return SIFT_E_HIP;

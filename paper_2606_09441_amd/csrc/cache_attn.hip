@@ -146,8 +146,16 @@ __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void cache_attn_k
         else
           bits &= static_cast<uint32_t>(low_bits(node + 1 - j0));
       }
+      if (a.sc.x != 0.f) cap_scores(a.sc, sc);
+      if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(sc, bits >> (4 * hf));
+      float off = 0.f;
+      const auto bias = [&](auto far) {
+        off = half_max(largest_bias(sc, slope, far));
+        if (off == -INFINITY) off = 0.f;
+        add_bias(a.sc, sc, slope, off, far);
+      };
       if (a.sc.slopes != nullptr && (fresh ? a.row_pos : a.key_pos) != nullptr) {
-        int dist[16];
+        float dist[16];
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           const int j = j0 + 4 * hf + key_of(v);
@@ -156,16 +164,15 @@ __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void cache_attn_k
                     : a.key_pos[((static_cast<int64_t>(b) * a.hkv + kvh) * a.max_pages
                                  << a.page_shift) +
                                 min(j, (a.max_pages << a.page_shift) - 1)];
-          dist[v] = my_pos - pos;
+          dist[v] = fabsf(static_cast<float>(my_pos - pos));
         }
-        score_block_at(a.sc, slope, dist, sc);
-      } else {
-        score_block(a.sc, slope,
-                    static_cast<float>(my_pos - (fresh ? len : 0) - j0 - 4 * hf), sc);
+        bias([&](int v) { return dist[v]; });
+      } else if (a.sc.slopes != nullptr) {
+        const float d0 = static_cast<float>(my_pos - (fresh ? len : 0) - j0 - 4 * hf);
+        bias([&](int v) { return fabsf(d0 - static_cast<float>(key_of(v))); });
       }
-      if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(sc, bits >> (4 * hf));
-      st.rescale(half_max(block_max(sc)) * c);
-      weigh_block<T, true>(sc, c, st.base(), st.l, st.le);
+      st.rescale(fmaf(half_max(block_max(sc)), c, off));
+      weigh_block<T, true>(sc, c, st.base() - off, st.l, st.le);
       if (more)
         wait_vm<kDmas>();  // V is there, the next K may not be
       else

@@ -34,7 +34,6 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -55,13 +54,6 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLazy = 8.0f;
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ __forceinline__ float xor32(float x) {
-  float a = x, b = x;
-  asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 1" : "+v"(a), "+v"(b));
-  // lower lanes: a is the own value, b the other half's; upper lanes: reverse
-  return (threadIdx.x & 32) ? a : b;
-}
 
 __device__ __forceinline__ float half_max(float x) {
   float a = x, b = x;
@@ -288,21 +280,29 @@ __device__ __forceinline__ void cap_scores(const ScoreArgs& sc, f32x16& s, int c
 // Key of register v of a 32-key block, less 4 hf.
 __device__ __forceinline__ constexpr int key_of(int v) { return 8 * (v >> 2) + (v & 3); }
 
-// Scores of a 32-key block in the log2 domain, but for the factor that is
-// returned: products with neither cap nor bias stay as they are.  dist0: the
-// query's position less that of the block's key 4 hf, for consecutive keys.
+// The scores of a block are its products, capped where there is a cap, times a
+// factor, in the log2 domain, and the bias.
 __device__ __forceinline__ float score_factor(const ScoreArgs& sc) {
   return sc.x != 0.f || sc.slopes != nullptr ? 1.f : sc.c;
 }
-__device__ __forceinline__ void score_block(const ScoreArgs& sc, float slope, float dist0,
-                                            f32x16& s) {
-  if (sc.x != 0.f) cap_scores(sc, s);
-  if (sc.slopes != nullptr) {
-    const float c = sc.x != 0.f ? 1.f : sc.c;
+// A bias may be far larger than what a row's scores differ by.  So it is taken
+// less the tile's largest bias of a seen key, and the reference too: what is
+// rounded then is as small as the difference.  far(v): the distance of register
+// v's key.
+template <typename Far>
+__device__ __forceinline__ float largest_bias(const f32x16& s, float slope, Far far) {
+  float a = -INFINITY;
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
-      s[v] = fmaf(s[v], c, -slope * fabsf(dist0 - static_cast<float>(key_of(v))));
-  }
+  for (int v = 0; v < 16; ++v)
+    if (s[v] > -INFINITY) a = fmaxf(a, -slope * far(v));
+  return a;
+}
+template <typename Far>
+__device__ __forceinline__ void add_bias(const ScoreArgs& sc, f32x16& s, float slope, float off,
+                                         Far far) {
+  const float c = sc.x != 0.f ? 1.f : sc.c;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) s[v] = fmaf(s[v], c, fmaf(-slope, far(v), -off));
 }
 
 // Scores of the keys whose bit is not set become -inf.  bits: one a key of the

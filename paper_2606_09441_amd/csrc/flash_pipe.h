@@ -19,12 +19,12 @@ namespace flash {
 
 constexpr int kKeys = 64;  // of a tile
 
-// A tile's exponents are z p(z^2) + slope_key key + at, less the reference, with
+// A tile's exponents are z p(z^2) + slope_key (key - d), less the reference, with
 // the tanh's p, or (1, 0, ..) where the scores are capped already; without kCap
 // p0 alone, the scale.  The key's terms only with kLinear.
 struct Form {
   float p0, p1, p2, p3;
-  float slope_key, at;
+  float slope_key, d;
 };
 
 template <bool kCap>
@@ -126,7 +126,7 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
       const float z = i < 2 ? s0[v + u] : s1[v + u];
       float b = -base, pz = f.p0;
       if constexpr (kLinear)
-        b = fmaf(f.slope_key, static_cast<float>(key_of(v + u) + (i < 2 ? 0 : 32)), f.at - base);
+        b = fmaf(f.slope_key, static_cast<float>(key_of(v + u) + (i < 2 ? 0 : 32)), fmaf(-f.slope_key, f.d, -base));
       if constexpr (kCap) {
         const float y = z * z;
         pz = fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);

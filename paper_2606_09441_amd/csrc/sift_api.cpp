@@ -938,10 +938,14 @@ sift_status sift_plan_create(const sift_layout* layout, int32_t num_q_heads,
                              sift_plan** plan_out) {
   if (plan_out == nullptr) return SIFT_E_NULL;
   *plan_out = nullptr;
-  PlanImage im;
-  const sift_status st = make_image(layout, num_q_heads, num_kv_heads, head_dim, tile, im, true);
-  if (st != SIFT_OK) return st;
-  return create_plan(im, nullptr, 0, nullptr, Upload::kBlocking, plan_out);
+  try {
+    PlanImage im;
+    const sift_status st = make_image(layout, num_q_heads, num_kv_heads, head_dim, tile, im, true);
+    if (st != SIFT_OK) return st;
+    return create_plan(im, nullptr, 0, nullptr, Upload::kBlocking, plan_out);
+  } catch (const std::bad_alloc&) {
+    return SIFT_E_HIP;  // as other failed allocations
+  }
 }
 
 sift_status sift_workspace_bytes(const sift_layout* layout, int32_t num_q_heads,
@@ -1220,6 +1224,7 @@ sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_te
   for (const void* p : {q->data, k->data, v->data, out->data})
     if (reinterpret_cast<uintptr_t>(p) % 16 != 0) return SIFT_E_UNSUPPORTED;
   if (mask < SIFT_MASK_CAUSAL || mask > SIFT_MASK_PREFIX) return SIFT_E_UNSUPPORTED;
+  if (in.num_kv_heads > sift::kMostKvHeads) return SIFT_E_UNSUPPORTED;
   sift::DenseArgs a{};
   if ((st = sift::make_score(score, in.head_dim, sift::kUnitLog2e, &a.sc)) != SIFT_OK) return st;
   if ((st = check_device(plan)) != SIFT_OK) return st;

@@ -409,6 +409,9 @@ constexpr double kTanhPolyBf16[4] = {0.9999999019, -0.3333136246, 0.1327097676, 
 // Caps beyond this would not show in fp32, and their squares would overflow.
 constexpr float kMaxCap = 1e15f;
 
+// 16 rows of so many kv heads, 512 bytes each, span less than 2^31 bytes.
+constexpr int32_t kMostKvHeads = 1 << 17;
+
 // Dense attention (attn_dense.hip).  A record: 128 query rows of a segment,
 // {first row, rows, first key, upto}: row i sees the keys j from the first on
 // with j < upto or j <= i.

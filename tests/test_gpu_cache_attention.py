@@ -69,9 +69,10 @@ def test_many_new_tokens(dtype):
     check(Batch([40, 0], [150, 90], 4, 4, 64, dtype, seed=5))
 
 
-@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 1), (12, 3), (64, 1), (40, 1)])
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 1), (12, 3), (64, 1), (40, 1), (20, 1)])
 def test_head_layouts(hq, hkv):
     check(Batch([200, 0, 77], [3, 1, 2], hq, hkv, 64, "bf16", seed=6))
+    check(Batch([200, 0, 77], [3, 1, 2], hq, hkv, 128, "f32", seed=6), bias=True)
 
 
 def test_many_sequences():
@@ -80,6 +81,8 @@ def test_many_sequences():
     lens = rng.integers(0, 90, 150).tolist()
     new = [int(rng.integers(0, 3)) for _ in lens]
     check(Batch(lens, new, 4, 2, 64, "bf16", 16, seed=7))
+    new = [int(rng.integers(0, 12)) for _ in lens]
+    check(Batch(lens, new, 16, 2, 64, "bf16", 16, tree=random_tree, seed=7))   # wide units
 
 
 def test_long_cache():
@@ -111,9 +114,10 @@ def test_rows_left_out():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-def test_unseen_new_tokens_do_not_matter(dtype, value):
+@pytest.mark.parametrize("hq", [2, 4])
+def test_unseen_new_tokens_do_not_matter(dtype, value, hq):
     """A drafted token with such values reaches the rows that see it and no other."""
-    x = Batch([70, 0], [9, 40], 4, 2, 128, dtype, tree=random_tree, seed=12)
+    x = Batch([70, 0], [9, 40], hq, 2, 128, dtype, tree=random_tree, seed=12)
     for bad, b in ((3, 0), (9 + 20, 1)):
         x.v_new[bad, 1, 5:9] = value
     import torch
@@ -129,7 +133,7 @@ def test_unseen_new_tokens_do_not_matter(dtype, value):
     with np.errstate(all="ignore"):
         ref, _ = x.oracle()
     assert max_abs(worse[~sees], ref[~sees]) <= TOL[dtype]
-    ref_k = Batch([70, 0], [9, 40], 4, 2, 128, dtype, tree=random_tree, seed=12)
+    ref_k = Batch([70, 0], [9, 40], hq, 2, 128, dtype, tree=random_tree, seed=12)
     ref_k.v_new.copy_(x.v_new)
     with np.errstate(all="ignore"):
         ref, _ = ref_k.oracle()
@@ -165,6 +169,36 @@ def test_streams_and_repeats():
             got = out.clone()
             assert torch.equal(got, cache.attention(*args, **kw))
         assert torch.equal(got, first)
+
+
+def test_offsets_beyond_32_bits():
+    """Pages at the far end of pools of more than 2^31 elements, through all three
+    calls: the same bits as from a small pool."""
+    import torch
+    from paper_2606_09441_amd import CachePages
+    x = Batch([300, 41], [3, 3], 16, 8, 128, "bf16", 64, seed=15)
+    page, rows = x.page, (1 << 31) // (8 * 128) + 64 * 32
+    rows -= rows % page
+    far = rows // page - 1 - torch.arange(x.B * x.max_pages, device=x.q.device).view(x.B, -1)
+    k = torch.empty(rows, 8, 128, dtype=torch.bfloat16, device=x.q.device)
+    v = torch.empty_like(k)
+    near = x.t["table"].long().clamp(0, x.k.shape[0] // page - 1)
+    at = lambda t: (t.long()[..., None] * page + torch.arange(page, device=t.device)).flatten()  # noqa: E731
+    k[at(far)], v[at(far)] = x.k[at(near)], x.v[at(near)]
+    small = x.pages()
+    big = CachePages(k, v, far.int().contiguous(), x.t["lens"])
+    with x.cache() as cache:
+        res = []
+        for kv in (small, big):
+            lse = torch.empty(6, 16, device=x.q.device)
+            out = cache.attention(x.q, x.k_new, x.v_new, kv, row_ptr=x.t["row_ptr"], lse=lse)
+            w = cache.accumulate(x.q, lse, kv, row_ptr=x.t["row_ptr"])
+            ev = cache.evict(kv, w, 100, 4, 8)
+            after = CachePages(kv.k_pages, kv.v_pages, kv.page_table, ev[2], key_pos=ev[1])
+            res.append((out, lse, w, *ev, cache.attention(x.q, x.k_new, x.v_new, after,
+                                                          row_ptr=x.t["row_ptr"])))
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*res))
 
 
 def test_refusals():

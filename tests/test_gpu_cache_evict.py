@@ -75,6 +75,14 @@ def test_protected(sinks, recent):
           own_next=True)
 
 
+@pytest.mark.parametrize("kind", ["any", "equal", "ties", "odd"])
+@pytest.mark.parametrize("budget", [1, 700, 8192, 15000, 40000])
+def test_long_caches(kind, budget):
+    """Caches that several workgroups select from."""
+    check(Batch([20000, 9000, 1, 0, 2048, 16385], [0] * 6, 2, 2, 64, "bf16", 16, budget % 2 == 0,
+                budget > 8000, seed=7), kind, budget, min(4, budget), min(64, budget // 2))
+
+
 def test_long():
     check(Batch([20000, 300], [0, 0], 2, 2, 64, "bf16", 128, gaps=True, seed=3), "any", 3000, 4, 64)
     check(Batch([20000], [0], 1, 1, 64, "bf16", 128, seed=3), "ties", 9999, 4, 64)

@@ -75,6 +75,23 @@ def test_against_the_oracle(dtype, d, page):
 
 
 @pytest.mark.parametrize("dtype,d", TYPES)
+def test_few_rows(dtype, d):
+    """Rows of a block or two, whose keys come through LDS."""
+    new = [2, 0, 1, 6, 3, 2, 9, 4, 0, 1, 5, 8]
+    for gaps, moved, cap, bias, weighted in [(False, False, 0.0, False, True),
+                                             (True, True, 20.0, True, True),
+                                             (True, False, 30.0, False, False)]:
+        check(Batch(LENS, new, 12, 2, d, dtype, 32, gaps, moved, seed=3), cap, bias,
+              weighted=weighted, name=f"gaps {gaps} moved {moved} cap {cap} bias {bias}")
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(11)
+    lens = rng.integers(0, 90, 150).tolist()
+    check(Batch(lens, [int(rng.integers(0, 3)) for _ in lens], 4, 2, 64, "bf16", 16, seed=11))
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
 def test_single_tokens(dtype, d):
     check(Batch(LENS, [1] * len(LENS), 8, 2, d, dtype, 64))
     check(Batch(LENS, [1] * len(LENS), 8, 1, d, dtype, 64), fresh=True)

@@ -48,24 +48,23 @@ def inputs(n, hq, hkv, d, dtype, seed=0):
     return dev, [x.float().cpu().numpy() for x in dev]
 
 
-def run(prompts, hq, hkv, d, dtype, mask, cap=0.0, bias=False, scale=None, seed=0, poison=None,
-        tile=64):
+def run(prompts, hq, hkv, d, dtype, mask, cap=0.0, bias=False, scale=None, seed=0, tile=64,
+        by_head=False, want_lse=True, slope=None):
     """(out, lse) of the library and of the oracle."""
     import torch
     from paper_2606_09441_amd import Plan
     so, ps = layout(prompts)
     n = so[-1]
     (q, k, v), (qn, kn, vn) = inputs(n, hq, hkv, d, dtype, seed)
-    if poison is not None:
-        poison(k, v)
-        kn, vn = k.float().cpu().numpy(), v.float().cpu().numpy()
     slopes = (2.0 ** (-4.0 * np.arange(1, hq + 1) / hq)).astype(np.float32) if bias else None
+    if slope is not None:
+        slopes = (slope * np.arange(1, hq + 1) / hq).astype(np.float32)
     lse = torch.full((n, hq), 7.0, device=q.device)
     with Plan(so, ps, hq, hkv, d, tile) as plan:
-        out = plan.dense(q, k, v, mask=mask, scale=scale, cap=cap, lse=lse,
+        out = plan.dense(q, k, v, mask=mask, scale=scale, cap=cap, lse=lse if want_lse else None,
                          slopes=None if slopes is None else torch.from_numpy(slopes).to(q.device))
         torch.cuda.synchronize()
-    want = S.dense(qn, kn, vn, so, ps, mask, scale, cap, slopes)
+    want = (S.dense_by_head if by_head else S.dense)(qn, kn, vn, so, ps, mask, scale, cap, slopes)
     return out.float().cpu().numpy(), lse.cpu().numpy(), *want
 
 
@@ -79,6 +78,34 @@ def test_masks_and_scores(dtype, d, mask, cap, bias):
         e, el = max_abs(out, ref), max_abs(lse, ref_lse)
         say(f"{name} {dtype} {d} {mask} cap {cap} bias {bias}: {e:.2e}, lse {el:.2e}")
         assert e <= TOL[dtype] and el <= LSE_TOL
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("mask", ["causal", "document", "prefix"])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (2.0, False), (50.0, False), (0.0, True),
+                                      (20.0, True)])
+def test_many_heads(dtype, d, mask, cap, bias):
+    """Enough records and heads for the 128-row workgroups; with and without lse."""
+    prompts = [[64, 63, 65, 1, 33], [1, 128, 1], [300, 129, 77], [200, 0]]
+    out, lse, ref, ref_lse = run(prompts, 24, 8, d, dtype, mask, cap, bias, by_head=True)
+    bare = run(prompts, 24, 8, d, dtype, mask, cap, bias, by_head=True, want_lse=False)[0]
+    e, el = max_abs(out, ref), max_abs(lse, ref_lse)
+    say(f"{dtype} {d} {mask} cap {cap} bias {bias}: {e:.2e}, lse {el:.2e}")
+    assert e <= TOL[dtype] and el <= LSE_TOL
+    assert max_abs(bare, ref) <= TOL[dtype]
+
+
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (40, 8)])
+@pytest.mark.parametrize("slope", [-0.7, -3.0, 5.0, 300.0])
+def test_steep_and_negative_slopes(hq, hkv, slope):
+    """Far keys favoured, and weights that vanish within a tile."""
+    for dtype in ("bf16", "f32"):
+        for mask in ("causal", "prefix"):
+            out, lse, ref, ref_lse = run([[150, 300, 77], [130, 5]], hq, hkv, 64, dtype, mask,
+                                         bias=True, by_head=True, slope=slope)
+            assert max_abs(out, ref) <= TOL[dtype]
+            # |slope| * distance in fp32: relative 2^-23
+            assert np.max(np.abs(lse - ref_lse) / np.maximum(1.0, np.abs(ref_lse) / 30)) <= LSE_TOL
 
 
 @pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 5), (6, 3), (16, 16), (12, 4)])
@@ -96,19 +123,20 @@ def test_scale():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
-def test_unseen_keys_do_not_matter(dtype, value):
+@pytest.mark.parametrize("hq,hkv", [(2, 1), (72, 1)])
+def test_unseen_keys_do_not_matter(dtype, value, hq, hkv):
     """A key with such values only reaches the rows that see it: under the causal
     mask the rows from it on, and no other prompt's."""
     import torch
     from paper_2606_09441_amd import Plan
     so, ps = layout([[90, 60], [40, 10]])
     n, bad = so[-1], 70
-    (q, k, v), (qn, kn, vn) = inputs(n, 2, 1, 128, dtype)
+    (q, k, v), (qn, kn, vn) = inputs(n, hq, hkv, 128, dtype)
     k[bad], v[bad] = value, value
     v[bad, :, 3:] = 0.5         # the other dims of a visible key stay as they are ...
     k[bad] = 0.25               # ... where its scores are finite
     kn, vn = k.float().cpu().numpy(), v.float().cpu().numpy()
-    with Plan(so, ps, 2, 1, 128, 64) as plan:
+    with Plan(so, ps, hq, hkv, 128, 64) as plan:
         out = plan.dense(q, k, v).float().cpu().numpy()
         k[bad] = value          # and a score that is none
         worse = plan.dense(q, k, v).float().cpu().numpy()
@@ -189,3 +217,29 @@ def test_refusals():
         refused(5, q, k, v, lse=torch.zeros(130, 3, device=q.device))
         odd = torch.empty(q.numel() + 1, dtype=q.dtype, device=q.device)[1:].view_as(q)
         refused(4, odd, k, v)
+
+
+def test_offsets_beyond_32_bits():
+    """Queries and outputs of more than 2^31 elements: the last prompt's rows equal
+    those of the same prompt alone."""
+    import torch
+    from paper_2606_09441_amd import Plan
+    one = [128] * 54 + [16]
+    so, ps = layout([one] * 51)
+    n, hq, hkv, d = so[-1], 48, 8, 128
+    assert n * hq * d > 1 << 31
+    gen = torch.Generator(device=device()).manual_seed(1)
+    q = torch.empty(n, hq, d, dtype=torch.bfloat16, device=device())
+    for i in range(0, n, 1 << 16):
+        q[i:i + (1 << 16)].normal_(generator=gen)
+    k = torch.randn(n, hkv, d, generator=gen, device=device()).to(torch.bfloat16)
+    v = torch.randn(n, hkv, d, generator=gen, device=device()).to(torch.bfloat16)
+    with Plan(so, ps, hq, hkv, d, 128) as plan:
+        out = plan.dense(q, k, v, mask="document", cap=50.0)
+    a = so[ps[-2]]
+    so1, ps1 = layout([one])
+    with Plan(so1, ps1, hq, hkv, d, 128) as plan:
+        alone = plan.dense(q[a:].contiguous(), k[a:].contiguous(), v[a:].contiguous(),
+                           mask="document", cap=50.0)
+    torch.cuda.synchronize()
+    assert torch.equal(out[a:], alone)
