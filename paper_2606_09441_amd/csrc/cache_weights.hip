@@ -15,9 +15,11 @@
 //  * Many rows: their Q takes that LDS, the VALU (four instructions and an
 //    exponential a score) bounds it, and K goes straight to registers.
 //
-// The exponent is formed as scale * q.k - lse in the natural domain and only
+// fp32: the exponent is formed as scale * q.k - lse in the natural domain and only
 // then multiplied by log2(e): the two are large and nearly equal for the keys
-// that count, and their difference is exact there.
+// that count, and their difference is exact there.  bf16: both are in the log2
+// domain, an instruction less; lse's rounding there (2^-24 of it) is far below a
+// bf16 score's.
 
 #include <algorithm>
 
@@ -30,9 +32,10 @@ namespace {
 using namespace cache;
 
 constexpr int kWaves = 8;
-constexpr int kStepKeys = 32 * kWaves;  // a step: 32 keys of each wavefront
+constexpr int kStepTiles = 8;           // tiles of 32 keys of a step
+constexpr int kStepKeys = 32 * kStepTiles;
 constexpr int kMostBlocks = 32;         // of 32 rows in LDS
-constexpr int kFewRows = 64;            // up to which K comes through LDS
+constexpr int kFewRows = 192;           // up to which K comes through LDS
 
 struct KeyCost {
   int32_t hkv;
@@ -45,9 +48,13 @@ struct KeyCost {
 template <typename T, int D, bool kDma>
 __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) void cache_weights_kernel(CacheWeightArgs p) {
   using G = Tile<T, D>;
-  constexpr int kTile = 32 * G::kRow;
+  constexpr bool kLog2 = G::kBf16;
+  constexpr float kUnit = kLog2 ? kLog2e : 1.f;
+  // LDS of a wavefront's keys: a tile of them, or as many rows as fit in 4 KB
+  constexpr int kTurn = kDma ? 32 : 4096 / G::kRow < 32 ? 4096 / G::kRow : 32;
+  constexpr int kKeys = kTurn * G::kRow;
   // chunk_rows rows of Q, swizzled as K tiles are, then {lse, slope, position} of
-  // each, then (kDma) a K tile of each wavefront
+  // each, then the keys of each wavefront
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];
   __shared__ int dead[kMostBlocks];  // whether a block has rows that count for nothing
   const CacheArgs& a = p.c;
@@ -76,8 +83,8 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
   const int qaddr = lds0 + G::lane_k(l32, hf);
   const int lse0 = lds0 + p.chunk_rows * G::kRow;  // three arrays of chunk_rows
   const int slope0 = lse0 + 4 * p.chunk_rows, pos0 = slope0 + 4 * p.chunk_rows;
-  const int kt = lds0 + (p.chunk_rows * (G::kRow + 12) + 1023) / 1024 * 1024 + wave * kTile;
-  const int kaddr = kt + G::lane_k(l32, hf);
+  const int kt = lds0 + (p.chunk_rows * (G::kRow + 12) + 1023) / 1024 * 1024 + wave * kKeys;
+  const int kaddr = kt + G::lane_k(l32 % kTurn, hf);
   const int koff = G::template dma_lane<false>(lane, stride);
   const bool bias = a.sc.slopes != nullptr;
   const float c = a.sc.x != 0.f ? 1.f : a.sc.c;
@@ -117,12 +124,18 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
                                               (r1.row * a.hkv + kvh) * G::kRow,
                                           r1.n, stride, G::kRow), koff, stride);
         } else {
+          // whole rows, kDmaRows of them an instruction
+          const int row = lane / G::kChunks;
           const uint8_t* src = static_cast<const uint8_t*>(a.k) +
-                               ((r.row + (l32 & 15)) * a.hkv + kvh) * G::kRow + 16 * hf;
+                               ((static_cast<int64_t>(row) * a.hkv) + kvh) * G::kRow +
+                               16 * (lane % G::kChunks);
 #pragma unroll
           for (int i = 0; i < G::kSteps; ++i) {
+            const int at = i * G::kDmaRows % 16;
+            const Rows16& x = i * G::kDmaRows < 16 ? r0 : r1;
             dst[i] = u32x4{0u, 0u, 0u, 0u};
-            if (k.valid) dst[i] = *reinterpret_cast<const u32x4*>(src + 32 * i);
+            if (at + row < x.n)
+              dst[i] = *reinterpret_cast<const u32x4*>(src + (x.row + at) * a.hkv * G::kRow);
           }
         }
         k.old = 0.f;
@@ -137,9 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
 
       u32x4 kf[G::kSteps], kn[G::kSteps];
       Key key{0.f, 0, false}, next{0.f, 0, false};
-      const int tend = min((len + 31) / 32, s1 * kWaves);
-      int t = s0 * kWaves + wave;
-      if (t < tend) fetch(t, kDma ? kn : kf, kDma ? next : key);
+      const int tend = min((len + 31) / 32, s1 * kStepTiles);
+      int t = s0 * kStepTiles + wave;
+      if (t < tend) fetch(t, kn, next);
 
       __syncthreads();  // the last chunk is read
       if (threadIdx.x < kMostBlocks) dead[threadIdx.x] = 0;
@@ -152,9 +165,9 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
         if (i < cn) {
           const float f = p.row_weight != nullptr ? p.row_weight[tok] : 1.f;
           const float y = p.lse[static_cast<int64_t>(tok) * a.hq + h];
-          if (f != 0.f && y != -INFINITY) l = f == 1.f ? y : y - logf(f);
+          if (f != 0.f && y != -INFINITY) l = (f == 1.f ? y : y - logf(f)) * kUnit;
           if (bias) {
-            slope = a.sc.slopes[h];
+            slope = a.sc.slopes[h] * kUnit;
             pos = a.row_pos != nullptr ? a.row_pos[tok] : len + r / g;
           }
         }
@@ -179,12 +192,28 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
           static_cast<uint32_t>(__ballot(lane < kMostBlocks && dead[lane % kMostBlocks] != 0));
 
       for (; t < tend; t += kWaves) {
+        key = next;
         if constexpr (kDma) {
           wait_vm<0>();
-          key = next;
 #pragma unroll
           for (int i = 0; i < G::kSteps; ++i) kf[i] = G::k_frag(kaddr, 0, i);
           wait_lds();  // the tile is in registers
+        } else {
+          // from rows to fragments, kTurn rows at a time (LDS keeps a wavefront's order)
+#pragma unroll
+          for (int z = 0; z < 32 / kTurn; ++z) {
+            constexpr int kOnce = kTurn / G::kDmaRows;
+#pragma unroll
+            for (int i = 0; i < kOnce; ++i) {
+              const int r = i * G::kDmaRows + lane / G::kChunks;
+              *reinterpret_cast<lds_u32x4*>(static_cast<size_t>(
+                  kt + r * G::kRow + 16 * (lane % G::kChunks ^ G::swz_k(r)))) = kn[z * kOnce + i];
+            }
+            if (l32 / kTurn == z) {
+#pragma unroll
+              for (int i = 0; i < G::kSteps; ++i) kf[i] = G::k_frag(kaddr, 0, i);
+            }
+          }
         }
         if (t + kWaves < tend) fetch(t + kWaves, kn, next);
 
@@ -213,7 +242,8 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
                 static_cast<size_t>(lse0 + 4 * (32 * rb + 8 * j + 4 * hf)));
         };
         const auto weight = [&](const f32x16& sc, const f32x4(&l)[4], int v) {
-          return __builtin_amdgcn_exp2f(fmaf(sc[v], cc, -l[v >> 2][v & 3]) * kLog2e);
+          const float x = fmaf(sc[v], cc, -l[v >> 2][v & 3]);
+          return __builtin_amdgcn_exp2f(kLog2 ? x : x * kLog2e);
         };
         // The sum of a block's weights, rows that count for nothing left out,
         // whatever the key holds.
@@ -238,7 +268,7 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
           return sc;
         };
         float sum = 0.f;
-        if constexpr (kDma) {
+        if constexpr (kDma || !G::kBf16) {
           for (int rb = 0; rb < blocks; ++rb) {
             f32x4 l[4];
             row_lse(rb, l);
@@ -298,11 +328,6 @@ __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) 
         sum = half_sum(sum);
         const int slot = t * 32 + l32;
         if (slot < len && hf == 0) p.out[at0 + slot] = key.valid ? key.old + sum : 0.f;
-        if constexpr (!kDma) {
-#pragma unroll
-          for (int i = 0; i < G::kSteps; ++i) kf[i] = kn[i];
-          key = next;
-        }
       }
     }
     x += s1 - s0;
@@ -328,13 +353,14 @@ hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int 
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
     constexpr int kRowLds = Tile<T, D>::kRow + 12;
-    constexpr int kKeyLds = kWaves * 32 * Tile<T, D>::kRow + 1024;
-    constexpr int kFit = std::min(144 * 1024 / kRowLds, 32 * kMostBlocks) / 32 * 32;
+    constexpr int kTileLds = kWaves * 32 * Tile<T, D>::kRow + 1024;
+    constexpr int kTurnLds = kWaves * 4096 + 1024;
+    constexpr int kFit = std::min((158 * 1024 - kTurnLds) / kRowLds, 32 * kMostBlocks) / 32 * 32;
     const int64_t need = std::max<int64_t>(32, (most + 31) / 32 * 32);
     a.chunk_rows = static_cast<int32_t>(std::min<int64_t>(need, kFit));
     int lds = a.chunk_rows * kRowLds;
-    const bool dma = need <= kFewRows && lds + kKeyLds <= 158 * 1024;
-    if (dma) lds += kKeyLds;
+    const bool dma = need <= kFewRows && lds + kTileLds <= 158 * 1024;
+    lds += dma ? kTileLds : kTurnLds;
     a.groups = cus * (lds <= 79 * 1024 ? 2 : 1);
     if (dma)
       hipLaunchKernelGGL((cache_weights_kernel<T, D, true>), dim3(a.groups), dim3(64 * kWaves), lds,
