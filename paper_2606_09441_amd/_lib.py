@@ -193,31 +193,33 @@ def check(fn: str, status: int) -> None:
 
 
 _torch_module = None
+_dtypes, _kinds = {}, {}
 
 
 def _torch():
     global _torch_module
     if _torch_module is None:
         import torch
+        _dtypes.update(uint8=torch.uint8, int32=torch.int32, int64=torch.int64,
+                       float32=torch.float32)
+        _kinds.update({torch.bfloat16: SIFT_BF16, torch.float32: SIFT_F32})
         _torch_module = torch
     return _torch_module
 
 
 def tensor_desc(t) -> SiftTensor:
-    torch = _torch()
+    _torch()
     if not getattr(t, "is_cuda", False):
         raise SiftError("tensor_desc", 4, "tensors must be in GPU memory")
-    if t.dim() != 3:
+    shape = t.shape
+    if len(shape) != 3:
         raise ValueError("expected a [tokens, heads, head_dim] tensor")
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    if t.dtype == torch.bfloat16:
-        dt = SIFT_BF16
-    elif t.dtype == torch.float32:
-        dt = SIFT_F32
-    else:
+    kind = _kinds.get(t.dtype)
+    if kind is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
-    return SiftTensor(t.data_ptr(), dt, t.shape[0], t.shape[1], t.shape[2])
+    return SiftTensor(t.data_ptr(), kind, *shape)
 
 
 def require(fn: str, t, name: str, dtype: str, min_numel: int, device=None) -> None:
@@ -226,15 +228,14 @@ def require(fn: str, t, name: str, dtype: str, min_numel: int, device=None) -> N
     `dtype` ("uint8", "int32", "int64", "float32"), contiguous, with at least
     min_numel elements.  Raises SiftError otherwise."""
     torch = _torch()
-    want = {"uint8": torch.uint8, "int32": torch.int32, "int64": torch.int64,
-            "float32": torch.float32}[dtype]
+    want = _dtypes[dtype]
     if t is None:
         if min_numel > 0:
             raise SiftError(fn, 1, f"{name} is required")
         return
     if not isinstance(t, torch.Tensor):
         raise SiftError(fn, 4, f"{name} must be a torch tensor")
-    if t.dtype != want:
+    if t.dtype is not want:
         raise SiftError(fn, 4, f"{name} must be {dtype}, not {t.dtype}")
     if not t.is_contiguous():
         raise SiftError(fn, 2, f"{name} must be contiguous")
@@ -279,7 +280,7 @@ def _stream_ptr(stream):
     torch = _torch()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object
     if raw is not None:
-        return ctypes.c_void_p(raw(torch.cuda.current_device()))
+        return raw(torch.cuda.current_device())
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -426,11 +427,10 @@ class Plan:
                     self.device)
         if out is None:
             out = _empty(q.shape, q.dtype, q.device, stream)
-        _on(fn, self.device, q=q, k=k, v=v, out=out)
-        qd, kd, vd, od = tensor_desc(q), tensor_desc(k), tensor_desc(v), tensor_desc(out)
+        dev = self.device
         check(fn, lib().sift_plan_dense(
-            self._h, ctypes.byref(qd), ctypes.byref(kd), ctypes.byref(vd), MASKS[mask],
-            ctypes.byref(score), ctypes.byref(od), _ptr(lse), _stream_ptr(stream)))
+            self._h, _desc(fn, q, "q", dev), _desc(fn, k, "k", dev), _desc(fn, v, "v", dev),
+            MASKS[mask], score, _desc(fn, out, "out", dev), _address(lse), _stream_ptr(stream)))
         return out
 
 
@@ -443,11 +443,14 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _on(fn, device, **tensors) -> None:
-    """All of these tensors on `device`."""
-    for name, t in tensors.items():
-        if getattr(t, "device", None) != device:
-            raise SiftError(fn, 7, f"{name} is not on {device}")
+def _desc(fn, t, name, device) -> SiftTensor:
+    if getattr(t, "device", None) != device:
+        raise SiftError(fn, 7, f"{name} is not on {device}")
+    return tensor_desc(t)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 def score_struct(fn, scale, cap, slopes, num_q_heads, device) -> SiftScore:
@@ -701,7 +704,9 @@ class CachePages:
             raise SiftError(fn, 7, f"v_pages is on {v_pages.device}, k_pages on {dev}")
         self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
         self.page_lens, self.key_pos = page_lens, key_pos
-        self._kd, self._vd = kd, vd
+        self._held = (k_pages, v_pages, page_table, lens, page_lens, key_pos, kd, vd)
+        self.sizes = (dev, *(None if t is None else t.numel()
+                             for t in (page_table, lens, page_lens, key_pos)))
         self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
                                   lens.data_ptr(), 0 if page_lens is None else page_lens.data_ptr(),
                                   0 if key_pos is None else key_pos.data_ptr())
@@ -723,6 +728,8 @@ class Cache:
         self.num_seqs, self.hq, self.hkv, self.d = num_seqs, num_q_heads, num_kv_heads, head_dim
         self.page, self.max_pages, self.max_rows = page, max_pages, max_rows
         self.slots = max_pages * page
+        pages = num_seqs * max_pages
+        self._tables = (pages, num_seqs, pages, num_seqs * num_kv_heads * self.slots)
 
     def close(self):
         if self._h is not None:
@@ -743,15 +750,13 @@ class Cache:
 
     def _kv(self, fn, kv):
         """The tables' sizes, which the library cannot see."""
-        pages = self.num_seqs * self.max_pages
-        if kv.k_pages.device != self.device:
-            raise SiftError(fn, 7, f"the pages are on {kv.k_pages.device}, the cache on {self.device}")
-        for name, t, n in (("page_table", kv.page_table, pages), ("lens", kv.lens, self.num_seqs),
-                           ("page_lens", kv.page_lens, pages),
-                           ("key_pos", kv.key_pos, self.num_seqs * self.hkv * self.slots)):
-            if t is not None and t.numel() < n:
-                raise SiftError(fn, 5, f"{name} holds {t.numel()} elements, needs {n}")
-        return ctypes.byref(kv.struct)
+        device, *have = kv.sizes
+        if device != self.device:
+            raise SiftError(fn, 7, f"the pages are on {device}, the cache on {self.device}")
+        for name, m, n in zip(("page_table", "lens", "page_lens", "key_pos"), have, self._tables):
+            if m is not None and m < n:
+                raise SiftError(fn, 5, f"{name} holds {m} elements, needs {n}")
+        return kv.struct
 
     def _rows(self, fn, q, row_ptr, row_pos):
         if row_ptr is not None:
@@ -782,12 +787,11 @@ class Cache:
             require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
         if out is None:
             out = _empty(q.shape, q.dtype, q.device, stream)
-        _on(fn, self.device, q=q, k_new=k_new, v_new=v_new, out=out)
-        qd, kd, vd, od = tensor_desc(q), tensor_desc(k_new), tensor_desc(v_new), tensor_desc(out)
+        dev = self.device
         check(fn, lib().sift_cache_attention(
-            self._h, self._kv(fn, kv), ctypes.byref(rows), ctypes.byref(qd), ctypes.byref(kd),
-            ctypes.byref(vd), _ptr(tree_mask), words, ctypes.byref(score), ctypes.byref(od),
-            _ptr(lse), _stream_ptr(stream)))
+            self._h, self._kv(fn, kv), rows, _desc(fn, q, "q", dev), _desc(fn, k_new, "k_new", dev),
+            _desc(fn, v_new, "v_new", dev), _address(tree_mask), words, score,
+            _desc(fn, out, "out", dev), _address(lse), _stream_ptr(stream)))
         return out
 
     def _slot_buffer(self, fn, t, name, dtype="float32"):
@@ -814,13 +818,11 @@ class Cache:
             out = _empty((self.num_seqs, self.hkv, self.slots), torch.float32, self.device, stream)
             with torch.cuda.stream(stream):  # (None: the current one)
                 out.zero_()
-        _on(fn, self.device, q=q)
         self._slot_buffer(fn, out, "out")
         score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
-        qd = tensor_desc(q)
         check(fn, lib().sift_cache_accumulate(
-            self._h, self._kv(fn, kv), ctypes.byref(rows), ctypes.byref(qd), _ptr(lse),
-            _ptr(row_weight), ctypes.byref(score), _ptr(weights), decay, _ptr(out),
+            self._h, self._kv(fn, kv), rows, _desc(fn, q, "q", self.device), _address(lse),
+            _address(row_weight), score, _address(weights), decay, _address(out),
             _stream_ptr(stream)))
         return out
 
@@ -838,14 +840,17 @@ class Cache:
         shape = (self.num_seqs, self.hkv, self.slots)
         if weights_out is None:
             weights_out = _empty(shape, torch.float32, self.device, stream)
+        else:
+            self._slot_buffer(fn, weights_out, "weights_out")
         if pos_out is None:
             pos_out = _empty(shape, torch.int32, self.device, stream)
+        else:
+            self._slot_buffer(fn, pos_out, "pos_out", "int32")
         if lens_out is None:
             lens_out = _empty((self.num_seqs,), torch.int32, self.device, stream)
-        self._slot_buffer(fn, weights_out, "weights_out")
-        self._slot_buffer(fn, pos_out, "pos_out", "int32")
-        require(fn, lens_out, "lens_out", "int32", self.num_seqs, self.device)
+        else:
+            require(fn, lens_out, "lens_out", "int32", self.num_seqs, self.device)
         check(fn, lib().sift_cache_evict(
-            self._h, self._kv(fn, kv), _ptr(weights), _ptr(next_pos), budget, sinks, recent,
-            _ptr(weights_out), _ptr(pos_out), _ptr(lens_out), _stream_ptr(stream)))
+            self._h, self._kv(fn, kv), _address(weights), _address(next_pos), budget, sinks, recent,
+            _address(weights_out), _address(pos_out), _address(lens_out), _stream_ptr(stream)))
         return weights_out, pos_out, lens_out
