@@ -426,7 +426,7 @@ class Plan:
             require(fn, lse, "lse", "float32", self.info["num_tokens"] * self.info["num_q_heads"],
                     self.device)
         if out is None:
-            out = _empty(q.shape, q.dtype, q.device, stream)
+            out = _empty_like(q, stream)
         dev = self.device
         check(fn, lib().sift_plan_dense(
             self._h, _desc(fn, q, "q", dev), _desc(fn, k, "k", dev), _desc(fn, v, "v", dev),
@@ -434,8 +434,16 @@ class Plan:
         return out
 
 
-def _empty(shape, dtype, device, stream):
+def _empty_like(t, stream):
     """A buffer for a call to write, of the pool of the stream that it runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty_like(t)
+    with torch.cuda.stream(stream):
+        return torch.empty_like(t)
+
+
+def _empty(shape, dtype, device, stream):
     torch = _torch()
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
@@ -786,7 +794,7 @@ class Cache:
         if lse is not None:
             require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
         if out is None:
-            out = _empty(q.shape, q.dtype, q.device, stream)
+            out = _empty_like(q, stream)
         dev = self.device
         check(fn, lib().sift_cache_attention(
             self._h, self._kv(fn, kv), rows, _desc(fn, q, "q", dev), _desc(fn, k_new, "k_new", dev),

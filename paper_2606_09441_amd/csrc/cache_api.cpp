@@ -150,7 +150,8 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
       hipDeviceGetAttribute(&c->cus, hipDeviceAttributeMultiprocessorCount, c->device) !=
           hipSuccess)
     return fail();
-  const bool wide = sift::cache_attn_wide(true, max_rows * g);
+  const bool wide = sift::cache_attn_wide(
+      true, max_rows * g, static_cast<int64_t>(num_seqs) * num_kv_heads * max_pages * page);
   const size_t rows = static_cast<size_t>(2 * 2 * c->cus) *
                       (wide ? sift::kCacheWideRows : sift::kCacheRows);
   const size_t o_bytes = rows * head_dim * sizeof(float);

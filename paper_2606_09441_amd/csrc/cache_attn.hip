@@ -210,77 +210,93 @@ __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void cache_attn_k
   }
 }
 
-// Merge of the parts of one (new token, query head), a workgroup each: eight
-// groups of 32 lanes take every eighth part, lane l dims l D / 32 and on.
+// Merge of the parts of each (new token, query head), `each` of them a workgroup:
+// eight groups of 32 lanes take every eighth part, lane l dims l D / 32 and on.
 template <typename U, typename T, int D>
-__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p) {
+__global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p, int each) {
   const CacheArgs& a = p.c;
   constexpr int kDims = D / 32;
   __shared__ float acc[8][D];
   __shared__ float part[8][2];
   const int g = a.hq / a.hkv;
   const UnitCost<U> cost{g, a.hkv};
-  const int64_t item = blockIdx.x;
-  const int token = static_cast<int>(item / a.hq), h = static_cast<int>(item % a.hq);
   const Work work(a, cost);
   const Split split(work.total, p.groups);
   if (split.total == 0) return;
-  const Place pl = work.find_token(token);
-  if (pl.b >= a.num_seqs) return;  // no sequence's
-  const Seq s = work.seq(pl.b);
-  const int steps = uniform(cost.steps(s));
-  const int r = (token - s.row0) * g + h % g;
-  const int u0 = uniform(pl.at + (h / g * cost.blocks(s) + r / U::kRows) * steps);
-  const int first = split.of(u0);
-  const int n = split.of(u0 + steps - 1) - first + 1;
-  if (n == 1) return;  // written already
-  // the first part is its workgroup's second, the others their workgroups' first
-  const auto slot = [&](int i) {
-    return (2 * static_cast<int64_t>(first + i) + (i == 0)) * U::kRows + r % U::kRows;
-  };
-  float top = -INFINITY;
-  for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p.part_ml[slot(i)].x);
+  const int end = min(static_cast<int>(blockIdx.x + 1) * each, a.rows * a.hq);
+  for (int item = blockIdx.x * each; item < end; ++item) {
+    const int token = item / a.hq, h = item % a.hq;
+    const Place pl = work.find_token(token);
+    if (pl.b >= a.num_seqs) continue;  // no sequence's
+    const Seq s = work.seq(pl.b);
+    const int steps = uniform(cost.steps(s));
+    const int r = (token - s.row0) * g + h % g;
+    const int u0 = uniform(pl.at + (h / g * cost.blocks(s) + r / U::kRows) * steps);
+    const int first = split.of(u0);
+    const int n = split.of(u0 + steps - 1) - first + 1;
+    if (n == 1) continue;  // written already
+    // the first part is its workgroup's second, the others their workgroups' first
+    const auto slot = [&](int i) {
+      return (2 * static_cast<int64_t>(first + i) + (i == 0)) * U::kRows + r % U::kRows;
+    };
+    float top = -INFINITY;
+    for (int i = threadIdx.x & 63; i < n; i += 64) top = fmaxf(top, p.part_ml[slot(i)].x);
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  const int grp = threadIdx.x >> 5, l32 = threadIdx.x & 31;
-  float l = 0.f, le = 0.f, o[kDims] = {};
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const int grp = threadIdx.x >> 5, l32 = threadIdx.x & 31;
+    float l = 0.f, le = 0.f, o[kDims] = {};
 #pragma unroll 4
-  for (int i = grp; i < n; i += 8) {
-    const float4 ml = p.part_ml[slot(i)];
-    const float* src = p.part_o + slot(i) * D + l32 * kDims;
-    const float wt = part_weight(ml.x, top);
-    l += ml.y * wt;
-    le += ml.z * wt;
+    for (int i = grp; i < n; i += 8) {
+      const float4 ml = p.part_ml[slot(i)];
+      const float* src = p.part_o + slot(i) * D + l32 * kDims;
+      const float wt = part_weight(ml.x, top);
+      l += ml.y * wt;
+      le += ml.z * wt;
 #pragma unroll
-    for (int e = 0; e < kDims; ++e) o[e] += src[e] * wt;
-  }
+      for (int e = 0; e < kDims; ++e) o[e] += src[e] * wt;
+    }
+    __syncthreads();  // the last item's sums are read
 #pragma unroll
-  for (int e = 0; e < kDims; ++e) acc[grp][l32 * kDims + e] = o[e];
-  if (l32 == 0) {
-    part[grp][0] = l;
-    part[grp][1] = le;
-  }
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  float y = 0.f;
-  l = le = 0.f;
+    for (int e = 0; e < kDims; ++e) acc[grp][l32 * kDims + e] = o[e];
+    if (l32 == 0) {
+      part[grp][0] = l;
+      part[grp][1] = le;
+    }
+    __syncthreads();
+    if (threadIdx.x >= D) continue;
+    float y = 0.f;
+    l = le = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    y += acc[i][threadIdx.x];
-    l += part[i][0];
-    le += part[i][1];
+    for (int i = 0; i < 8; ++i) {
+      y += acc[i][threadIdx.x];
+      l += part[i][0];
+      le += part[i][1];
+    }
+    const int64_t at = static_cast<int64_t>(item) * D + threadIdx.x;
+    static_cast<T*>(p.out)[at] = static_cast<T>(y * inverse(l));
+    if (p.lse != nullptr && threadIdx.x == 0) p.lse[item] = log_sum(top, le);
   }
-  static_cast<T*>(p.out)[item * D + threadIdx.x] = static_cast<T>(y * inverse(l));
-  if (p.lse != nullptr && threadIdx.x == 0) p.lse[item] = log_sum(top, le);
 }
 
 }  // namespace
 
-// Rows of a kv head beyond which bf16 goes by the wide units, whose 128 rows share
-// what the workgroup reads and whose matrix work is pipelined.
-constexpr int64_t kNarrowMost = 64;
+// bf16 with more than 32 rows of a kv head goes by the wide units, whose 128 rows
+// share what the workgroup reads and whose matrix work is pipelined, but whose
+// workgroups take longer to start and to end: only where there are so many rows
+// times cached keys.  us of narrow / wide, 8 kv heads, D = 128: 48 rows of 65536 keys
+// 88 / 65, of 32768 48 / 46; 128 rows of 32768 59 / 54, of 16384 40 / 44; 256 rows of
+// 16384 55 / 55, of 4096 29 / 38; 32 rows of 65536 54 / 61.
+constexpr int64_t kNarrowMost = int64_t(24) << 20;
 
-bool cache_attn_wide(bool bf16, int64_t rows_of_kv) { return bf16 && rows_of_kv > kNarrowMost; }
+// Workgroups of the merge: as many as are resident at once, since where there are
+// many items most have nothing to merge and a workgroup of its own costs more than
+// they (us of the call with an item each / with 2048 workgroups: 256 sequences of
+// 512 keys, 65536 items 299 / 218, 8192 items 133 / 125; up to 1024 items the same).
+constexpr int64_t kMergeGroups = 2048;
+
+bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys) {
+  return bf16 && rows_of_kv > kRows && rows_of_kv >= (kNarrowMost + keys - 1) / keys;
+}
 
 int64_t cache_attn_steps(const CacheArgs& a) {
   // of the narrow units: the wide ones are a quarter as many, of twice the steps
@@ -296,16 +312,20 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hi
   const int64_t items = static_cast<int64_t>(a.c.rows) * a.c.hq;
   if (items >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
   const int64_t most = static_cast<int64_t>(std::min(a.c.rows, a.c.max_rows)) * (a.c.hq / a.c.hkv);
-  const bool wide = cache_attn_wide(bf16, most);
+  const bool wide = cache_attn_wide(
+      bf16, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
-    const dim3 grid(static_cast<unsigned>(items)), block(256);
+    // no more workgroups than are resident at once: most have nothing to merge where
+    // there are many
+    const int each = static_cast<int>((items + kMergeGroups - 1) / kMergeGroups);
+    const dim3 grid(static_cast<unsigned>((items + each - 1) / each)), block(256);
     if constexpr (Tile<T, D>::kBf16) {
       if (wide) {
         const hipError_t e = launch_cache_wide(a, D, stream);
         if (e != hipSuccess) return e;
-        hipLaunchKernelGGL((cache_merge_kernel<Wide, T, D>), grid, block, 0, stream, a);
+        hipLaunchKernelGGL((cache_merge_kernel<Wide, T, D>), grid, block, 0, stream, a, each);
         return hipGetLastError();
       }
     }
@@ -313,7 +333,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hi
       hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), block, 0, stream, a);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a);
+      hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a, each);
     }
     return hipGetLastError();
   };
