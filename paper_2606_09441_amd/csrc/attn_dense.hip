@@ -84,16 +84,18 @@ struct Row {
 // This wavefront's 16 rows of a 64-key tile, K or V, to LDS address `slot`; off0:
 // dma_lane.
 template <typename T, int D, bool kV>
-__device__ __forceinline__ void stage(const DenseArgs& a, const Row& w, int t, int slot, int off0) {
+__device__ __forceinline__ i32x4 tile_rows(const DenseArgs& a, const Row& w, int t) {
   using G = Tile<T, D>;
   const int k0 = w.first + t * kKeys + 16 * w.wave;
-  const int stride = a.hkv * G::kRow;
-  dma_rows<T, D, kV>(
-      slot + w.wave * 16 * G::kRow,
-      rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
-                    (static_cast<int64_t>(k0) * a.hkv + w.kvh) * G::kRow,
-                min(16, w.kend - k0), stride, G::kRow),
-      off0, stride);
+  return rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
+                       (static_cast<int64_t>(k0) * a.hkv + w.kvh) * G::kRow,
+                   min(16, w.kend - k0), a.hkv * G::kRow, G::kRow);
+}
+template <typename T, int D, bool kV>
+__device__ __forceinline__ void stage(const DenseArgs& a, const Row& w, int t, int slot, int off0) {
+  using G = Tile<T, D>;
+  dma_rows<T, D, kV>(slot + w.wave * 16 * G::kRow, tile_rows<T, D, kV>(a, w, t), off0,
+                     a.hkv * G::kRow);
 }
 
 // Adds what clean_tile took out to the rows that see it.
@@ -223,8 +225,8 @@ struct DenseTiles {
   // reference, which the near keys set, then hardly moves.
   __device__ __forceinline__ int tile(int i) const { return !kBias ? i : i <= mid ? mid - i : i; }
   template <bool kV>
-  __device__ __forceinline__ void fetch(int i, int lds, int off0) const {
-    stage<T, D, kV>(a, w, tile(i), lds, off0);
+  __device__ __forceinline__ i32x4 rows(int i) const {
+    return tile_rows<T, D, kV>(a, w, tile(i));
   }
   __device__ __forceinline__ void clean(int i, int lds) {
     if (w.mixed(w.first + tile(i) * kKeys)) cleaned |= clean_tile<T, D>(lds);
@@ -236,7 +238,7 @@ struct DenseTiles {
     const bool around = kBias && j0 + kKeys - 1 > lo && j0 < lo + 31;  // a row inside the tile
     const float d = static_cast<float>(w.tok - j0 - 4 * w.hf);
     mx = take_tile<kCap, kBias>(
-        a.sc, s0, s1, mx, mn, masked || around, w.bits(j0), w.hf, slope,
+        a.sc, s0, s1, mx, mn, masked || around, [&] { return w.bits(j0); }, w.hf, slope,
         [&](int key) { return fabsf(d - static_cast<float>(key)); }, f);
     if constexpr (kBias) {
       if (!masked && !around) {

@@ -32,18 +32,15 @@ struct CacheTiles {
   // (with a bias the near keys, which set the reference, come first)
   __device__ __forceinline__ int tile(int i) const { return kBias ? s0 + steps - 1 - i : s0 + i; }
   template <bool kV>
-  __device__ __forceinline__ void fetch(int i, int lds, int off0) const {
+  __device__ __forceinline__ i32x4 rows(int i) const {
     const CacheArgs& a = p.c;
     const int t = tile(i), j = (t - ct) * kKeys + 16 * wave;
     const Rows16 r = t < ct ? cached_rows(a, b, len, t * kKeys + 16 * wave)
                             : Rows16{static_cast<int64_t>(row0) + j, min(max(n - j, 0), 16)};
     const void* base = t < ct ? (kV ? a.v : a.k) : (kV ? p.v_new : p.k_new);
-    const int stride = a.hkv * G::kRow;
-    dma_rows<T, D, kV>(lds + wave * 16 * G::kRow,
-                       rows_rsrc(reinterpret_cast<unsigned long long>(base) +
-                                     (r.row * a.hkv + kvh) * G::kRow,
-                                 r.n, stride, G::kRow),
-                       off0, stride);
+    return rows_rsrc(
+        reinterpret_cast<unsigned long long>(base) + (r.row * a.hkv + kvh) * G::kRow, r.n,
+        a.hkv * G::kRow, G::kRow);
   }
   __device__ __forceinline__ void clean(int i, int lds) {
     if (tile(i) >= ct) cleaned |= clean_tile<T, D>(lds);
@@ -89,7 +86,8 @@ struct CacheTiles {
     }
     const float d = static_cast<float>(pos - (fresh ? len : 0) - j0);
     return take_tile<kCap, kBias>(
-        a.sc, s0_, s1_, mx, mn, kBias || __builtin_amdgcn_ballot_w64(~m != 0) != 0, m, hf, slope,
+        a.sc, s0_, s1_, mx, mn, kBias || __builtin_amdgcn_ballot_w64(~m != 0) != 0, [&] { return m; }, hf,
+        slope,
         [&](int key) {
           return fabsf(table != nullptr ? static_cast<float>(pos - table[min(j0 + key, last)])
                                         : d - static_cast<float>(key));

@@ -36,12 +36,12 @@ __device__ __forceinline__ float capped(const Form& f, float z) {
 
 // The form of a tile whose products, s0 and s1, have the largest mx and the
 // smallest mn.  Large products are capped in place.  Then, where `odd`, whatever
-// else sets the tile apart: keys whose bit is not set (bits: one a key), and the
+// else sets the tile apart: keys whose bit is not set (bits(): one a key), and the
 // bias, slope * dist(key), where kBias.  Returns the bound of the row's scores,
 // its largest.
-template <bool kCap, bool kBias, typename Dist>
+template <bool kCap, bool kBias, typename Bits, typename Dist>
 __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x16& s1, float mx,
-                                           float mn, bool odd, uint64_t bits, int hf, float slope,
+                                           float mn, bool odd, Bits bits, int hf, float slope,
                                            Dist dist, Form& f) {
   // Masked scores: -inf, or where z p(z^2) has to stay a number one that no score
   // comes near (|capped score| <= kMaxCap log2(e)).
@@ -60,8 +60,9 @@ __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x
     }
   }
   if (odd) {
-    const uint32_t m0 = static_cast<uint32_t>(bits >> (4 * hf));
-    const uint32_t m1 = static_cast<uint32_t>(bits >> (32 + 4 * hf));
+    const uint64_t m = bits();
+    const uint32_t m0 = static_cast<uint32_t>(m >> (4 * hf));
+    const uint32_t m1 = static_cast<uint32_t>(m >> (32 + 4 * hf));
     mx = -INFINITY;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -92,7 +93,7 @@ __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x
 // Src: what the tiles are.
 //   int steps               of the workgroup
 //   int mine                of this wavefront: it takes the first ones
-//   fetch<kV>(i, lds, off0) DMA of this wavefront's 16 rows of step i's K or V tile
+//   rows<kV>(i)             this wavefront's 16 rows of step i's K or V tile
 //   clean(i, lds)           the V tile that the step is about to use (all
 //                           wavefronts): see only_finite
 //   take(i, s0, s1, mx, mn, form) -> bound   as take_tile
@@ -103,12 +104,14 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
   using G = Tile<T, D>;
   constexpr int kTile = kKeys * G::kRow;
   constexpr int kSteps = G::kSteps;         // of QK^T: 16 dims each
+  static_assert(kSteps == 2 * G::kGroupDmas, "a DMA instruction a step");
   constexpr int kEach = 32 / kSteps;        // present scores that go with one
   constexpr int kPv = 4 * (D / 32);         // matrix instructions of PV
   constexpr int kDone = 32 / kPv;           // next scores that go with one
   const int l32 = lane & 31, hf = lane >> 5;
   // K slots 0 and 1, V slots 0 and 1
   const int lds0 = static_cast<int>(reinterpret_cast<size_t>((lds_u8*)smem));
+  const int own = lds0 + uniform(threadIdx.x >> 6) * 16 * G::kRow;  // rows that it brings
   int kaddr = lds0 + G::lane_k(l32, hf);
   int vaddr = lds0 + 2 * kTile + G::lane_v(lane, l32, hf);
   int koff = G::template dma_lane<false>(lane, stride);
@@ -141,8 +144,9 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
   };
 
   // n0, n1 = K Q^T from K slot `slot`, beside the weights of the tile c0, c1
+  // and issue(s), s = 0 .. kSteps - 1
   const auto qk_and_weigh = [&](int slot, f32x16& n0, f32x16& n1, const f32x16& c0,
-                                const f32x16& c1, const Form& f) {
+                                const f32x16& c1, const Form& f, auto issue) {
     const float base = st.base();
     float sum = 0.f, le = 0.f;
     u32x4 x[3][2];
@@ -158,6 +162,7 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
       n1 = dot_step<T>(x[s % 3][1], q.x[s], n1);
 #pragma unroll
       for (int u = 0; u < kEach; u += 2) weigh(s * kEach + u, c0, c1, f, base, sum, le);
+      issue(s);
       if (s + 3 < kSteps) {
         x[s % 3][0] = G::k_frag(kaddr + slot, 0, s + 3);
         x[s % 3][1] = G::k_frag(kaddr + slot, 1, s + 3);
@@ -191,13 +196,21 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
     const int par = i & 1;
     // addresses made anew in every step: kept, each would hold a register
     asm volatile("" : "+v"(kaddr), "+v"(vaddr), "+v"(koff), "+v"(voff));
-    if (i + 1 < src.steps)
-      src.template fetch<true>(i + 1, lds0 + (2 + (par ^ 1)) * kTile, voff);
-    if (i + 2 < src.steps) src.template fetch<false>(i + 2, lds0 + par * kTile, koff);
+    // K of step i + 2 and V of step i + 1 (past the last step zeros, from nowhere)
+    const i32x4 none = i32x4{0, 0, 0, kBufferWord3};
+    const i32x4 krs = i + 2 < src.steps ? src.template rows<false>(i + 2) : none;
+    const i32x4 vrs = i + 1 < src.steps ? src.template rows<true>(i + 1) : none;
+    const auto issue = [&](int s) {
+      if (s < G::kGroupDmas)
+        dma_b128(own + par * kTile + s * 1024, G::template dma_off<false>(koff, s, stride), krs);
+      else
+        dma_b128(own + (2 + (par ^ 1)) * kTile + (s - G::kGroupDmas) * 1024,
+                 G::template dma_off<true>(voff, s - G::kGroupDmas, stride), vrs);
+    };
     src.clean(i, lds0 + (2 + par) * kTile);
     if (i < src.mine) {
       // (past the last tile a body like the others: its scores go nowhere)
-      qk_and_weigh((par ^ 1) * kTile, n0, n1, c0, c1, f);
+      qk_and_weigh((par ^ 1) * kTile, n0, n1, c0, c1, f, issue);
       float mx = -INFINITY, mn = INFINITY;
       pv_and(par * kTile, [&](int e) {
 #pragma unroll
@@ -207,16 +220,20 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
           mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
           if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
         }
+        asm volatile("" : "+v"(mx), "+v"(mn));  // here, not where they are used
       });
       if (i + 1 < src.mine) st.rescale(src.take(i + 1, n0, n1, mx, mn, f));
+    } else {
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) issue(s);
     }
     wait_vm<0>();
     __syncthreads();
   };
 
-  src.template fetch<false>(0, lds0, koff);
-  src.template fetch<true>(0, lds0 + 2 * kTile, voff);
-  if (src.steps > 1) src.template fetch<false>(1, lds0 + kTile, koff);
+  dma_rows<T, D, false>(own, src.template rows<false>(0), koff, stride);
+  dma_rows<T, D, true>(own + 2 * kTile, src.template rows<true>(0), voff, stride);
+  if (src.steps > 1) dma_rows<T, D, false>(own + kTile, src.template rows<false>(1), koff, stride);
   wait_vm<0>();
   __syncthreads();
   f32x16 a0{}, a1{}, b0{}, b1{};
