@@ -23,7 +23,7 @@ constexpr int kKeys = 64;  // of a tile
 // the tanh's p, or (1, 0, ..) where the scores are capped already; without kCap
 // p0 alone, the scale.  The key's terms only with kLinear.
 struct Form {
-  float p0, p1, p2;
+  float p0, p1, p2, p3;
   float slope_key, d;
 };
 
@@ -31,7 +31,7 @@ template <bool kCap>
 __device__ __forceinline__ float capped(const Form& f, float z) {
   if constexpr (!kCap) return z * f.p0;
   const float y = z * z;
-  return z * fmaf(y, fmaf(y, f.p2, f.p1), f.p0);
+  return z * fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
 }
 
 // The form of a tile whose products, s0 and s1, have the largest mx and the
@@ -46,7 +46,7 @@ __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x
   // Masked scores: -inf, or where z p(z^2) has to stay a number one that no score
   // comes near (|capped score| <= kMaxCap log2(e)).
   constexpr float kOut = kCap ? -1e18f : -INFINITY;
-  f = Form{kCap ? sc.b[0] : sc.c, sc.b[1], sc.b[2], 0.f, 0.f};
+  f = Form{kCap ? sc.b[0] : sc.c, sc.b[1], sc.b[2], sc.b[3], 0.f, 0.f};
   if constexpr (kCap) {
     if (__builtin_amdgcn_ballot_w64(fmaxf(mx, -mn) * sc.x > kTanhSmallBf16)) {
 #pragma unroll
@@ -56,7 +56,7 @@ __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x
       }
       mx = cap_any(sc, mx);
       f.p0 = 1.f;
-      f.p1 = f.p2 = 0.f;
+      f.p1 = f.p2 = f.p3 = 0.f;
     }
   }
   if (odd) {
@@ -82,7 +82,7 @@ __device__ __forceinline__ float take_tile(const ScoreArgs& sc, f32x16& s0, f32x
     }
     if constexpr (kCap || kBias) {  // all of the exponent is in the scores
       f.p0 = 1.f;
-      f.p1 = f.p2 = 0.f;
+      f.p1 = f.p2 = f.p3 = 0.f;
       return half_max(mx);
     }
   }
@@ -132,7 +132,7 @@ __device__ __forceinline__ void run_pipe(Src& src, const QFrag<__bf16, D>& q, Ro
         b = fmaf(f.slope_key, static_cast<float>(key_of(v + u) + (i < 2 ? 0 : 32)), fmaf(-f.slope_key, f.d, -base));
       if constexpr (kCap) {
         const float y = z * z;
-        pz = fmaf(y, fmaf(y, f.p2, f.p1), f.p0);
+        pz = fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
       }
       p[u] = __builtin_amdgcn_exp2f(fmaf(z, pz, b));
     }

@@ -32,7 +32,7 @@ inline sift_status make_score(const sift_score* score, int32_t head_dim, double 
   double power = scale * unit;  // unit scale (scale / cap)^2i
   for (int i = 0; i < 5; ++i, power *= x * x) {
     out->a[i] = static_cast<float>(kTanhPoly[i] * power);
-    if (i < 3) out->b[i] = static_cast<float>(kTanhPolyBf16[i] * power);
+    if (i < 4) out->b[i] = static_cast<float>(kTanhPolyBf16[i] * power);
   }
   // a factor that fp32 does not hold, or holds as a denormal, would be a cap of another value
   if (!std::isnormal(out->x) || !std::isnormal(out->cap2)) return SIFT_E_UNSUPPORTED;

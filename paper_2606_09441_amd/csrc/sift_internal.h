@@ -393,19 +393,19 @@ struct ScoreArgs {
   float x;        // scale / cap: x z0 is the tanh's argument (z0 = q.k); 0: no cap
   float cap2;     // cap * unit
   float a[5];     // unit * s = z0 * poly(z0^2) where |x z0| <= kTanhSmall
-  float b[3];     // the same to bf16's needs where |x z0| <= kTanhSmallBf16
+  float b[4];     // the same to bf16's needs where |x z0| <= kTanhSmallBf16
   const float* slopes;  // [Hq] or nullptr
 };
 
-// tanh(y) / y as a polynomial in y^2, minimax fits made by reweighted least
-// squares: of the relative error, degree 4 over |y| <= kTanhSmall (1.4e-8), and of
-// tanh's absolute error, degree 2 over |y| <= kTanhSmallBf16 (5.9e-07: at a cap of 50 a
-// score, and a weight, is off by 3e-05, where rounding the weight to bf16 takes 4e-3).
+// tanh(y) / y as a polynomial in y^2, minimax fits of the relative error made by
+// reweighted least squares: degree 4 over |y| <= kTanhSmall (1.4e-8), degree 3
+// over |y| <= kTanhSmallBf16 (1.0e-7: a score of 16 is off by 1.6e-6, a weight
+// by as much of it, where rounding it to bf16 takes 4e-3).
 constexpr float kTanhSmall = 0.5f;
 constexpr double kTanhPoly[5] = {0.9999999869, -0.3333306939, 0.1332477931, -0.05298607504,
                                  0.01713500614};
-constexpr float kTanhSmallBf16 = 0.36f;
-constexpr double kTanhPolyBf16[3] = {0.9999884686, -0.3326102606, 0.1218926843};
+constexpr float kTanhSmallBf16 = 0.4f;
+constexpr double kTanhPolyBf16[4] = {0.9999999019, -0.3333136246, 0.1327097676, -0.04755360348};
 // Caps beyond this would not show in fp32, and their squares would overflow.
 constexpr float kMaxCap = 1e15f;
 
