@@ -33,14 +33,14 @@ class PromptCache:
         self.plan = Plan(so, ps, num_q_heads, num_kv_heads, head_dim, page)
         seqs = len(ps) - 1
         tiles = [-(-(b - a) // page) for a, b in zip(so, so[1:])]
-        longest = max(so[b] - so[a] for a, b in zip(ps, ps[1:]))
         most = max(sum(tiles[a:b]) for a, b in zip(ps, ps[1:]))
         max_pages = max(1, most + -(-room // page))
         sizes = (seqs, num_q_heads, num_kv_heads, head_dim, page, max_pages)
+        self.longest = max(so[b] - so[b - 1] for b in ps[1:])  # query
         # of the queries' tokens, and of the answers'
-        self._queries = Cache(*sizes, max(1, max(so[b] - so[b - 1] for b in ps[1:])))
+        self._queries = Cache(*sizes, max(1, self.longest))
         self.cache = Cache(*sizes, max_rows)
-        self.max_rows, self.longest = max_rows, longest
+        self.max_rows = max_rows
 
         table = [[b * max_pages + p for p in range(max_pages)] for b in range(seqs)]
         tile_page, tile_rows, lens, page_lens, pos = [], [], [], [], []
@@ -97,6 +97,8 @@ class PromptCache:
         under `mask`; leaves the documents' keys in the pages, with the weights that
         the query's tokens give them, and the query's own to be appended by cut."""
         torch = _torch()
+        if self.weights is not None:
+            raise SiftError("PromptCache.prefill", 6, "the prompts are prefilled already")
         if la is not None and (cap or slopes is not None):
             raise SiftError("PromptCache.prefill", 4, "the sparse prefill takes no cap and no bias")
         self._score = dict(scale=scale, cap=cap, slopes=slopes)
@@ -120,6 +122,8 @@ class PromptCache:
     def cut(self, budget, sinks=4, recent=0):
         """Every kv head keeps `budget` keys: the first `sinks`, the last `recent` and
         those of the largest weights."""
+        if self.weights is None:
+            raise SiftError("PromptCache.cut", 6, "the prompts are not prefilled yet")
         self.weights, key_pos, lens = self.cache.evict(self.pages, self.weights, budget, sinks,
                                                        recent, self.next_pos)
         self.pages = CachePages(self.pages.k_pages, self.pages.v_pages, self.pages.page_table, lens,
@@ -135,7 +139,7 @@ class PromptCache:
         """(out, lse) of new tokens over the cache and each other; row_pos None: each
         follows the one before."""
         torch = _torch()
-        if self._pending is not None:
+        if self.weights is None or self._pending is not None:
             raise SiftError("PromptCache.step", 6, "the prompts' caches are not cut yet")
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
         out = self.cache.attention(q, k_new, v_new, self.pages, row_ptr=row_ptr, tree_mask=tree_mask,
@@ -174,11 +178,16 @@ class PromptCache:
     def _store(self, k, v, rows, row_ptr, row_pos, most):
         """Rows of k and v into the slots after their prompt's last; how many of each."""
         torch = _torch()
-        self.used += min(rows.shape[0], most)
-        if self.used > self.cache.slots:
-            raise SiftError("PromptCache.append", 5, f"{self.used} slots, room for {self.cache.slots}")
         pages, page = self.pages, self.cache.page
         seq = torch.searchsorted(row_ptr, rows.int(), right=True) - 1
+        used = self.used + min(rows.shape[0], most)
+        if used > self.cache.slots:
+            # a bound that knows no prompt's own rows; the exact number, read from the device
+            used = int((pages.lens + torch.bincount(seq, minlength=self.cache.num_seqs)).max())
+            if used > self.cache.slots:
+                raise SiftError("PromptCache.append", 5,
+                                f"{used} slots, room for {self.cache.slots}")
+        self.used = used
         at = torch.arange(rows.shape[0], device=rows.device)
         slot = pages.lens[seq] + at - torch.searchsorted(seq, seq)
         to = pages.page_table[seq, slot // page].long() * page + slot % page

@@ -135,3 +135,39 @@ def test_refusals():
             for _ in range(40):
                 _, lse = c.step(q[:2], q[:2], q[:2])
                 c.append(q[:2], q[:2], q[:2], lse, torch.arange(2, device="cuda"))
+
+
+def test_room_counts_each_prompts_own_rows():
+    """Queries and answers fill their own prompt's slots: many prompts do not use up the
+    room of one."""
+    import torch
+    from paper_2606_09441_amd.serve import PromptCache
+    so, ps = [0], [0]
+    for _ in range(6):
+        so += [so[-1] + 64, so[-1] + 80]
+        ps.append(len(so) - 1)
+    x = torch.randn(so[-1], 2, 64, device="cuda").bfloat16()
+    with PromptCache(so, ps, 2, 2, 64, page=16, room=16, max_rows=4) as c:
+        c.prefill(x, x, x)
+        c.cut(64)
+        assert c.pages.lens.tolist() == [80] * 6
+        for _ in range(15):                      # a token of each of four rows is accepted
+            _, lse = c.step(x[:24], x[:24], x[:24])
+            c.append(x[:24], x[:24], x[:24], lse, torch.arange(0, 24, 4, device="cuda"))
+        assert c.pages.lens.tolist() == [95] * 6
+
+
+def test_order_of_the_calls():
+    import torch
+    from paper_2606_09441_amd import SiftError
+    from paper_2606_09441_amd.serve import PromptCache
+    x = torch.randn(40, 2, 64, device="cuda").bfloat16()
+    with PromptCache([0, 30, 40], [0, 2], 2, 2, 64, page=16, room=8, max_rows=2) as c:
+        for call in (lambda: c.cut(8), lambda: c.step(x[:1], x[:1], x[:1])):
+            with pytest.raises(SiftError) as e:
+                call()
+            assert e.value.status == 6
+        c.prefill(x, x, x)
+        with pytest.raises(SiftError) as e:
+            c.prefill(x, x, x)
+        assert e.value.status == 6
