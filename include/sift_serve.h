@@ -58,8 +58,8 @@ typedef enum sift_mask {
  * sums are fp32.
  * out and lse overlap no input.
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (mask, cap, dtypes,
- *   alignment, more than 2^17 kv heads), SIFT_E_PLAN (another device is current), SIFT_E_CAPACITY (2^24
- *   workgroups of 128 rows of a head or more), SIFT_E_HIP.
+ *   alignment, more than 2^17 kv heads), SIFT_E_PLAN (another device is current),
+ *   SIFT_E_CAPACITY (2^24 workgroups of 128 rows of a head or more), SIFT_E_HIP.
  */
 sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_tensor* k,
                             const sift_tensor* v, int32_t mask, const sift_score* score,
@@ -137,9 +137,10 @@ sift_status sift_cache_destroy(sift_cache* cache);
  * influence on it.  Rows that row_ptr leaves out are not written.  Results
  * depend on nothing but the arguments (no atomics).
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, alignment,
- *   cap), SIFT_E_CAPACITY (mask_words; 2^24 rows x heads or more; more
- *   than 2^31 steps of 128 keys of 32 rows in all), SIFT_E_PLAN
- *   (another device is current), SIFT_E_HIP.
+ *   cap), SIFT_E_CAPACITY (mask_words; 2^24 rows x heads or more; 2^31 steps of 128
+ *   keys of 32 rows of a kv head or more, were all sequences as long and as many new
+ *   tokens as the handle and q allow), SIFT_E_PLAN (another device is current),
+ *   SIFT_E_HIP.
  */
 sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
                                  const sift_cache_rows* new_rows, const sift_tensor* q,

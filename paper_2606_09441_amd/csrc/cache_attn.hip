@@ -299,12 +299,15 @@ bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys) {
 }
 
 int64_t cache_attn_steps(const CacheArgs& a) {
-  // of the narrow units: the wide ones are a quarter as many, of twice the steps
-  const int64_t units =
-      a.hkv * (static_cast<int64_t>(a.rows) * (a.hq / a.hkv) / kRows + a.num_seqs);
-  const int64_t keys = (static_cast<int64_t>(a.max_pages) << a.page_shift) +
-                       std::min(a.rows, a.max_rows) + 2 * kTileKeys;
-  return units * (keys / (kTileKeys * kStepTiles) + 1);
+  // as if every sequence had the most rows, which row pointers may say whatever they
+  // add up to; of the narrow units: the wide ones are no more, and take twice the steps
+  // where there are half as many
+  const int64_t rows = std::min(a.rows, a.max_rows);
+  const int64_t units = static_cast<int64_t>(a.num_seqs) * a.hkv *
+                        ((rows * (a.hq / a.hkv) + kRows - 1) / kRows);
+  const int64_t keys = (static_cast<int64_t>(a.max_pages) << a.page_shift) + rows + 4 * kTileKeys;
+  const int64_t steps = keys / (kTileKeys * kStepTiles) + 1;
+  return units >= int64_t(1) << 31 ? units : units * steps;
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream) {

@@ -237,3 +237,20 @@ def test_refusals():
         refused(2, f, x.q, x.k_new, x.v_new, other)
     refused(4, CachePages, x.k, x.v, x.t["table"].long(), x.t["lens"])
     refused(1, CachePages, x.k, x.v, None, x.t["lens"])
+
+
+def test_more_steps_than_the_split_counts():
+    """Row pointers may give every sequence the most rows, whatever they add up to."""
+    import torch
+    from paper_2606_09441_amd import Cache, CachePages, SiftError
+    dev = torch.device("cuda")
+    seqs, pages, rows = 64, 8192, 2048
+    pool = torch.zeros(128, 1, 64, dtype=torch.bfloat16, device=dev)
+    ints = dict(dtype=torch.int32, device=dev)
+    kv = CachePages(pool, pool.clone(), torch.zeros(seqs, pages, **ints), torch.zeros(seqs, **ints))
+    new = torch.zeros(rows, 1, 64, dtype=torch.bfloat16, device=dev)
+    with Cache(seqs, 64, 1, 64, page=128, max_pages=pages, max_rows=rows) as cache:
+        with pytest.raises(SiftError) as e:
+            cache.attention(new.expand(-1, 64, -1).contiguous(), new, new, kv,
+                            row_ptr=torch.zeros(seqs + 1, **ints))
+    assert e.value.status == 5
