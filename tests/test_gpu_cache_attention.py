@@ -254,3 +254,34 @@ def test_more_steps_than_the_split_counts():
             cache.attention(new.expand(-1, 64, -1).contiguous(), new, new, kv,
                             row_ptr=torch.zeros(seqs + 1, **ints))
     assert e.value.status == 5
+
+
+# so many rows times slots that bf16 goes by the units of 128 rows, and so many steps
+# that a workgroup has runs of several, which end inside units
+WIDE = ([9000, 300, 0], [100, 40, 3])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tree,gaps,moved,cap,bias", [
+    (None, False, False, 0.0, False), (random_tree, True, False, 0.0, False),
+    (some_empty, False, False, 30.0, False), (random_tree, False, True, 0.0, True),
+    (None, True, True, 20.0, True)])
+def test_many_rows_over_long_caches(d, tree, gaps, moved, cap, bias):
+    x = Batch(*WIDE, 8, 1, d, "bf16", 128, gaps, moved, tree, seed=16, extra_pages=16)
+    assert x.max_rows * 8 * x.B * x.slots >= 24 << 20
+    check(x, cap, bias)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_unseen_new_tokens_of_many_rows(value):
+    x = Batch(*WIDE, 8, 1, 64, "bf16", 128, tree=random_tree, seed=17, extra_pages=16)
+    x.v_new[20, 0, 5:9] = value
+    x.v_new[100 + 30, 0, 40] = value
+    with x.cache() as cache:
+        out = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"],
+                              tree_mask=x.mask).float().cpu().numpy()
+    with np.errstate(all="ignore"):
+        ref, _ = x.oracle()
+    fine = np.isfinite(ref)
+    assert np.array_equal(fine, np.isfinite(out))
+    assert max_abs(out[fine], ref[fine]) <= TOL["bf16"]
