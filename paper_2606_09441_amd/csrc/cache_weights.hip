@@ -46,7 +46,8 @@ struct KeyCost {
 };
 
 template <typename T, int D, bool kDma>
-__global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) void cache_weights_kernel(CacheWeightArgs p) {
+__global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) void
+cache_weights_kernel(CacheWeightArgs p) {
   using G = Tile<T, D>;
   constexpr bool kLog2 = G::kBf16;
   constexpr float kUnit = kLog2 ? kLog2e : 1.f;
