@@ -243,3 +243,42 @@ def test_offsets_beyond_32_bits():
                            mask="document", cap=50.0)
     torch.cuda.synchronize()
     assert torch.equal(out[a:], alone)
+
+
+def lse_error(lse, ref):
+    """Largest error of log sums, |slope| * distance in fp32 among their terms
+    (relative 2^-23)."""
+    return np.max(np.abs(lse - ref) / np.maximum(1.0, np.abs(ref) / 30))
+
+
+@pytest.mark.parametrize("cap", [0.0, 300.0])
+@pytest.mark.parametrize("mask", ["causal", "document", "prefix"])
+@pytest.mark.parametrize("slope", [2.0, 4.0, -3.0])
+def test_bias_beside_widely_spread_products(slope, mask, cap):
+    """Scores of standard deviation 9 (36 for some keys) under slopes that no key's
+    neighbours share: the largest product and the largest bias of a tile are of
+    different keys, hundreds apart."""
+    for d in (64, 128):
+        out, lse, ref, ref_lse = run([[150, 300, 77], [130, 5]], 40, 8, d, "bf16", mask, cap, True,
+                                     scale=9 * d ** -0.5, by_head=True, slope=slope)
+        say(f"slope {slope} {mask} cap {cap} {d}: {max_abs(out, ref):.2e}, {lse_error(lse, ref_lse):.2e}")
+        assert max_abs(out, ref) <= TOL["bf16"] and lse_error(lse, ref_lse) <= LSE_TOL
+
+
+@pytest.mark.parametrize("slope,score", [(1.5, 90.0), (2.0, 100.0), (2.0, 120.0), (-1.5, 90.0)])
+def test_a_far_key_with_a_large_score(slope, score):
+    """It is the largest product of a tile whose nearest key has the largest bias."""
+    import torch
+    from paper_2606_09441_amd import Plan
+    so, ps = layout([[300, 20]])
+    n, hq, hkv, d = so[-1], 128, 8, 64
+    (q, k, v), _ = inputs(n, hq, hkv, d, "bf16", 5)
+    unit = q[256].view(hkv, hq // hkv, d)[:, 0].float()
+    k[192] = (unit * (score * d ** 0.5 / (unit * unit).sum(1, keepdim=True))).to(k.dtype)
+    slopes = torch.full((hq,), slope, device=q.device)
+    lse = torch.empty(n, hq, device=q.device)
+    with Plan(so, ps, hq, hkv, d, 64) as plan:
+        out = plan.dense(q, k, v, slopes=slopes, lse=lse)
+    f = lambda x: x.float().cpu().numpy()  # noqa: E731
+    ref, ref_lse = S.dense_by_head(f(q), f(k), f(v), so, ps, "causal", None, 0.0, f(slopes))
+    assert max_abs(f(out), ref) <= TOL["bf16"] and lse_error(f(lse), ref_lse) <= LSE_TOL
