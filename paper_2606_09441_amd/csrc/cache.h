@@ -2,6 +2,7 @@
 // lie, and the even split of all sequences' work over a launch.
 #pragma once
 
+#include "clamp.h"
 #include "flash.h"
 
 namespace sift {
@@ -25,13 +26,13 @@ struct Seq {
 // (any lane may ask for its own b)
 __device__ __forceinline__ Seq sequence(const CacheArgs& a, int b) {
   Seq s;
-  s.len = min(max(a.lens[b], 0), a.max_pages << a.page_shift);
+  s.len = within(a.lens[b], a.max_pages << a.page_shift);
   if (a.row_ptr == nullptr) {
     s.n = a.rows / a.num_seqs;
     s.row0 = b * s.n;
   } else {
-    s.row0 = min(max(a.row_ptr[b], 0), a.rows);
-    s.n = max(min(min(a.row_ptr[b + 1], a.rows) - s.row0, a.max_rows), 0);
+    s.row0 = within(a.row_ptr[b], a.rows);
+    s.n = rows_between(s.row0, a.row_ptr[b + 1], a.rows, a.max_rows);
   }
   return s;
 }
@@ -195,10 +196,10 @@ __device__ __forceinline__ Rows16 cached_rows(const CacheArgs& a, int b, int len
   const int pi = min(slot >> a.page_shift, a.max_pages - 1);
   const int in = slot & ((1 << a.page_shift) - 1);
   const int64_t at = static_cast<int64_t>(b) * a.max_pages + pi;
-  int n = len - slot;
-  if (a.page_lens != nullptr) n = min(n, scalar(a.page_lens, at) - in);
-  const int page = min(max(scalar(a.table, at), 0), a.num_pages - 1);
-  return Rows16{(static_cast<int64_t>(page) << a.page_shift) + in, min(max(n, 0), 16)};
+  const int n = a.page_lens != nullptr ? keys_of_page(scalar(a.page_lens, at), in, len - slot)
+                                       : within(len - slot, 16);
+  const int page = within(scalar(a.table, at), a.num_pages - 1);
+  return Rows16{(static_cast<int64_t>(page) << a.page_shift) + in, n};
 }
 
 }  // namespace cache

@@ -285,3 +285,25 @@ def test_unseen_new_tokens_of_many_rows(value):
     fine = np.isfinite(ref)
     assert np.array_equal(fine, np.isfinite(out))
     assert max_abs(out[fine], ref[fine]) <= TOL["bf16"]
+
+
+@pytest.mark.parametrize("end", [-2 ** 31, -1, 2 ** 31 - 1])
+def test_row_pointers_out_of_range(end):
+    """They give a sequence no rows that the buffers do not have: rows past the last
+    are not written, the other sequence's are its own."""
+    import torch
+    x = Batch([50, 60], [0, 4], 4, 2, 64, "bf16", seed=23)
+    out = torch.full((12, 4, 64), 7.0, dtype=x.dtype, device=x.q.device)
+    lse = torch.full((12, 4), 7.0, device=x.q.device)
+    ptr = torch.tensor([3, end, 4], dtype=torch.int32, device=x.q.device)
+    with x.cache() as cache:
+        want = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"])
+        cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=ptr, out=out[:4], lse=lse[:4])
+        torch.cuda.synchronize()
+        assert bool((out[4:] == 7).all()) and bool((lse[4:] == 7).all())
+        if end < 0:      # (else row 3 is the first one's, and the second has none)
+            assert torch.equal(out[:4], want)
+        w = cache.accumulate(x.q, lse[:4], x.pages(), row_ptr=ptr)
+        torch.cuda.synchronize()
+        if end < 0:
+            assert not bool(w[0].any())
