@@ -342,9 +342,11 @@ __global__ __launch_bounds__(64 * kPickWaves) void cache_pick_kernel(CacheEvictA
     if (part == 0)
       for (int i = threadIdx.x; i < 1024 + 2048; i += 64 * kPickWaves) hist_of(p, head, 0)[i] = 0;
   } else {
-    // of the units before this one, and of all
+    // of the units before this one, and of all that the sequence reaches (with those of
+    // its capacity the time would grow as the square of that)
     int k0 = 0, t0 = 0, k1 = 0, t1 = 0, all_k1 = 0, all_t0 = 0, all_t = 0;
-    for (int u = lane; u < units; u += 64) {
+    const int reached = x.len / kUnitSlots + 1;
+    for (int u = lane; u < min(units, reached); u += 64) {
       const int4 n = counts[u];
       if (u < unit) {
         k0 += n.x;
@@ -402,7 +404,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheEvictArgs p, int p
   const int n = p.num_moves[head];
   const int b = static_cast<int>(head / a.hkv), kvh = static_cast<int>(head % a.hkv);
   const int64_t at0 = head * slots;
-  for (int i = p.lens_out[b] + first * 256 + threadIdx.x; i < slots; i += per_head * 256) {
+  // (64 bits: a step from the last slots passes 2^31)
+  for (int64_t i = p.lens_out[b] + first * 256 + threadIdx.x; i < slots; i += per_head * 256) {
     p.weights_out[at0 + i] = 0.f;
     p.pos_out[at0 + i] = -1;
   }

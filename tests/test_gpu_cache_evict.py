@@ -155,3 +155,33 @@ def test_refusals():
         refused(4, kv, w, 10, pos_out=kv.key_pos)
         refused(4, kv, w, 10, lens_out=kv.lens)
         refused(5, kv, w, 10, next_pos=kv.lens[:1])
+
+
+def test_as_many_slots_as_a_cache_can_have():
+    """Slots near 2^31, whose index a step of the clearing loop passes: all past the
+    kept ones are cleared, and nothing outside."""
+    import torch
+    from paper_2606_09441_amd import Cache, CachePages
+    dev = torch.device("cuda")
+    max_pages, guard = (1 << 24) - 2, 1 << 20
+    slots = max_pages * 128
+    pool = torch.randn(8 * 128, 1, 64, device=dev).bfloat16()
+    table = torch.zeros(1, max_pages, dtype=torch.int32, device=dev)
+    table[0, :8] = torch.arange(8)
+    kv = CachePages(pool, pool.clone(), table, torch.tensor([300], dtype=torch.int32, device=dev))
+    w = torch.zeros(slots, device=dev)
+    w[:300] = torch.arange(300, device=dev)
+    weights = torch.full((slots + 2 * guard,), 7.0, device=dev)
+    pos = torch.full((slots + 2 * guard,), 7, dtype=torch.int32, device=dev)
+    inner = slice(guard, guard + slots)
+    with Cache(1, 1, 1, 64, page=128, max_pages=max_pages) as cache:
+        for budget, n in ((1 << 20, 300), (100, 100)):
+            _, _, lens = cache.evict(kv, w, budget, weights_out=weights[inner], pos_out=pos[inner])
+            torch.cuda.synchronize()
+            assert lens.tolist() == [n]
+            assert sorted(pos[inner][:n].tolist()) == list(range(300 - n, 300))
+            for t, none in ((weights, 0), (pos, -1)):
+                at = torch.cat([t[:guard], t[-guard:]])
+                assert bool((at == 7).all())
+                for a in range(n, slots, 1 << 28):
+                    assert bool((t[inner][a:a + (1 << 28)] == none).all())
