@@ -247,7 +247,7 @@ cache_weights_kernel(CacheWeightArgs p) {
           return __builtin_amdgcn_exp2f(kLog2 ? x : x * kLog2e);
         };
         // The sum of a block's weights, rows that count for nothing left out,
-        // whatever the key holds.
+        // whatever the key holds (a log sum that is no number is none of these).
         const auto careful = [&](int rb, const f32x16& sc, const f32x4(&l)[4]) {
           float part[2] = {0.f, 0.f};
 #pragma unroll
@@ -256,7 +256,7 @@ cache_weights_kernel(CacheWeightArgs p) {
 #pragma unroll
             for (int v = 4 * j; v < 4 * j + 4; ++v) {
               const float w = weight(sc, l, v);
-              part[v & 1] += l[j][v & 3] < INFINITY ? w : 0.f;
+              part[v & 1] += l[j][v & 3] == INFINITY ? 0.f : w;
             }
           }
           return part[0] + part[1];

@@ -181,3 +181,24 @@ def test_refusals():
         refused(4, x.q, lse, kv, w, out=w.int())
         refused(2, x.q[:3], lse, kv, w)
         refused(4, x.q, lse, kv, w, cap=-1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 40, 300, 320])
+def test_a_log_sum_that_is_no_number(dtype, rows):
+    """Every weight it is part of is none either, however the rows are dealt out; where
+    the row counts for nothing, none is."""
+    import torch
+    x = Batch([80, 50], [rows, 2], 2, 2, 64, dtype, seed=18)
+    lse = torch.full((x.rows, 2), 5.0, device=x.q.device)
+    lse[rows - 1] = float("nan")
+    ones = torch.ones(x.rows, device=x.q.device)
+    some = ones.clone()
+    some[0] = 0.0 if rows > 1 else 1.0
+    without = ones.clone()
+    without[rows - 1] = 0.0
+    with x.cache() as cache:
+        for rw, number in ((None, False), (ones, False), (some, False), (without, True)):
+            w = cache.accumulate(x.q, lse, x.pages(), row_ptr=x.t["row_ptr"], row_weight=rw)
+            assert torch.isfinite(w[0, :, :80]).unique().tolist() == [number]
+            assert bool(torch.isfinite(w[1, :, :50]).all())
