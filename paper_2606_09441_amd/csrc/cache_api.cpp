@@ -240,8 +240,7 @@ sift_status sift_cache_accumulate(sift_cache* cache, const sift_cache_kv* kv,
   sift_status st;
   if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
   const int32_t dtype = kv->k_pages->dtype;
-  const double unit = dtype == SIFT_BF16 ? sift::kUnitLog2e : 1.0;
-  if ((st = check_rows(cache, new_rows, q, dtype, score, unit, &a.c)) != SIFT_OK) return st;
+  if ((st = check_rows(cache, new_rows, q, dtype, score, 1.0, &a.c)) != SIFT_OK) return st;
   if (out == nullptr || (lse == nullptr && q->tokens > 0)) return SIFT_E_NULL;
   if (!std::isfinite(decay)) return SIFT_E_UNSUPPORTED;
   if (sift::cache_weights_steps(a.c) >= int64_t(1) << 31) return SIFT_E_CAPACITY;

@@ -12,14 +12,15 @@
 //  * Few rows (one block or two): HBM bounds it.  K comes by DMA through LDS of
 //    the wavefront's own, whole lines at a time, the next tile as soon as the
 //    present one is in registers.
-//  * Many rows: their Q takes that LDS, the VALU (four instructions and an
-//    exponential a score) bounds it, and K goes straight to registers.
+//  * Many rows: their Q takes that LDS, and K goes straight to registers.  A score
+//    costs the VALU an FMA, a product, an exponential and a sum.
 //
-// fp32: the exponent is formed as scale * q.k - lse in the natural domain and only
-// then multiplied by log2(e): the two are large and nearly equal for the keys
-// that count, and their difference is exact there.  bf16: both are in the log2
-// domain, an instruction less; lse's rounding there (2^-24 of it) is far below a
-// bf16 score's.
+// The exponent is formed as scale * q.k - lse in the natural domain and only then
+// multiplied by log2(e): the two are large and nearly equal for the keys that count,
+// and their difference is exact there, also for bf16, whose products are exact in
+// fp32.  In the log2 domain, an instruction a score less (384 rows of 66048 keys, 8 kv
+// heads, D = 128: 84 us instead of 88), rounding lse and the scale put up to 5e-6 on
+// the weights of scores near 120, ten times what remains.
 
 #include <algorithm>
 
@@ -49,8 +50,6 @@ template <typename T, int D, bool kDma>
 __global__ __launch_bounds__(64 * kWaves, kDma && sizeof(T) * D <= 256 ? 4 : 2) void
 cache_weights_kernel(CacheWeightArgs p) {
   using G = Tile<T, D>;
-  constexpr bool kLog2 = G::kBf16;
-  constexpr float kUnit = kLog2 ? kLog2e : 1.f;
   // LDS of a wavefront's keys: a tile of them, or as many rows as fit in 4 KB
   constexpr int kTurn = kDma ? 32 : 4096 / G::kRow < 32 ? 4096 / G::kRow : 32;
   constexpr int kKeys = kTurn * G::kRow;
@@ -166,9 +165,9 @@ cache_weights_kernel(CacheWeightArgs p) {
         if (i < cn) {
           const float f = p.row_weight != nullptr ? p.row_weight[tok] : 1.f;
           const float y = p.lse[static_cast<int64_t>(tok) * a.hq + h];
-          if (f != 0.f && y != -INFINITY) l = (f == 1.f ? y : y - logf(f)) * kUnit;
+          if (f != 0.f && y != -INFINITY) l = f == 1.f ? y : y - logf(f);
           if (bias) {
-            slope = a.sc.slopes[h] * kUnit;
+            slope = a.sc.slopes[h];
             pos = a.row_pos != nullptr ? a.row_pos[tok] : len + r / g;
           }
         }
@@ -243,8 +242,7 @@ cache_weights_kernel(CacheWeightArgs p) {
                 static_cast<size_t>(lse0 + 4 * (32 * rb + 8 * j + 4 * hf)));
         };
         const auto weight = [&](const f32x16& sc, const f32x4(&l)[4], int v) {
-          const float x = fmaf(sc[v], cc, -l[v >> 2][v & 3]);
-          return __builtin_amdgcn_exp2f(kLog2 ? x : x * kLog2e);
+          return __builtin_amdgcn_exp2f(fmaf(sc[v], cc, -l[v >> 2][v & 3]) * kLog2e);
         };
         // The sum of a block's weights, rows that count for nothing left out,
         // whatever the key holds (a log sum that is no number is none of these).

@@ -480,8 +480,7 @@ int64_t cache_attn_steps(const CacheArgs& a);
 hipError_t launch_cache_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream);
 
-// Accumulated attention weights (cache_weights.hip); c.sc in the log2 domain for bf16,
-// in the natural one for fp32.
+// Accumulated attention weights (cache_weights.hip); c.sc in the natural domain.
 struct CacheWeightArgs {
   CacheArgs c;
   const float* lse;          // [rows][hq]

@@ -202,3 +202,29 @@ def test_a_log_sum_that_is_no_number(dtype, rows):
             w = cache.accumulate(x.q, lse, x.pages(), row_ptr=x.t["row_ptr"], row_weight=rw)
             assert torch.isfinite(w[0, :, :80]).unique().tolist() == [number]
             assert bool(torch.isfinite(w[1, :, :50]).all())
+
+
+@pytest.mark.parametrize("dtype,d", TYPES)
+@pytest.mark.parametrize("rows", [1, 8, 300])
+def test_scores_near_the_log_sum_keep_their_bits(dtype, d, rows):
+    """Scores that fp32 holds exactly (one product each), all large and near the log
+    sum of the one row that counts: their difference x is rounded once, its product
+    with log2(e) once more and the exponential to its last bit, 2^-22 (1 + |x|) in
+    all.  Rounding log sum or score in another unit would cost 2^-24 of 120."""
+    import torch
+    x = Batch([200], [rows], 4, 4, d, dtype, seed=19)
+    rng = np.random.default_rng(20)
+    x.q.zero_()
+    x.k.zero_()
+    x.q[:, :, 0] = 8.0
+    s = 112.0 + 0.5 * rng.integers(0, 16, tuple(x.k.shape[:2]))
+    x.k[:, :, 0] = torch.from_numpy(s).to(x.k)
+    lse = np.full((rows, 4), 1e4, np.float32)        # weights of 0
+    lse[rows // 2] = rng.uniform(119.0, 121.0, 4)
+    with x.cache() as cache:
+        w = cache.accumulate(x.q, torch.from_numpy(lse).to(x.q.device), x.pages(), scale=0.125)
+    p = x.host()
+    e = p.k[p.rows(0, np.arange(200)), :, 0].astype(np.float64).T - lse[rows // 2][:, None].astype(np.float64)
+    rel = np.abs(w[0, :, :200].cpu().numpy() / np.exp(e) - 1)
+    say(f"{dtype} {d} {rows}: {rel.max():.2e}, of the bound {(rel / (2.0 ** -22 * (1 + np.abs(e)))).max():.2f}")
+    assert (rel <= 2.0 ** -22 * (1 + np.abs(e))).all()
