@@ -20,9 +20,15 @@ extern "C" {
  * softmax_scale * (q . k), a score is s = cap * tanh(z / cap) (z itself where
  * cap is 0), less slopes[h] * |position of the query - position of the key|
  * where slopes are given.
- *   softmax_scale  <= 0 selects 1/sqrt(D)
- *   cap            0 for none; negative, NaN or beyond 1e15: SIFT_E_UNSUPPORTED
- *   slopes         device float [Hq], or NULL; positions are exact up to 2^24
+ *   softmax_scale  <= 0 selects 1/sqrt(D); one that is not a float any more times
+ *                  log2(e): SIFT_E_UNSUPPORTED
+ *   cap            0 for none; negative, NaN or beyond 1e15: SIFT_E_UNSUPPORTED, and
+ *                  so are caps too small or too large beside the scale: scale / cap
+ *                  has to be a normal float and scale (scale / cap)^8 a finite one
+ *                  (at the scale of D = 128 caps from 1e-6 on).  q . k beyond 1e19
+ *                  has no defined score under a cap.
+ *   slopes         device float [Hq], or NULL; positions are exact up to 2^24, and
+ *                  |slope| * distance stays below 1e17
  * A NULL score is the default scale alone.
  */
 typedef struct sift_score {

@@ -25,6 +25,7 @@ inline sift_status make_score(const sift_score* score, int32_t head_dim, double 
   for (float& a : out->a) a = 0.f;
   for (float& b : out->b) b = 0.f;
   out->slopes = s.slopes;
+  if (!std::isfinite(out->c)) return SIFT_E_UNSUPPORTED;
   if (s.cap == 0.f) return SIFT_OK;
   const double x = scale / static_cast<double>(s.cap);
   out->x = static_cast<float>(x);
@@ -36,6 +37,11 @@ inline sift_status make_score(const sift_score* score, int32_t head_dim, double 
   }
   // a factor that fp32 does not hold, or holds as a denormal, would be a cap of another value
   if (!std::isnormal(out->x) || !std::isnormal(out->cap2)) return SIFT_E_UNSUPPORTED;
+  // and an infinite coefficient makes a score of 0 none at all
+  for (float a : out->a)
+    if (!std::isfinite(a)) return SIFT_E_UNSUPPORTED;
+  for (float b : out->b)
+    if (!std::isfinite(b)) return SIFT_E_UNSUPPORTED;
   return SIFT_OK;
 }
 

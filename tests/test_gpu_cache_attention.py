@@ -307,3 +307,17 @@ def test_row_pointers_out_of_range(end):
         torch.cuda.synchronize()
         if end < 0:
             assert not bool(w[0].any())
+
+
+def test_scales_and_caps_that_fp32_does_not_hold():
+    import torch
+    from paper_2606_09441_amd import SiftError
+    x = Batch([100, 30], [2, 2], 4, 2, 128, "bf16", seed=14)
+    lse = torch.zeros(4, 4, device=x.q.device)
+    with x.cache() as cache:
+        for kw in (dict(cap=2e-7), dict(cap=1e-20), dict(scale=3.4e38, cap=1.0), dict(scale=1e30, cap=1.0)):
+            for call in (lambda: cache.attention(x.q, x.k_new, x.v_new, x.pages(), **kw),
+                         lambda: cache.accumulate(x.q, lse, x.pages(), **kw)):
+                with pytest.raises(SiftError) as e:
+                    call()
+                assert e.value.status == 4

@@ -282,3 +282,23 @@ def test_a_far_key_with_a_large_score(slope, score):
     f = lambda x: x.float().cpu().numpy()  # noqa: E731
     ref, ref_lse = S.dense_by_head(f(q), f(k), f(v), so, ps, "causal", None, 0.0, f(slopes))
     assert max_abs(f(out), ref) <= TOL["bf16"] and lse_error(f(lse), ref_lse) <= LSE_TOL
+
+
+def test_scales_and_caps_that_fp32_does_not_hold():
+    """Their coefficients would be infinite, and a score of 0 no number."""
+    import torch
+    from paper_2606_09441_amd import Plan, SiftError
+    so, ps = layout([[40, 10]])
+    (q, k, v), (qn, kn, vn) = inputs(50, 2, 1, 128, "f32")
+    q[:, 0], qn[:, 0] = 0, 0
+    with Plan(so, ps, 2, 1, 128, 64) as plan:
+        for kw in (dict(cap=5e-7), dict(cap=1e-20), dict(scale=3e38), dict(scale=1e30, cap=1.0)):
+            with pytest.raises(SiftError) as e:
+                plan.dense(q, k, v, **kw)
+            assert e.value.status == 4
+        for kw in (dict(cap=1e-6), dict(cap=1e15), dict(scale=1e30)):
+            out = plan.dense(q, k, v, **kw).cpu().numpy()
+            ref = S.dense(qn, kn, vn, so, ps, "causal", **kw)[0]
+            assert max_abs(out[:, 0], ref[:, 0]) <= TOL["f32"]
+            if "cap" in kw:
+                assert max_abs(out, ref) <= TOL["f32"]
