@@ -151,6 +151,8 @@ class PromptCache:
         """Takes a step's accepted rows (int64, ascending; those of a prompt follow each
         other in the answer) into the cache, and their weights into the keys'."""
         torch = _torch()
+        if self.weights is None or self._pending is not None:
+            raise SiftError("PromptCache.append", 6, "the prompts' caches are not cut yet")
         ptr = self._pointers(q.shape[0], row_ptr)
         pos = self._positions(q.shape[0], row_ptr, row_pos)
         counts = torch.zeros(q.shape[0], device=q.device).index_fill_(0, rows, 1.0)

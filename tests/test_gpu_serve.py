@@ -171,3 +171,21 @@ def test_order_of_the_calls():
         with pytest.raises(SiftError) as e:
             c.prefill(x, x, x)
         assert e.value.status == 6
+
+
+def test_answers_follow_the_first_cut():
+    """A row taken in before it would lie behind a document's last page, where nothing
+    sees it."""
+    import torch
+    from paper_2606_09441_amd import SiftError
+    from paper_2606_09441_amd.serve import PromptCache
+    x = torch.randn(40, 2, 64, device="cuda").bfloat16()
+    lse, rows = torch.zeros(2, 2, device="cuda"), torch.arange(2, device="cuda")
+    with PromptCache([0, 30, 40], [0, 2], 2, 2, 64, page=16, room=8, max_rows=2) as c:
+        for prefilled in (False, True):
+            with pytest.raises(SiftError) as e:
+                c.append(x[:2], x[:2], x[:2], lse, rows)
+            assert e.value.status == 6
+            if not prefilled:
+                c.prefill(x, x, x)
+        assert c.pages.lens.tolist() == [30] and c.next_pos.tolist() == [40]
