@@ -133,7 +133,8 @@ class PromptCache:
             k, v = self._pending
             self._pending = None
             rows = _torch().arange(k.shape[0], device=k.device)
-            self._store(k, v, rows, self._query_ptr, self._query_pos, self.longest)
+            seq, used = self._room("PromptCache.cut", k, v, rows, self._query_ptr, self.longest)
+            self._store(k, v, rows, seq, used, self._query_pos)
 
     def step(self, q, k_new, v_new, row_ptr=None, tree_mask=None, row_pos=None):
         """(out, lse) of new tokens over the cache and each other; row_pos None: each
@@ -155,10 +156,12 @@ class PromptCache:
             raise SiftError("PromptCache.append", 6, "the prompts' caches are not cut yet")
         ptr = self._pointers(q.shape[0], row_ptr)
         pos = self._positions(q.shape[0], row_ptr, row_pos)
+        # whatever may be refused comes before the weights and the pages change
+        seq, used = self._room("PromptCache.append", k_new, v_new, rows, ptr, self.max_rows)
         counts = torch.zeros(q.shape[0], device=q.device).index_fill_(0, rows, 1.0)
         self.cache.accumulate(q, lse, self.pages, self.weights, decay, row_ptr=row_ptr, row_pos=pos,
                               row_weight=counts, **self._score)
-        added = self._store(k_new, v_new, rows, ptr, pos, self.max_rows)
+        added = self._store(k_new, v_new, rows, seq, used, pos)
         self.next_pos = self.next_pos + added
 
     def _pointers(self, rows, row_ptr):
@@ -177,18 +180,26 @@ class PromptCache:
         seq = torch.searchsorted(ptr, row, right=True).clamp_(max=self.cache.num_seqs) - 1
         return (self.next_pos[seq] + row - ptr[seq]).int()
 
-    def _store(self, k, v, rows, row_ptr, row_pos, most):
-        """Rows of k and v into the slots after their prompt's last; how many of each."""
+    def _room(self, fn, k, v, rows, row_ptr, most):
+        """The prompts of rows of k and v, and how many slots one has with them at most."""
         torch = _torch()
-        pages, page = self.pages, self.cache.page
+        pages = self.pages
+        for name, x in (("k", k), ("v", v)):
+            if x.shape[1:] != pages.k_pages.shape[1:] or x.dtype != pages.k_pages.dtype:
+                raise SiftError(fn, 2, f"{name} holds {tuple(x.shape)} {x.dtype}")
         seq = torch.searchsorted(row_ptr, rows.int(), right=True) - 1
         used = self.used + min(rows.shape[0], most)
         if used > self.cache.slots:
             # a bound that knows no prompt's own rows; the exact number, read from the device
             used = int((pages.lens + torch.bincount(seq, minlength=self.cache.num_seqs)).max())
             if used > self.cache.slots:
-                raise SiftError("PromptCache.append", 5,
-                                f"{used} slots, room for {self.cache.slots}")
+                raise SiftError(fn, 5, f"{used} slots, room for {self.cache.slots}")
+        return seq, used
+
+    def _store(self, k, v, rows, seq, used, row_pos):
+        """Rows of k and v into the slots after their prompt's last; how many of each."""
+        torch = _torch()
+        pages, page = self.pages, self.cache.page
         self.used = used
         at = torch.arange(rows.shape[0], device=rows.device)
         slot = pages.lens[seq] + at - torch.searchsorted(seq, seq)

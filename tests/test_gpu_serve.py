@@ -189,3 +189,61 @@ def test_answers_follow_the_first_cut():
             if not prefilled:
                 c.prefill(x, x, x)
         assert c.pages.lens.tolist() == [30] and c.next_pos.tolist() == [40]
+
+
+def test_a_refused_append_changes_nothing():
+    """It can be made again after a cut, and then gives what it would have given."""
+    import torch
+    from paper_2606_09441_amd import SiftError
+    from paper_2606_09441_amd.serve import PromptCache
+    gen = torch.Generator("cuda").manual_seed(4)
+    draw = lambda n: torch.randn(n, 2, 64, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    rows = torch.arange(2, device="cuda")
+    x, steps = draw(40), [draw(2) for _ in range(30)]
+    state = lambda c: [t.clone() for t in (c.weights, c.pages.lens, c.pages.key_pos, c.next_pos,  # noqa: E731
+                                           c.pages.k_pages, c.pages.v_pages)] + [c.used]
+    same = lambda a, b: all(torch.equal(s, t) for s, t in zip(a[:-1], b[:-1])) and a[-1] == b[-1]  # noqa: E731
+
+    def run(cut_at):
+        """The states after each step; cuts before step cut_at, or where a step is refused."""
+        after, refused = [], None
+        with PromptCache([0, 30, 40], [0, 2], 2, 2, 64, page=16, room=8, max_rows=2) as c:
+            c.prefill(x, x, x)
+            c.cut(100)
+            for i, q in enumerate(steps[:16]):
+                _, lse = c.step(q, q, q)
+                if i == cut_at:
+                    c.cut(20)
+                before = state(c)
+                try:
+                    c.append(q, q, q, lse, rows, decay=0.5)
+                except SiftError as e:
+                    assert e.status == 5 and refused is None and same(before, state(c))
+                    refused = i
+                    c.cut(20)
+                    c.append(q, q, q, lse, rows, decay=0.5)
+                after.append(state(c))
+        return after, refused
+
+    first, at = run(None)
+    assert at is not None
+    again, none = run(at)
+    assert none is None
+    assert all(same(a, b) for a, b in zip(first, again))
+
+
+def test_append_checks_its_rows_first():
+    import torch
+    from paper_2606_09441_amd import SiftError
+    from paper_2606_09441_amd.serve import PromptCache
+    x = torch.randn(40, 2, 64, device="cuda").bfloat16()
+    rows = torch.arange(2, device="cuda")
+    with PromptCache([0, 30, 40], [0, 2], 2, 2, 64, page=16, room=8, max_rows=2) as c:
+        c.prefill(x, x, x)
+        c.cut(100)
+        _, lse = c.step(x[:2], x[:2], x[:2])
+        before = c.weights.clone()
+        for k, v in ((x[:2].float(), x[:2]), (x[:2], x[:2, :1])):
+            with pytest.raises(SiftError) as e:
+                c.append(x[:2], k, v, lse, rows)
+            assert e.value.status == 2 and torch.equal(before, c.weights)
