@@ -73,6 +73,7 @@ class PromptCache:
         for b in range(seqs):
             first.append(first[-1] + so[ps[b + 1]] - so[ps[b + 1] - 1])
         self._query, self._query_ptr = torch.tensor(query, device=dev), ints(first)
+        self._query_rows = first
         self._query_pos = ints([t - so[ps[b]] for b in range(seqs)
                                 for t in range(so[ps[b + 1] - 1], so[ps[b + 1]])])
         self.next_pos = ints([so[b] - so[a] for a, b in zip(ps, ps[1:])])  # of the next token
@@ -95,7 +96,8 @@ class PromptCache:
     def prefill(self, q, k, v, la=None, ca=None, mask="causal", scale=None, cap=0.0, slopes=None):
         """Attention of every token of the prompts: over the bits la and ca, or dense
         under `mask`; leaves the documents' keys in the pages, with the weights that
-        the query's tokens give them, and the query's own to be appended by cut."""
+        the query's tokens give them, and the query's own (with those that they give
+        each other) to be appended by cut."""
         torch = _torch()
         if self.weights is not None:
             raise SiftError("PromptCache.prefill", 6, "the prompts are prefilled already")
@@ -116,7 +118,9 @@ class PromptCache:
             lse = lse[self._query]
         self.weights = self._queries.accumulate(qq, lse, pages, row_ptr=self._query_ptr,
                                                 row_pos=self._query_pos, **self._score)
-        self._pending = (kq, vq)
+        own = [self._drawn(qq[a:z], kq[a:z], lse[a:z], self._query_pos[a:z])
+               for a, z in zip(self._query_rows, self._query_rows[1:])]
+        self._pending = (kq, vq, torch.cat(own))
         return out
 
     def cut(self, budget, sinks=4, recent=0):
@@ -130,11 +134,11 @@ class PromptCache:
                                 None, key_pos)
         self.used = min(self.used, budget)
         if self._pending is not None:
-            k, v = self._pending
+            k, v, own = self._pending
             self._pending = None
             rows = _torch().arange(k.shape[0], device=k.device)
             seq, used = self._room("PromptCache.cut", k, v, rows, self._query_ptr, self.longest)
-            self._store(k, v, rows, seq, used, self._query_pos)
+            self._store(k, v, rows, seq, used, self._query_pos, own)
 
     def step(self, q, k_new, v_new, row_ptr=None, tree_mask=None, row_pos=None):
         """(out, lse) of new tokens over the cache and each other; row_pos None: each
@@ -150,7 +154,8 @@ class PromptCache:
 
     def append(self, q, k_new, v_new, lse, rows, row_ptr=None, row_pos=None, decay=1.0):
         """Takes a step's accepted rows (int64, ascending; those of a prompt follow each
-        other in the answer) into the cache, and their weights into the keys'."""
+        other in the answer) into the cache, with the weights that they give each other,
+        and adds those that they give the cached keys."""
         torch = _torch()
         if self.weights is None or self._pending is not None:
             raise SiftError("PromptCache.append", 6, "the prompts' caches are not cut yet")
@@ -158,10 +163,11 @@ class PromptCache:
         pos = self._positions(q.shape[0], row_ptr, row_pos)
         # whatever may be refused comes before the weights and the pages change
         seq, used = self._room("PromptCache.append", k_new, v_new, rows, ptr, self.max_rows)
+        own = self._drawn(q[rows], k_new[rows], lse[rows], pos[rows], seq)
         counts = torch.zeros(q.shape[0], device=q.device).index_fill_(0, rows, 1.0)
         self.cache.accumulate(q, lse, self.pages, self.weights, decay, row_ptr=row_ptr, row_pos=pos,
                               row_weight=counts, **self._score)
-        added = self._store(k_new, v_new, rows, seq, used, pos)
+        added = self._store(k_new, v_new, rows, seq, used, pos, own)
         self.next_pos = self.next_pos + added
 
     def _pointers(self, rows, row_ptr):
@@ -196,8 +202,38 @@ class PromptCache:
                 raise SiftError(fn, 5, f"{used} slots, room for {self.cache.slots}")
         return seq, used
 
-    def _store(self, k, v, rows, seq, used, row_pos):
-        """Rows of k and v into the slots after their prompt's last; how many of each."""
+    def _drawn(self, q, k, lse, pos, seq=None):
+        """The attention weight that each of these tokens, which the cache does not hold
+        yet, draws from those that see it: itself and its prompt's later ones.  seq:
+        the tokens' prompts (None: one).  [tokens, kv heads]"""
+        torch = _torch()
+        n, hq, d = q.shape
+        hkv = k.shape[1]
+        scale, cap, slopes = (self._score[x] for x in ("scale", "cap", "slopes"))
+        scale = scale if scale is not None and scale > 0 else d ** -0.5
+        qt = q.float().view(n, hkv, hq // hkv, d).permute(1, 0, 2, 3)
+        kt = k.float().permute(1, 2, 0).contiguous()
+        out = torch.zeros(hkv, n, device=q.device)
+        some = max(1, (1 << 24) // max(1, hq * n))   # rows at a time: 64 MB of scores
+        for a in range(0, n, some):
+            z = min(n, a + some)                     # (they see no key past their last)
+            s = torch.matmul(qt[:, a:z].reshape(hkv, -1, d), kt[:, :, :z]).mul_(scale)
+            if cap:
+                s = (s / cap).tanh_().mul_(cap)
+            s = s.view(hkv, z - a, -1, z)
+            if slopes is not None:
+                far = (pos[a:z, None] - pos[None, :z]).abs().float()
+                s = s - slopes[:hq].view(hkv, 1, -1, 1) * far[None, :, None, :]
+            w = (s - lse[a:z].view(z - a, hkv, -1, 1).transpose(0, 1)).exp_()
+            sees = torch.arange(z, device=q.device) <= torch.arange(a, z, device=q.device)[:, None]
+            if seq is not None:
+                sees &= seq[a:z, None] == seq[None, :z]
+            out[:, :z] += torch.where(sees[None, :, None, :], w, 0.0).sum((1, 2))
+        return out.t()
+
+    def _store(self, k, v, rows, seq, used, row_pos, own):
+        """Rows of k and v into the slots after their prompt's last, with the weights
+        `own`; how many of each."""
         torch = _torch()
         pages, page = self.pages, self.cache.page
         self.used = used
@@ -206,7 +242,7 @@ class PromptCache:
         to = pages.page_table[seq, slot // page].long() * page + slot % page
         pages.k_pages[to], pages.v_pages[to] = k[rows], v[rows]
         pages.key_pos[seq, :, slot] = row_pos[rows, None]
-        self.weights[seq, :, slot] = 0.0
+        self.weights[seq, :, slot] = own
         added = torch.zeros_like(pages.lens).index_add_(0, seq, torch.ones_like(seq, dtype=torch.int32))
         pages.lens += added
         return added

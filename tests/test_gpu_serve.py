@@ -247,3 +247,84 @@ def test_append_checks_its_rows_first():
             with pytest.raises(SiftError) as e:
                 c.append(x[:2], k, v, lse, rows)
             assert e.value.status == 2 and torch.equal(before, c.weights)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("dense", [False, True])
+def test_new_keys_enter_with_the_weights_they_have_drawn(dtype, d, dense):
+    """A query's or an answer's token has the weight that it and the later tokens of
+    its prompt, taken in with it, give it."""
+    import torch
+    from paper_2606_09441_amd.serve import PromptCache
+    hq, hkv, g = 6, 2, 3
+    so, ps = [0], [0]
+    for p in PROMPTS:
+        for n in p:
+            so.append(so[-1] + n)
+        ps.append(len(so) - 1)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator("cuda").manual_seed(6)
+    draw = lambda n, h: torch.randn(n, h, d, generator=gen, device="cuda").to(dt)  # noqa: E731
+    host = lambda t: t.double().cpu().numpy()  # noqa: E731
+    slopes = [.5, .1, .02, .3, .05, .01] if dense else [0.0] * 6
+    cap = 10.0 if dense else 0.0
+    score = dict(cap=cap, slopes=torch.tensor(slopes, device="cuda"), scale=0.2) if dense else {}
+    scale = 0.2 if dense else d ** -0.5
+    # scores and log sums are within 1e-4 (tests of the operators), weights so relative to them
+    REL = 2e-4
+
+    def drawn(q, k, lse, pos):
+        """[n, Hkv] of a prompt's new tokens."""
+        w = np.zeros((len(q), hkv))
+        for i in range(len(q)):
+            for h in range(hq):
+                s = S.scores(q[i, h], k[:i + 1, h // g], scale, cap, slopes[h], pos[i] - pos[:i + 1])
+                w[:i + 1, h // g] += np.exp(s - lse[i, h])
+        return w
+
+    q, k, v = draw(so[-1], hq), draw(so[-1], hkv), draw(so[-1], hkv)
+    with PromptCache(so, ps, hq, hkv, d, page=32, room=64, max_rows=4, dtype=dt) as c:
+        bits = [torch.full((c.plan.info[x],), 255, dtype=torch.uint8, device="cuda")
+                for x in ("la_bytes", "ca_bytes")] if not dense else (None, None)
+        c.prefill(q, k, v, *bits, **score)
+        _, lse = S.dense(host(q), host(k), host(v), so, ps, "causal", scale, cap, slopes)
+        c.cut(24, sinks=2)
+        for b in range(4):
+            n, a, z = int(c.pages.lens[b]), so[ps[b + 1] - 1], so[ps[b + 1]]
+            want = drawn(host(q)[a:z], host(k)[a:z], lse[a:z], np.arange(a, z))
+            got = host(c.weights[b, :, n - (z - a):n]).T
+            assert np.max(np.abs(got / want - 1)) <= REL
+            assert not bool(c.weights[b, :, n:].any())
+        for accepted in ([0, 1, 3, 4, 5, 8], [7], [1, 2, 12, 13, 14, 15]):
+            before, lens = c.weights.clone(), c.pages.lens.tolist()
+            qn, kn, vn = draw(16, hq), draw(16, hkv), draw(16, hkv)
+            _, lse = c.step(qn, kn, vn)
+            at = c.next_pos.cpu().numpy().repeat(4) + np.arange(16) % 4
+            rows = torch.tensor(accepted, device="cuda")
+            c.append(qn, kn, vn, lse, rows, decay=0.5)
+            for b in range(4):
+                r = [x for x in accepted if x // 4 == b]
+                want = drawn(host(qn)[r], host(kn)[r], host(lse)[r], at[r])
+                got = host(c.weights[b, :, lens[b]:lens[b] + len(r)]).T
+                assert int(c.pages.lens[b]) == lens[b] + len(r)
+                assert not len(r) or np.max(np.abs(got / want - 1)) <= REL
+                # the others' share of the accepted rows: no less than what decay leaves
+                assert bool((c.weights[b, :, :lens[b]] >= 0.5 * before[b, :, :lens[b]]).all())
+
+
+def test_answers_outlast_a_cut_without_protection():
+    """Tokens that their own rows attend to are not the first to go."""
+    import torch
+    from paper_2606_09441_amd.serve import PromptCache
+    gen = torch.Generator("cuda").manual_seed(7)
+    draw = lambda n: torch.randn(n, 1, 64, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    x = draw(330)
+    with PromptCache([0, 300, 330], [0, 2], 1, 1, 64, page=32, room=32, max_rows=1) as c:
+        c.prefill(x, x, x)
+        c.cut(100, sinks=0)
+        for _ in range(10):
+            q = 3 * draw(1)                   # 24 at itself, far above the others' scores
+            _, lse = c.step(q, q, q)
+            c.append(q, q, q, lse, torch.zeros(1, dtype=torch.int64, device="cuda"))
+        c.cut(60, sinks=0)
+        assert set(range(330, 340)) <= set(c.pages.key_pos[0, 0, :60].tolist())
