@@ -67,12 +67,13 @@ class PromptCache:
         k, v = (torch.zeros(pool, dtype=dtype, device=dev) for _ in range(2))
         key_pos = ints(pos)[:, None, :].expand(-1, num_kv_heads, -1).contiguous()
         self.pages = CachePages(k, v, ints(table), ints(lens), ints(page_lens), key_pos)
-        self._tile_page, self._tile_rows = ints(tile_page), torch.tensor(tile_rows, device=dev)
+        longs = lambda x: torch.tensor(x, dtype=torch.int64, device=dev)  # noqa: E731
+        self._tile_page, self._tile_rows = ints(tile_page), longs(tile_rows)
         query = [t for b in range(seqs) for t in range(so[ps[b + 1] - 1], so[ps[b + 1]])]
         first = [0]
         for b in range(seqs):
             first.append(first[-1] + so[ps[b + 1]] - so[ps[b + 1] - 1])
-        self._query, self._query_ptr = torch.tensor(query, device=dev), ints(first)
+        self._query, self._query_ptr = longs(query), ints(first)
         self._query_rows = first
         self._query_pos = ints([t - so[ps[b]] for b in range(seqs)
                                 for t in range(so[ps[b + 1] - 1], so[ps[b + 1]])])

@@ -328,3 +328,28 @@ def test_answers_outlast_a_cut_without_protection():
             c.append(q, q, q, lse, torch.zeros(1, dtype=torch.int64, device="cuda"))
         c.cut(60, sinks=0)
         assert set(range(330, 340)) <= set(c.pages.key_pos[0, 0, :60].tolist())
+
+
+@pytest.mark.parametrize("sparse", [True, False])
+@pytest.mark.parametrize("prompts", [[[30, 0]], [[40, 7, 0], [5], [33, 0]]])
+def test_prompts_without_a_query(prompts, sparse):
+    """Documents alone: all keys draw nothing, the lowest slots stay."""
+    import torch
+    from paper_2606_09441_amd.serve import PromptCache
+    so, ps = [0], [0]
+    for p in prompts:
+        for n in p:
+            so.append(so[-1] + n)
+        ps.append(len(so) - 1)
+    x = torch.randn(so[-1], 2, 64, device="cuda")
+    with PromptCache(so, ps, 2, 2, 64, page=16, room=8, max_rows=2,
+                     dtype=torch.float32) as c:
+        bits = [torch.full((c.plan.info[n],), 255, dtype=torch.uint8, device="cuda")
+                for n in ("la_bytes", "ca_bytes")] if sparse else (None, None)
+        c.prefill(x, x, x, *bits)
+        c.cut(16, sinks=0)
+        docs, query = [sum(p[:-1]) for p in prompts], [p[-1] for p in prompts]
+        assert c.pages.lens.tolist() == [min(16, n) + m for n, m in zip(docs, query)]
+        assert c.pages.key_pos[0, 0, :16].tolist() == list(range(16))
+        out, lse = c.step(x[:2 * len(prompts)], x[:2 * len(prompts)], x[:2 * len(prompts)])
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
