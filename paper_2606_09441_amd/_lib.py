@@ -266,6 +266,24 @@ def bitmap_bytes(seg_offsets, prompt_seg_ptr, num_q_heads: int, tile: int) -> tu
     return la.value, ca.value
 
 
+def require_laid_out(fn: str, t, name: str, dtype: str, sizes: tuple, device=None) -> None:
+    """require of a buffer that the library reads as one of these sizes."""
+    n = 1
+    for x in sizes:
+        n *= x
+    require(fn, t, name, dtype, n, device)
+    if t is not None and t.numel() != n:
+        check_laid_out(fn, name, t.shape, sizes)
+
+
+def check_laid_out(fn: str, name: str, shape, sizes: tuple) -> None:
+    """A contiguous buffer of more elements than the library reads has to hold those
+    at the same places: it may have more rows, or be flat, but no longer rows."""
+    for i in range(1, min(len(shape), len(sizes))):   # dimensions from the last on
+        if shape[-i] != sizes[-i] and math.prod(sizes[:-i]) > 1:
+            raise SiftError(fn, 2, f"{name} is {tuple(shape)}, has to be {sizes}")
+
+
 def layout_struct(seg_offsets, prompt_seg_ptr):
     so = np.ascontiguousarray(np.asarray(seg_offsets, dtype=np.int32))
     ps = np.ascontiguousarray(np.asarray(prompt_seg_ptr, dtype=np.int32))
@@ -423,8 +441,8 @@ class Plan:
             raise SiftError(fn, 4, f"mask must be one of {sorted(MASKS)}")
         score = score_struct(fn, scale, cap, slopes, self.info["num_q_heads"], self.device)
         if lse is not None:
-            require(fn, lse, "lse", "float32", self.info["num_tokens"] * self.info["num_q_heads"],
-                    self.device)
+            require_laid_out(fn, lse, "lse", "float32",
+                             (self.info["num_tokens"], self.info["num_q_heads"]), self.device)
         if out is None:
             out = _empty_like(q, stream)
         dev = self.device
@@ -713,7 +731,7 @@ class CachePages:
         self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
         self.page_lens, self.key_pos = page_lens, key_pos
         self._held = (k_pages, v_pages, page_table, lens, page_lens, key_pos, kd, vd)
-        self.sizes = (dev, *(None if t is None else t.numel()
+        self.sizes = (dev, *(None if t is None else (t.numel(), t.shape)
                              for t in (page_table, lens, page_lens, key_pos)))
         self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
                                   lens.data_ptr(), 0 if page_lens is None else page_lens.data_ptr(),
@@ -736,8 +754,10 @@ class Cache:
         self.num_seqs, self.hq, self.hkv, self.d = num_seqs, num_q_heads, num_kv_heads, head_dim
         self.page, self.max_pages, self.max_rows = page, max_pages, max_rows
         self.slots = max_pages * page
-        pages = num_seqs * max_pages
-        self._tables = (pages, num_seqs, pages, num_seqs * num_kv_heads * self.slots)
+        self._slot_sizes = (num_seqs, num_kv_heads, self.slots)
+        sizes = (("page_table", (num_seqs, max_pages)), ("lens", (num_seqs,)),
+                 ("page_lens", (num_seqs, max_pages)), ("key_pos", self._slot_sizes))
+        self._tables = tuple((name, math.prod(x), x) for name, x in sizes)
 
     def close(self):
         if self._h is not None:
@@ -761,9 +781,12 @@ class Cache:
         device, *have = kv.sizes
         if device != self.device:
             raise SiftError(fn, 7, f"the pages are on {device}, the cache on {self.device}")
-        for name, m, n in zip(("page_table", "lens", "page_lens", "key_pos"), have, self._tables):
-            if m is not None and m < n:
-                raise SiftError(fn, 5, f"{name} holds {m} elements, needs {n}")
+        for t, (name, n, sizes) in zip(have, self._tables):
+            if t is None or t[0] == n:
+                continue
+            if t[0] < n:
+                raise SiftError(fn, 5, f"{name} holds {t[0]} elements, needs {n}")
+            check_laid_out(fn, name, t[1], sizes)
         return kv.struct
 
     def _rows(self, fn, q, row_ptr, row_pos):
@@ -792,7 +815,7 @@ class Cache:
             require(fn, tree_mask, "tree_mask", "int64", q.shape[0] * words, self.device)
         score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
         if lse is not None:
-            require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
+            require_laid_out(fn, lse, "lse", "float32", (q.shape[0], self.hq), self.device)
         if out is None:
             out = _empty_like(q, stream)
         dev = self.device
@@ -803,7 +826,7 @@ class Cache:
         return out
 
     def _slot_buffer(self, fn, t, name, dtype="float32"):
-        require(fn, t, name, dtype, self.num_seqs * self.hkv * self.slots, self.device)
+        require_laid_out(fn, t, name, dtype, self._slot_sizes, self.device)
 
     def accumulate(self, q, lse, kv, weights=None, decay=1.0, row_ptr=None, row_pos=None,
                    row_weight=None, scale=None, cap=0.0, slopes=None, out=None, stream=None):
@@ -815,7 +838,7 @@ class Cache:
         torch = _torch()
         fn = "sift_cache_accumulate"
         rows = self._rows(fn, q, row_ptr, row_pos)
-        require(fn, lse, "lse", "float32", q.shape[0] * self.hq, self.device)
+        require_laid_out(fn, lse, "lse", "float32", (q.shape[0], self.hq), self.device)
         if row_weight is not None:
             require(fn, row_weight, "row_weight", "float32", q.shape[0], self.device)
         if weights is not None:

@@ -97,3 +97,16 @@ def test_layer_ops_without_the_frameworks_dual_level(monkeypatch):
     x = torch.ones(2, 64, dtype=torch.bfloat16)
     assert rms_norm(x, x[0], 1e-5) is None
     assert silu_mul(x, x) is None
+
+
+def test_buffers_of_more_elements_hold_them_at_the_same_places():
+    """More rows, or a flat buffer, are fine; longer rows would be read as others."""
+    for shape, sizes in (((5, 8), (3, 8)), ((64,), (3, 8)), ((2, 3, 8), (3, 8)), ((1, 99), (1, 8)),
+                         ((4, 2, 8), (3, 2, 8)), ((8, 8), (3, 2, 8)), ((1, 5, 8), (1, 2, 8)),
+                         ((1, 1, 12), (1, 1, 8)), ((9,), (3,)), ((2, 9), (3,)), ((), (1,))):
+        L.check_laid_out("f", "x", shape, sizes)
+    for shape, sizes in (((3, 9), (3, 8)), ((3, 3, 8), (3, 2, 8)), ((3, 2, 9), (3, 2, 8)),
+                         ((1, 2, 9), (1, 2, 8)), ((9, 9), (3, 2, 8)), ((2, 4, 9), (3, 8))):
+        with pytest.raises(SiftError) as e:
+            L.check_laid_out("f", "x", shape, sizes)
+        assert e.value.status == 2

@@ -321,3 +321,33 @@ def test_scales_and_caps_that_fp32_does_not_hold():
                 with pytest.raises(SiftError) as e:
                     call()
                 assert e.value.status == 4
+
+
+def test_tables_of_longer_rows():
+    """A table made for larger caches would be read as another one."""
+    import torch
+    from paper_2606_09441_amd import CachePages, SiftError
+    x = Batch([100, 30], [2, 2], 4, 2, 128, "bf16", seed=24, moved=True)
+    more = lambda t, n: torch.cat([t, torch.zeros_like(t[..., :n])], -1)  # noqa: E731
+    t, lens, pos = x.t["table"], x.t["lens"], x.t["key_pos"]
+    lse = torch.zeros(4, 4, device=x.q.device)
+    w = torch.zeros(2, 2, x.slots, device=x.q.device)
+    args = (x.q, x.k_new, x.v_new)
+    with x.cache() as cache:
+        want = cache.attention(*args, x.pages())
+        rows = CachePages(x.k, x.v, torch.cat([t, t]), torch.cat([lens, lens]), key_pos=torch.cat([pos, pos]))
+        assert torch.equal(want, cache.attention(*args, rows))
+        for bad in (CachePages(x.k, x.v, more(t, 2), lens), CachePages(x.k, x.v, t, lens, page_lens=more(t, 1)),
+                    CachePages(x.k, x.v, t, lens, key_pos=more(pos, 64))):
+            for call in (lambda: cache.attention(*args, bad), lambda: cache.evict(bad, w, 8),
+                         lambda: cache.accumulate(x.q, lse, bad)):
+                with pytest.raises(SiftError) as e:
+                    call()
+                assert e.value.status == 2
+        kv = x.pages()
+        for call in (lambda: cache.evict(kv, more(w, 64), 8), lambda: cache.accumulate(x.q, lse, kv, more(w, 64)),
+                     lambda: cache.accumulate(x.q, more(lse, 2), kv),
+                     lambda: cache.attention(*args, kv, lse=more(lse, 2))):
+            with pytest.raises(SiftError) as e:
+                call()
+            assert e.value.status == 2
