@@ -351,3 +351,51 @@ def test_tables_of_longer_rows():
             with pytest.raises(SiftError) as e:
                 call()
             assert e.value.status == 2
+
+
+def wide(x):
+    """Whether bf16 goes by the units of 128 rows: 24 * 2^20 rows of a kv head times
+    slots of all caches."""
+    return x.max_rows * (x.hq // x.hkv) * x.B * x.hkv * x.slots >= 24 << 20
+
+
+@pytest.mark.parametrize("hq,hkv", [(8, 2), (9, 3), (16, 8)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tree,gaps,moved,cap,bias", [
+    (None, False, False, 0.0, False), (random_tree, True, False, 0.0, False),
+    (some_empty, False, False, 30.0, False), (random_tree, False, True, 0.0, True),
+    (None, True, True, 20.0, True)])
+def test_many_rows_of_several_kv_heads(hq, hkv, d, tree, gaps, moved, cap, bias):
+    x = Batch([5000, 300, 0], WIDE[1], hq, hkv, d, "bf16", 128, gaps, moved, tree, seed=21, extra_pages=47)
+    assert wide(x)
+    check(x, cap, bias)
+
+
+@pytest.mark.parametrize("gaps,moved,cap,bias", [(False, False, 0.0, False), (True, False, 0.0, False),
+                                                 (False, True, 0.0, True), (False, False, 20.0, True)])
+def test_many_rows_of_many_sequences(gaps, moved, cap, bias):
+    """More sequences than a wavefront has lanes, some without rows or keys."""
+    rng = np.random.default_rng(22)
+    lens = rng.integers(0, 300, 70).tolist()
+    new = rng.integers(0, 21, 70).tolist()
+    lens[5], new[3], new[66] = 0, 20, 0
+    x = Batch(lens, new, 8, 2, 64, "bf16", 128, gaps, moved, random_tree, seed=22, extra_pages=16)
+    assert wide(x)
+    check(x, cap, bias)
+
+
+def test_units_by_rows_and_slots():
+    """The same rows over the same keys by either unit: a handle with room for more
+    slots goes by the wide ones."""
+    import torch
+    outs = []
+    for extra, is_wide in ((1, False), (400, True)):
+        x = Batch([500, 90], [40, 9], 16, 2, 128, "bf16", 128, tree=random_tree, seed=25, extra_pages=1)
+        x.max_pages += extra - 1
+        x.slots = x.max_pages * 128
+        x.table = np.concatenate([x.table, np.zeros((2, extra - 1), np.int32)], 1)
+        x.t["table"] = torch.from_numpy(x.table).to(x.q.device)
+        assert wide(x) == is_wide
+        outs.append(check(x))
+    assert max_abs(outs[0][0], outs[1][0]) <= TOL["bf16"]
+    assert max_abs(outs[0][1], outs[1][1]) <= LSE_TOL
