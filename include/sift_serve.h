@@ -138,6 +138,9 @@ sift_status sift_cache_destroy(sift_cache* cache);
  *                NULL: a chain, each row sees those up to itself.
  *   score        see sift_score
  *   lse          device float [rows][Hq], or NULL: the rows' log sum exp
+ * bf16 handles of many rows and slots (max_pages, not the lengths, which only the
+ *   device knows) go by larger units of work, slower for short caches: make a
+ *   handle for the sizes that it meets.
  * A row that sees no key gets 0, and -infinity for its log sum; so does one
  * whose every visible score is -infinity.  Keys that a row does not see have no
  * influence on it.  Rows that row_ptr leaves out are not written.  Results

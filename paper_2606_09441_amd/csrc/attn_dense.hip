@@ -272,6 +272,7 @@ struct DenseTiles {
   }
 };
 
+// (D = 128 with bias and log sums: two registers of a lane are spilled)
 template <int D, bool kCap, bool kBias, bool kLse>
 __global__ __launch_bounds__(256, 2) void attn_dense_bf16_kernel(DenseArgs a) {
   using T = __bf16;
@@ -397,7 +398,7 @@ __global__ __launch_bounds__(256, sizeof(T) * D > 256 ? 1 : 2) void attn_dense_s
 // full, so what counts is how long one takes.  us of 128 / 32 rows (causal, bf16 D =
 // 128, then fp32 D = 64): 6 workgroups 11.8 / 8.1, 25.8 / 11.6; 136: 45 / 30, 156 /
 // 77; 264: 86 / 73, 315 / 205; but 224 of a short prompt 19.3 / 20.0, 544: 59 / 82,
-// 216 / 194.
+// 216 / 194.  (One limit for both types, where bf16's lies; fp32's own lies higher.)
 constexpr int64_t kDenseFew = 256;
 
 int64_t dense_grid(int32_t num_recs, int32_t hq, int32_t hkv) {

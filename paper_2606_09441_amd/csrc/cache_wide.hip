@@ -1,8 +1,11 @@
 // The attention of many new tokens over a paged cache (bf16): units of 128 rows of
 // a (sequence, kv head), 32 of each wavefront, which share the 64-key tiles of the
 // pipeline (flash_pipe.h).  With hundreds of rows to a key (64 drafted tokens, 6
-// query heads) the matrix cores bound it, not HBM.  The tiles of all units form one
-// list, cut into equal runs, as in cache_attn.hip, whose merge this shares.
+// query heads) the products are what there is to do, not the bytes.  The tiles of all
+// units form one list, cut into equal runs, as in cache_attn.hip, whose merge this
+// shares.  64 tokens, 48/8 heads, D = 128 over 66048 slots: 143 us, 730 TFLOP/s, the
+// MFMAs busy in 37% of the SIMDs' cycles, the VALU in 42%: runs of 48 tiles a
+// workgroup, and the instances of D = 128 spill 120 to 148 bytes of registers a lane.
 
 #include "cache.h"
 #include "flash_pipe.h"
