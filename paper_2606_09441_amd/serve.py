@@ -139,7 +139,7 @@ class PromptCache:
             self._pending = None
             rows = _torch().arange(k.shape[0], device=k.device)
             seq, used = self._room("PromptCache.cut", k, v, rows, self._query_ptr, self.longest)
-            self._store(k, v, rows, seq, used, self._query_pos, own)
+            self._store(k, v, seq, used, self._query_pos, own)
 
     def step(self, q, k_new, v_new, row_ptr=None, tree_mask=None, row_pos=None):
         """(out, lse) of new tokens over the cache and each other; row_pos None: each
@@ -164,11 +164,12 @@ class PromptCache:
         pos = self._positions(q.shape[0], row_ptr, row_pos)
         # whatever may be refused comes before the weights and the pages change
         seq, used = self._room("PromptCache.append", k_new, v_new, rows, ptr, self.max_rows)
-        own = self._drawn(q[rows], k_new[rows], lse[rows], pos[rows], seq)
+        k, v, at = k_new[rows], v_new[rows], pos[rows]
+        own = self._drawn(q[rows], k, lse[rows], at, seq)
         counts = torch.zeros(q.shape[0], device=q.device).index_fill_(0, rows, 1.0)
         self.cache.accumulate(q, lse, self.pages, self.weights, decay, row_ptr=row_ptr, row_pos=pos,
                               row_weight=counts, **self._score)
-        added = self._store(k_new, v_new, rows, seq, used, pos, own)
+        added = self._store(k, v, seq, used, at, own)
         self.next_pos = self.next_pos + added
 
     def _pointers(self, rows, row_ptr):
@@ -210,39 +211,43 @@ class PromptCache:
         torch = _torch()
         n, hq, d = q.shape
         hkv = k.shape[1]
+        g = hq // hkv
         scale, cap, slopes = (self._score[x] for x in ("scale", "cap", "slopes"))
-        scale = scale if scale is not None and scale > 0 else d ** -0.5
-        qt = q.float().view(n, hkv, hq // hkv, d).permute(1, 0, 2, 3)
-        kt = k.float().permute(1, 2, 0).contiguous()
-        out = torch.zeros(hkv, n, device=q.device)
+        scale = scale if scale is not None and 0 < scale < float("inf") else d ** -0.5
+        qt = torch.empty(hkv, n, g, d, device=q.device).copy_(q.view(n, hkv, g, d).transpose(0, 1))
+        kt = k.float().permute(1, 2, 0)
+        if seq is None:
+            seq = torch.zeros(n, dtype=torch.bool, device=q.device)
         some = max(1, (1 << 24) // max(1, hq * n))   # rows at a time: 64 MB of scores
+        out = torch.zeros(n, hkv, device=q.device) if some < n or n == 0 else None
         for a in range(0, n, some):
             z = min(n, a + some)                     # (they see no key past their last)
-            s = torch.matmul(qt[:, a:z].reshape(hkv, -1, d), kt[:, :, :z]).mul_(scale)
+            s = torch.matmul(qt[:, a:z].view(hkv, -1, d), kt[:, :, :z]).mul_(scale)
             if cap:
-                s = (s / cap).tanh_().mul_(cap)
-            s = s.view(hkv, z - a, -1, z)
+                s = s.div_(cap).tanh_().mul_(cap)
+            s = s.view(hkv, z - a, g, z)
             if slopes is not None:
-                far = (pos[a:z, None] - pos[None, :z]).abs().float()
-                s = s - slopes[:hq].view(hkv, 1, -1, 1) * far[None, :, None, :]
-            w = (s - lse[a:z].view(z - a, hkv, -1, 1).transpose(0, 1)).exp_()
-            sees = torch.arange(z, device=q.device) <= torch.arange(a, z, device=q.device)[:, None]
-            if seq is not None:
-                sees &= seq[a:z, None] == seq[None, :z]
-            out[:, :z] += torch.where(sees[None, :, None, :], w, 0.0).sum((1, 2))
-        return out.t()
+                far = (pos[a:z, None] - pos[:z]).abs_()
+                s = s.sub_(slopes[:hq].view(hkv, 1, g, 1) * far[:, None])
+            w = s.sub_(lse[a:z].view(z - a, hkv, g, 1).transpose(0, 1)).exp_()
+            hidden = (seq[a:z, None] == seq[:z]).tril_(a).logical_not_()
+            own = w.masked_fill_(hidden[:, None], 0.0).sum((1, 2)).t()
+            if out is None:
+                return own
+            out[:z] += own
+        return out
 
-    def _store(self, k, v, rows, seq, used, row_pos, own):
-        """Rows of k and v into the slots after their prompt's last, with the weights
-        `own`; how many of each."""
+    def _store(self, k, v, seq, used, pos, own):
+        """Keys of prompts seq into the slots after their last, with the weights `own`;
+        how many of each."""
         torch = _torch()
         pages, page = self.pages, self.cache.page
         self.used = used
-        at = torch.arange(rows.shape[0], device=rows.device)
+        at = torch.arange(seq.shape[0], device=seq.device)
         slot = pages.lens[seq] + at - torch.searchsorted(seq, seq)
         to = pages.page_table[seq, slot // page].long() * page + slot % page
-        pages.k_pages[to], pages.v_pages[to] = k[rows], v[rows]
-        pages.key_pos[seq, :, slot] = row_pos[rows, None]
+        pages.k_pages[to], pages.v_pages[to] = k, v
+        pages.key_pos[seq, :, slot] = pos[:, None]
         self.weights[seq, :, slot] = own
         added = torch.zeros_like(pages.lens).index_add_(0, seq, torch.ones_like(seq, dtype=torch.int32))
         pages.lens += added

@@ -353,3 +353,27 @@ def test_prompts_without_a_query(prompts, sparse):
         assert c.pages.key_pos[0, 0, :16].tolist() == list(range(16))
         out, lse = c.step(x[:2 * len(prompts)], x[:2 * len(prompts)], x[:2 * len(prompts)])
         assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+
+
+def test_a_long_query_draws_weights_in_parts():
+    """More scores than are made at a time."""
+    import torch
+    from paper_2606_09441_amd.serve import PromptCache
+    n, hq, hkv, d = 2100, 8, 2, 64
+    assert hq * n * n > 2 << 24
+    gen = torch.Generator("cuda").manual_seed(8)
+    draw = lambda h: torch.randn(n + 10, h, d, generator=gen, device="cuda")  # noqa: E731
+    q, k, v = draw(hq), draw(hkv), draw(hkv)
+    host = lambda t: t.double().cpu().numpy()  # noqa: E731
+    with PromptCache([0, 10, n + 10], [0, 2], hq, hkv, d, page=64, dtype=torch.float32) as c:
+        c.prefill(q, k, v)
+        c.cut(10, sinks=0)
+        got = host(c.weights[0, :, 10:n + 10])
+    want = np.zeros((hkv, n))
+    for h in range(hq):
+        s = host(q[10:, h]) @ host(k[:, h // 4]).T * d ** -0.5
+        s[:, 10:][np.triu_indices(n, 1)] = -np.inf
+        m = s.max(1, keepdims=True)
+        w = np.exp(s - m)
+        want[h // 4] += (w / w.sum(1, keepdims=True))[:, 10:].sum(0)
+    assert np.max(np.abs(got / want - 1)) <= 2e-4      # scores and log sums within 1e-4
