@@ -72,6 +72,44 @@ sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_te
                             sift_tensor* out, float* lse, void* stream);
 
 /*
+ * Rotary positions.  The first rot_dim dims of a head turn in pairs (x, y) by the
+ * angle position * inv_freq[i], i < rot_dim / 2:
+ *   x' = magnitude * (x cos - y sin),  y' = magnitude * (y cos + x sin)
+ * the others stay.  The angle is the product of the integer and the float, reduced
+ * without loss (sift_rope rounds that product to fp32).
+ *   inv_freq     device float [rot_dim / 2]: any table, so that any scaling of the
+ *                frequencies for long contexts is one
+ *   rot_dim      even, 2 .. D
+ *   interleaved  0: pair i is dims i and rot_dim / 2 + i; else 2 i and 2 i + 1
+ *   magnitude    finite, > 0
+ */
+typedef struct sift_rotary {
+  const float* inv_freq;
+  int32_t rot_dim;
+  int32_t interleaved;
+  float magnitude;
+} sift_rotary;
+
+/*
+ * q and k turned by their tokens' positions, into q_out and k_out.
+ *   q, q_out     [tokens][Hq][D];  k, k_out: [tokens][Hkv][D], or both NULL.  All
+ *                SIFT_BF16 or all SIFT_F32, any D; an output is its input's buffer, or
+ *                apart from all others.  16-byte aligned buffers of whole 16-byte
+ *                chunks (rot_dim, and its half where pairs lie in halves, too) go
+ *                fastest.
+ *   positions    device int32 [tokens]
+ *   back         not 0: by the negative angles.  That is the gradient of the call (its
+ *                transpose), and where the magnitude is 1 its inverse: keys turned back
+ *                and then by other positions have moved.
+ * Rounded once.  Values that are not finite reach the other one of their pair.
+ * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, magnitude, buffers that
+ *   overlap), SIFT_E_CAPACITY (a token of 2^31 numbers or more), SIFT_E_HIP.
+ */
+sift_status sift_rotate(const sift_tensor* q, const sift_tensor* k, const int32_t* positions,
+                        const sift_rotary* rotary, int32_t back, sift_tensor* q_out,
+                        sift_tensor* k_out, void* stream);
+
+/*
  * The paged cache of a batch of sequences, of one layer.
  *
  * Slots: sequence b owns max_pages pages of `page` slots.  Slot i is row

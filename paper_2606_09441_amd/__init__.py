@@ -9,6 +9,7 @@ from ._lib import (  # noqa: F401
     Cache,
     CachePages,
     Plan,
+    Rotary,
     SiftError,
     decode_tiles,
     decode_workspace_bytes,
@@ -18,10 +19,11 @@ from ._lib import (  # noqa: F401
     header_functions,
     lib,
     rope_,
+    rotary_frequencies,
     sparse_prefill,
     sparse_prefill_ex,
     workspace_bytes,
 )
 
-__all__ = ["Cache", "CachePages", "Plan", "SiftError", "decode_tiles", "decode_workspace_bytes", "sparse_prefill", "sparse_prefill_ex", "workspace_bytes", "extract_bits", "extract_sizes", "rope_", "lib",
+__all__ = ["Cache", "CachePages", "Plan", "Rotary", "SiftError", "decode_tiles", "decode_workspace_bytes", "sparse_prefill", "sparse_prefill_ex", "workspace_bytes", "extract_bits", "extract_sizes", "rope_", "rotary_frequencies", "lib",
            "header_functions", "default_scale"]

@@ -67,6 +67,11 @@ class SiftCacheRows(ctypes.Structure):
     _fields_ = [("row_ptr", ctypes.c_void_p), ("row_pos", ctypes.c_void_p)]
 
 
+class SiftRotary(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
 MASKS = {"causal": 0, "document": 1, "prefix": 2}
 
 _P = ctypes.c_void_p
@@ -129,6 +134,9 @@ _SERVE_SIGS = {
                                        ctypes.POINTER(SiftTensor), ctypes.c_int32,
                                        ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor), _P,
                                        _P]),
+    "sift_rotate": (ctypes.c_int, [ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor), _P,
+                                   ctypes.POINTER(SiftRotary), ctypes.c_int32,
+                                   ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor), _P]),
     "sift_cache_create": (ctypes.c_int, [ctypes.c_int32] * 7 + [ctypes.POINTER(_P)]),
     "sift_cache_destroy": (ctypes.c_int, [_P]),
     "sift_cache_attention": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv),
@@ -662,6 +670,133 @@ def rope_(q, k, positions, inv_freq, stream=None):
     check("sift_rope", lib().sift_rope(ctypes.byref(qd), ctypes.byref(kd), _ptr(positions),
                                        _ptr(inv_freq), _stream_ptr(stream)))
     return q, k
+
+
+def rotary_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, context=None, low=None,
+                       high=None):
+    """(float32 numpy array [rot_dim / 2], magnitude) of a Rotary: f_i = base^(-2 i / rot_dim),
+    for contexts `factor` times as long as those of the training scaled by
+
+      "linear"  all divided by the factor
+      "base"    the base raised so that the slowest is divided by the factor and the
+                fastest stays: base factor^(rot_dim / (rot_dim - 2))
+      "smooth"  by wavelength: those longer than context / low (1) divided, those shorter
+                than context / high (4) kept, and between them a mean of both, linear in
+                context / wavelength
+      "parts"   by index: kept up to the floor of where a wavelength makes `high` (32)
+                turns in the context, divided from the ceiling of where it makes `low` (1)
+                on, a mean linear in the index between; the magnitude is
+                1 + 0.1 ln(factor)
+
+    context: the length trained on."""
+    fn = "rotary_frequencies"
+    if rot_dim < 2 or rot_dim % 2 or not base > 1 or not factor >= 1:
+        raise SiftError(fn, 2, "needs an even rot_dim, a base above 1 and a factor of 1 at least")
+    i = np.arange(rot_dim // 2, dtype=np.float64)
+    freq, magnitude = np.power(float(base), -2.0 * i / rot_dim), 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "base":
+        if rot_dim < 4:
+            raise SiftError(fn, 2, "one pair has no slowest beside its fastest frequency")
+        freq = np.power(base * factor ** (rot_dim / (rot_dim - 2)), -2.0 * i / rot_dim)
+    elif scaling in ("smooth", "parts"):
+        low = 1.0 if low is None else low
+        high = (4.0 if scaling == "smooth" else 32.0) if high is None else high
+        if context is None or not context > 0 or not 0 < low < high:
+            raise SiftError(fn, 2, "needs the context, and low below high")
+        if scaling == "smooth":
+            keep = np.clip((context * freq / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
+        else:
+            at = lambda turns: rot_dim / 2 * math.log(context / (2 * np.pi * turns)) / math.log(base)  # noqa: E731
+            first = min(max(math.floor(at(high)), 0), rot_dim // 2 - 1)
+            last = min(max(math.ceil(at(low)), 0), rot_dim // 2 - 1)
+            keep = 1.0 - np.clip((i - first) / max(last - first, 1e-3), 0.0, 1.0)
+            magnitude = 1.0 + 0.1 * math.log(factor)
+        freq = freq * keep + freq / factor * (1.0 - keep)
+    elif scaling is not None:
+        raise SiftError(fn, 4, f"no scaling {scaling!r}")
+    return freq.astype(np.float32), magnitude
+
+
+class Rotary:
+    """Rotary positions (sift_rotate): the first 2 len(inv_freq) dims of a head turn in
+    pairs, dims i and len(inv_freq) + i or, interleaved, 2 i and 2 i + 1.  inv_freq:
+    float32 GPU tensor, used where it is, or the numbers (rotary_frequencies)."""
+
+    def __init__(self, inv_freq, interleaved=False, magnitude=1.0):
+        torch = _torch()
+        if not isinstance(inv_freq, torch.Tensor):
+            inv_freq = torch.tensor(np.asarray(inv_freq, np.float32), device="cuda")
+        require("Rotary", inv_freq, "inv_freq", "float32", 1)
+        if not (magnitude > 0 and math.isfinite(magnitude)):
+            raise SiftError("Rotary", 4, f"magnitude {magnitude}")
+        self.inv_freq, self.interleaved, self.magnitude = inv_freq, bool(interleaved), magnitude
+        self.device = inv_freq.device
+        self.struct = SiftRotary(inv_freq.data_ptr(), 2 * inv_freq.numel(), self.interleaved,
+                                 magnitude)
+
+    def rotate(self, q, k, positions, back=False, q_out=None, k_out=None, stream=None):
+        """(q_out, k_out): q [tokens, Hq, D] and k [tokens, Hkv, D] (or None) turned by
+        positions (int32 [tokens]); back: by the negative angles, the gradient of the
+        call.  The outputs are new, or given, and may be the inputs."""
+        fn, dev = "sift_rotate", self.device
+        _current(fn, dev)
+        if k is None and k_out is not None:
+            raise SiftError(fn, 1, "k_out without k")
+        require(fn, positions, "positions", "int32", q.shape[0], dev)
+        if q_out is None:
+            q_out = _empty_like(q, stream)
+        if k is not None and k_out is None:
+            k_out = _empty_like(k, stream)
+        check(fn, lib().sift_rotate(
+            _desc(fn, q, "q", dev), None if k is None else _desc(fn, k, "k", dev),
+            positions.data_ptr(), self.struct, back, _desc(fn, q_out, "q_out", dev),
+            None if k is None else _desc(fn, k_out, "k_out", dev), _stream_ptr(stream)))
+        return q_out, k_out
+
+    def rotate_(self, q, k, positions, back=False, stream=None):
+        """rotate in place."""
+        return self.rotate(q, k, positions, back, q, k, stream)
+
+    def __call__(self, q, k, positions):
+        """rotate with gradients for q and k (any order), on the current stream."""
+        return _turn_function().apply(q, k, positions, self, False)
+
+
+_turn_class = None
+
+
+def _turn_function():
+    """rotate as an autograd function: its gradient is the same with the angles negative,
+    and so on."""
+    global _turn_class
+    if _turn_class is None:
+        torch = _torch()
+
+        class Turn(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, positions, rotary, back):
+                ctx.save_for_backward(positions)
+                ctx.rotary, ctx.back, ctx.pair = rotary, back, k is not None
+                return rotary.rotate(q, k, positions, back)
+
+            @staticmethod
+            def backward(ctx, dq, dk):
+                positions, = ctx.saved_tensors
+                # (a gradient may be a view, or expanded)
+                dq, dk = _turn_class.apply(dq.contiguous(), dk.contiguous() if ctx.pair else None,
+                                           positions, ctx.rotary, not ctx.back)
+                return dq, dk, None, None, None
+
+        _turn_class = Turn
+    return _turn_class
+
+
+def _current(fn, device):
+    """Kernels go to the current device: the tensors' own."""
+    if device.index != _torch().cuda.current_device():
+        raise SiftError(fn, 7, f"the tensors are on {device}, which is not the current device")
 
 
 def _plain(*ts) -> bool:

@@ -385,6 +385,27 @@ hipError_t launch_rms_norm(const void* x, const void* weight, int64_t rows, int 
 hipError_t launch_silu_mul(const void* gate, const void* up, int64_t count, void* out,
                            hipStream_t stream);
 
+// Rotary positions (rotary.hip, cache_append.hip).
+struct RotaryArgs {
+  const float* inv_freq;  // [half]
+  int32_t half;           // pairs of dims that turn
+  int32_t interleaved;    // pairs 2 i, 2 i + 1; 0: i, half + i
+  int32_t back;           // by the negative angles
+  float magnitude;
+};
+struct RotateArgs {
+  RotaryArgs r;
+  const void* q;          // [tokens][hq][d]
+  const void* k;          // [tokens][hk][d], hk may be 0
+  void* q_out;            // the same, may be the input
+  void* k_out;
+  const int32_t* positions;
+  int64_t tokens;
+  int32_t hq, hk, d;
+  int32_t copy;           // the dims that do not turn are copied
+};
+hipError_t launch_rotate(const RotateArgs& a, bool bf16, hipStream_t stream);
+
 // Scores of the dense and the cache attention: z = scale * q.k, then
 // cap * tanh(z / cap) where cap > 0, then - slope[head] * |distance|; in the
 // unit of log2(e) (the attention, whose weights are powers of 2) or of 1.

@@ -1,9 +1,9 @@
 """Decoder-layer prefill slice around the sparse attention.
 
 One pre-norm layer of the Llama-3.1-8B architecture (the model of Section 6):
-RMSNorm, the q/k/v projections, rotary embedding (libsift's `sift_rope`), the
-sparse attention (libsift's plan: decode + attention over the bits), the
-output projection and residual, then optionally the SwiGLU MLP.  The
+RMSNorm, the q/k/v projections, rotary embedding (libsift's `sift_rope`, or
+`sift_rotate` where a Rotary is given), the sparse attention (libsift's
+plan: decode + attention over the bits), the output projection and residual, then optionally the SwiGLU MLP.  The
 projections are library GEMMs (torch.matmul -> hipBLASLt on bf16); the norms
 and the MLP activation are one kernel each, or torch elementwise ops for
 tensors that those do not take (other types or widths, recorded gradients).  It serves to measure the
@@ -13,13 +13,14 @@ paper's time-to-first-token results aggregate (Section 7).
 
 from __future__ import annotations
 
-from ._lib import _torch, rms_norm, rope_, silu_mul
+from ._lib import Rotary, _torch, rms_norm, rope_, silu_mul
 
 
 class PrefillLayer:
     """weights: dict of torch bf16 device tensors w_in, Wqkv, Wo and, for the
     MLP, w_post, Wg, Wu, Wd (shapes as in workloads.layer_weights);
-    inv_freq: float32 device tensor [D/2]."""
+    inv_freq: float32 device tensor [D/2], or a Rotary (part of the head, interleaved
+    pairs, a magnitude)."""
 
     def __init__(self, weights: dict, hq: int, hkv: int, head_dim: int, inv_freq, eps: float = 1e-5):
         self.w = weights
@@ -47,7 +48,10 @@ class PrefillLayer:
         q = (h @ self.Wq.T).view(n, self.hq, self.d)
         k = (h @ self.Wk.T).view(n, self.hkv, self.d)
         v = (h @ self.Wv.T).view(n, self.hkv, self.d)
-        rope_(q, k, positions, self.inv_freq)
+        if isinstance(self.inv_freq, Rotary):
+            self.inv_freq.rotate_(q, k, positions)
+        else:
+            rope_(q, k, positions, self.inv_freq)
         a = plan.run(q, k, v, la, ca)
         return x + a.view(n, self.hq * self.d) @ self.w["Wo"].T
 

@@ -1,0 +1,109 @@
+"""Rotary positions on the host: the frequency tables and their scalings, and what
+sift_rotate refuses before the device is touched."""
+
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from paper_2606_09441_amd import SiftError, rotary_frequencies
+from paper_2606_09441_amd import _lib as B
+
+
+def test_plain_and_evenly_scaled_tables():
+    f, m = rotary_frequencies(8, 10000.0)
+    assert m == 1.0 and f.dtype == np.float32
+    assert np.allclose(f, [1.0, 0.1, 0.01, 0.001], rtol=2.0 ** -24, atol=0)
+    assert np.allclose(rotary_frequencies(8, scaling="linear", factor=4.0)[0], f / 4, rtol=2.0 ** -23)
+    g, _ = rotary_frequencies(8, scaling="base", factor=4.0)
+    assert g[0] == 1.0 and math.isclose(g[-1], f[-1] / 4, rel_tol=2.0 ** -23)
+    assert (g[1:-1] < f[1:-1]).all() and (g[1:-1] > f[1:-1] / 4).all()
+
+
+def test_tables_scaled_by_wavelength():
+    """The table of the architecture that the decoder layer has: factor 8, 8192 tokens."""
+    f, _ = rotary_frequencies(128, 500000.0)
+    g, m = rotary_frequencies(128, 500000.0, "smooth", 8.0, context=8192)
+    assert m == 1.0
+    wave = 2 * np.pi / f.astype(np.float64)
+    for a, b, w in zip(f.astype(np.float64), g, wave):
+        if w < 8192 / 4:
+            want = a
+        elif w > 8192:
+            want = a / 8
+        else:
+            t = (8192 / w - 1) / 3
+            want = (1 - t) * a / 8 + t * a
+        assert math.isclose(b, want, rel_tol=2.0 ** -22)
+    assert (wave < 2048).any() and (wave > 8192).any()
+
+
+def test_tables_scaled_by_parts():
+    f, _ = rotary_frequencies(64, 10000.0)
+    g, m = rotary_frequencies(64, 10000.0, "parts", 16.0, context=4096)
+    assert math.isclose(m, 1 + 0.1 * math.log(16))
+    # 32 turns of 4096 tokens: index 32 ln(4096 / 64 pi) / ln 10^4 = 10.47; one turn: 22.51
+    assert np.array_equal(g[:11], f[:11])
+    assert np.allclose(g[23:], f[23:] / 16, rtol=2.0 ** -22)
+    for i in range(11, 23):
+        t = (i - 10) / 13
+        assert math.isclose(g[i], f[i] / 16 * t + f[i] * (1 - t), rel_tol=2.0 ** -21)
+
+
+@pytest.mark.parametrize("args,kw", [
+    ((7,), {}), ((0,), {}), ((8, 1.0), {}), ((8,), {"scaling": "linear", "factor": 0.5}),
+    ((8,), {"scaling": "smooth", "factor": 2.0}), ((2,), {"scaling": "base", "factor": 2.0}),
+    ((8,), {"scaling": "parts", "factor": 2.0, "context": 100, "low": 4.0, "high": 2.0}),
+    ((8,), {"scaling": "other"}),
+])
+def test_refused_tables(args, kw):
+    with pytest.raises(SiftError):
+        rotary_frequencies(*args, **kw)
+
+
+def _call(q, k, qo, ko, pos=1, rotary=None, null_rotary=False):
+    b = lambda t: None if t is None else ctypes.byref(t)  # noqa: E731
+    r = rotary or B.SiftRotary(1, 64, 0, 1.0)
+    return B.lib().sift_rotate(b(q), b(k), pos, None if null_rotary else ctypes.byref(r), 0, b(qo),
+                               b(ko), None)
+
+
+def _t(data=1 << 20, dtype=B.SIFT_BF16, tokens=3, heads=4, d=64):
+    return B.SiftTensor(data, dtype, tokens, heads, d)
+
+
+def test_refusals():
+    q, k, qo, ko = _t(), _t(2 << 20, heads=2), _t(3 << 20), _t(4 << 20, heads=2)
+    NULL, SHAPE, UNSUPPORTED, CAPACITY = 1, 2, 4, 5
+    assert _call(None, k, qo, ko) == NULL and _call(q, k, None, ko) == NULL
+    assert _call(q, None, qo, ko) == NULL and _call(q, k, qo, None) == NULL
+    assert _call(q, k, qo, ko, null_rotary=True) == NULL
+    assert _call(q, k, qo, ko, pos=None) == NULL
+    assert _call(_t(None), k, qo, ko) == NULL
+    assert _call(q, k, _t(None), ko) == NULL
+    for bad in (_t(tokens=2), _t(d=128), _t(heads=0), _t(tokens=-1)):
+        assert _call(q, bad, qo, ko) == SHAPE
+    assert _call(q, k, _t(3 << 20, heads=3), ko) == SHAPE
+    assert _call(q, k, qo, _t(4 << 20, heads=4)) == SHAPE
+    for dt in (B.SIFT_F32, 2, 9):
+        assert _call(q, _t(2 << 20, dt, heads=2), qo, ko) == UNSUPPORTED
+        assert _call(q, k, _t(3 << 20, dt), ko) == UNSUPPORTED
+    assert _call(_t(dtype=2), None, _t(dtype=2), None) == UNSUPPORTED
+    for rot in (0, 1, 63, 66, -2):
+        assert _call(q, k, qo, ko, rotary=B.SiftRotary(1, rot, 0, 1.0)) == SHAPE
+    assert _call(q, k, qo, ko, rotary=B.SiftRotary(None, 64, 0, 1.0)) == NULL
+    for m in (0.0, -1.0, math.inf, math.nan):
+        assert _call(q, k, qo, ko, rotary=B.SiftRotary(1, 64, 0, m)) == UNSUPPORTED
+    # 3 * 4 * 64 * 2 = 1536 bytes of q
+    assert _call(q, k, _t((1 << 20) + 1535), ko) == UNSUPPORTED
+    assert _call(q, k, qo, _t((3 << 20) + 16, heads=2)) == UNSUPPORTED
+    assert _call(q, k, qo, _t(1 << 20, heads=2)) == UNSUPPORTED
+    assert _call(q, _t(3 << 20, heads=2), qo, ko) == UNSUPPORTED
+    big = _t(tokens=1, heads=1 << 25)
+    assert _call(big, None, big, None) == CAPACITY
+
+
+def test_nothing_to_do():
+    q = _t(None, tokens=0)
+    assert _call(q, None, q, None, pos=None) in (0,)
