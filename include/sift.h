@@ -74,7 +74,9 @@ typedef enum sift_status {
   SIFT_E_PLAN = 7         /* the plan does not match the arguments            */
 } sift_status;
 
-typedef enum sift_dtype { SIFT_F32 = 0, SIFT_BF16 = 1 } sift_dtype;
+/* SIFT_E4M3: 8-bit floats (OCP: 4 bits of exponent, 3 of mantissa, no infinities), only
+ * where a call says so. */
+typedef enum sift_dtype { SIFT_F32 = 0, SIFT_BF16 = 1, SIFT_E4M3 = 2 } sift_dtype;
 
 /* A dense device tensor [tokens][heads][head_dim]. */
 typedef struct sift_tensor {

@@ -130,6 +130,10 @@ typedef struct sift_cache_kv {
   const int32_t* lens;         /* [num_seqs], 0 .. max_pages * page              */
   const int32_t* page_lens;    /* [num_seqs][max_pages], or NULL: full pages     */
   const int32_t* key_pos;      /* [num_seqs][Hkv][max_pages * page], or NULL     */
+  /* Read with SIFT_E4M3 pools only (programs built without them pass none): a key is
+   * its pool row times its page's and kv head's scale. */
+  float* k_scales;             /* [num_pages][Hkv]                               */
+  float* v_scales;
 } sift_cache_kv;
 
 /* The new tokens of the sequences, rows row_ptr[b] .. row_ptr[b+1]-1 (at most
@@ -168,7 +172,8 @@ sift_status sift_cache_destroy(sift_cache* cache);
  * token, a chain or a drafted tree for each sequence, in one call.
  *   q, out       [rows][Hq][D];  k_new, v_new: [rows][Hkv][D], the new tokens'
  *                own keys, which the cache does not hold yet.  All tensors and
- *                the pools SIFT_BF16 or all SIFT_F32, 16-byte aligned.
+ *                the pools SIFT_BF16 or all SIFT_F32, 16-byte aligned; with pools of
+ *                SIFT_E4M3 (under any scales) all others SIFT_BF16.
  *   tree_mask    device uint64 [rows][mask_words], mask_words >=
  *                ceil(max_rows / 64): bit j % 64 of word j / 64 says whether the
  *                row sees new token j of its sequence (its ancestors and
@@ -195,6 +200,40 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
                                  const uint64_t* tree_mask, int32_t mask_words,
                                  const sift_score* score, sift_tensor* out, float* lse,
                                  void* stream);
+
+/*
+ * New keys and values of every sequence into its pages, the keys turned by their
+ * positions on the way.
+ *   k, v         [rows][Hkv][D], 16-byte aligned, the pools' type; SIFT_BF16 where the
+ *                pools are SIFT_E4M3.  They overlap no pool.
+ *   new_rows     row_ptr: any number of rows of a sequence (max_rows is not meant);
+ *                row_pos: the keys' positions
+ *   rotary       how the keys turn, or NULL: as they are
+ *   slots        device int32 [rows]: the slot of its sequence that a row goes to (none
+ *                twice), or NULL: lens[b] and on, in order.  Not with SIFT_E4M3.
+ *                row_pos NULL: a row's position is its slot.
+ *   pos_out      device int32 [num_seqs][Hkv][max_pages * page], may be the key_pos, or
+ *                NULL: receives the positions of the slots that are written
+ *   lens_out     device int32 [num_seqs], may be the lens (a second, small launch), or
+ *                NULL: the lens of the next calls.  Without slots only.
+ * Rows past a sequence's last slot are left out.  page_lens are neither read nor
+ * changed.  The pages that rows enter must be the sequence's own.
+ * SIFT_E4M3: a page's scale becomes the least power of two (2^-100 at least) such that
+ *   448 times it holds max |x| of the page's new rows of the head (of dims that turn,
+ *   sqrt(2) times that and the magnitude), or stays where the page held keys under a
+ *   larger one.  Where it grows the codes of the keys held are rounded again.  Values
+ *   that are not finite are held as NaN and take no part in the scale.  The first row
+ *   that enters a page begins it: whatever else it holds, and its scale, is forgotten.
+ * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, alignment, magnitude;
+ *   slots with lens_out or SIFT_E4M3; lens_out that overlaps the lens in part),
+ *   SIFT_E_CAPACITY (2^31 rows x kv heads, or (sequence, page, kv head) triples that
+ *   they could enter), SIFT_E_PLAN (another device is current), SIFT_E_HIP.
+ */
+sift_status sift_cache_append(sift_cache* cache, const sift_cache_kv* kv,
+                              const sift_cache_rows* new_rows, const sift_tensor* k,
+                              const sift_tensor* v, const sift_rotary* rotary,
+                              const int32_t* slots, int32_t* pos_out, int32_t* lens_out,
+                              void* stream);
 
 /*
  * Accumulated attention weights of the cached keys, what an eviction goes by:

@@ -18,6 +18,7 @@ SERVE_HEADER = os.path.join(os.path.dirname(HERE), "include", "sift_serve.h")
 
 SIFT_F32 = 0
 SIFT_BF16 = 1
+SIFT_E4M3 = 2
 
 STATUS = {
     0: "SIFT_OK", 1: "SIFT_E_NULL", 2: "SIFT_E_SHAPE", 3: "SIFT_E_LAYOUT",
@@ -60,7 +61,8 @@ class SiftScore(ctypes.Structure):
 class SiftCacheKv(ctypes.Structure):
     _fields_ = [("k_pages", ctypes.POINTER(SiftTensor)), ("v_pages", ctypes.POINTER(SiftTensor)),
                 ("page_table", ctypes.c_void_p), ("lens", ctypes.c_void_p),
-                ("page_lens", ctypes.c_void_p), ("key_pos", ctypes.c_void_p)]
+                ("page_lens", ctypes.c_void_p), ("key_pos", ctypes.c_void_p),
+                ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
 
 
 class SiftCacheRows(ctypes.Structure):
@@ -145,6 +147,10 @@ _SERVE_SIGS = {
                                             ctypes.POINTER(SiftTensor), _P, ctypes.c_int32,
                                             ctypes.POINTER(SiftScore), ctypes.POINTER(SiftTensor),
                                             _P, _P]),
+    "sift_cache_append": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv),
+                                         ctypes.POINTER(SiftCacheRows),
+                                         ctypes.POINTER(SiftTensor), ctypes.POINTER(SiftTensor),
+                                         ctypes.POINTER(SiftRotary), _P, _P, _P, _P]),
     "sift_cache_accumulate": (ctypes.c_int, [_P, ctypes.POINTER(SiftCacheKv),
                                              ctypes.POINTER(SiftCacheRows),
                                              ctypes.POINTER(SiftTensor), _P, _P,
@@ -215,7 +221,8 @@ def _torch():
     return _torch_module
 
 
-def tensor_desc(t) -> SiftTensor:
+def tensor_desc(t, kind=None) -> SiftTensor:
+    """kind: the library's number of the type, where it is not one of most calls'."""
     _torch()
     if not getattr(t, "is_cuda", False):
         raise SiftError("tensor_desc", 4, "tensors must be in GPU memory")
@@ -224,7 +231,8 @@ def tensor_desc(t) -> SiftTensor:
         raise ValueError("expected a [tokens, heads, head_dim] tensor")
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    kind = _kinds.get(t.dtype)
+    if kind is None:
+        kind = _kinds.get(t.dtype)
     if kind is None:
         raise ValueError(f"unsupported dtype {t.dtype}")
     return SiftTensor(t.data_ptr(), kind, *shape)
@@ -851,11 +859,14 @@ class CachePages:
     v_pages [num_pages * page, Hkv, D], page_table int32 [seqs, max_pages], lens
     int32 [seqs]; page_lens int32 [seqs, max_pages] where pages end early, key_pos
     int32 [seqs, Hkv, max_pages * page] where a key's position is not its slot.
+    Pools of torch.float8_e4m3fn go with k_scales and v_scales, float32 [num_pages,
+    Hkv]: a key is its row times its page's and head's scale.
     The tensors are used where they are: write into them, or make another."""
 
-    def __init__(self, k_pages, v_pages, page_table, lens, page_lens=None, key_pos=None):
+    def __init__(self, k_pages, v_pages, page_table, lens, page_lens=None, key_pos=None,
+                 k_scales=None, v_scales=None):
         fn = "CachePages"
-        kd, vd = tensor_desc(k_pages), tensor_desc(v_pages)
+        kd, vd = _pool_desc(k_pages), _pool_desc(v_pages)
         dev = k_pages.device
         for name, t in (("page_table", page_table), ("lens", lens), ("page_lens", page_lens),
                         ("key_pos", key_pos)):
@@ -863,14 +874,31 @@ class CachePages:
                 require(fn, t, name, "int32", 1, dev)
         if v_pages.device != dev:
             raise SiftError(fn, 7, f"v_pages is on {v_pages.device}, k_pages on {dev}")
+        codes = kd.dtype == SIFT_E4M3
+        for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if codes:
+                require(fn, t, name, "float32", 1, dev)
+            elif t is not None:
+                raise SiftError(fn, 4, f"{name} with pools of {k_pages.dtype}")
         self.k_pages, self.v_pages, self.page_table, self.lens = k_pages, v_pages, page_table, lens
         self.page_lens, self.key_pos = page_lens, key_pos
-        self._held = (k_pages, v_pages, page_table, lens, page_lens, key_pos, kd, vd)
+        self.k_scales, self.v_scales = k_scales, v_scales
+        self._held = (k_pages, v_pages, page_table, lens, page_lens, key_pos, kd, vd, k_scales,
+                      v_scales)
         self.sizes = (dev, *(None if t is None else (t.numel(), t.shape)
                              for t in (page_table, lens, page_lens, key_pos)))
+        ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
-                                  lens.data_ptr(), 0 if page_lens is None else page_lens.data_ptr(),
-                                  0 if key_pos is None else key_pos.data_ptr())
+                                  lens.data_ptr(), ptr(page_lens), ptr(key_pos), ptr(k_scales),
+                                  ptr(v_scales))
+
+
+def _pool_desc(t) -> SiftTensor:
+    """tensor_desc, of e4m3 too."""
+    torch = _torch()
+    if getattr(t, "dtype", None) is not torch.float8_e4m3fn:
+        return tensor_desc(t)
+    return tensor_desc(t, SIFT_E4M3)
 
 
 class Cache:
@@ -922,6 +950,11 @@ class Cache:
             if t[0] < n:
                 raise SiftError(fn, 5, f"{name} holds {t[0]} elements, needs {n}")
             check_laid_out(fn, name, t[1], sizes)
+        if kv.k_scales is not None:
+            sizes = (kv.k_pages.shape[0] // self.page, self.hkv)
+            for name, t in (("k_scales", kv.k_scales), ("v_scales", kv.v_scales)):
+                if t.shape != sizes:
+                    require_laid_out(fn, t, name, "float32", sizes, self.device)
         return kv.struct
 
     def _rows(self, fn, q, row_ptr, row_pos):
@@ -962,6 +995,37 @@ class Cache:
 
     def _slot_buffer(self, fn, t, name, dtype="float32"):
         require_laid_out(fn, t, name, dtype, self._slot_sizes, self.device)
+
+    def append(self, kv, k, v, row_ptr=None, row_pos=None, rotary=None, slots=None, pos_out=None,
+               lens_out=None, stream=None):
+        """New keys and values k, v [rows, Hkv, D] into the sequences' pages, behind those
+        that they hold (sift_cache_append); returns lens_out, the lens of the cache then
+        (int32 [seqs]; new when None, may be kv.lens).  row_ptr int32 [seqs + 1] delimits
+        the sequences' rows (None: as many of each), row_pos int32 [rows] holds the keys'
+        positions (None: their slots), rotary the Rotary that turns them (None: as they
+        are).  slots: int32 [rows], where the rows go instead; then lens_out is not
+        written, and nothing returned.  pos_out: int32 [seqs, Hkv, max_pages * page] that
+        receives the positions, kv.key_pos when None."""
+        torch = _torch()
+        fn, dev = "sift_cache_append", self.device
+        rows = self._rows(fn, k, row_ptr, row_pos)
+        if rotary is not None and rotary.device != dev:
+            raise SiftError(fn, 7, f"the rotary is on {rotary.device}, the cache on {dev}")
+        if slots is not None:
+            require(fn, slots, "slots", "int32", k.shape[0], dev)
+        if pos_out is None:
+            pos_out = kv.key_pos
+        if pos_out is not None:
+            self._slot_buffer(fn, pos_out, "pos_out", "int32")
+        if lens_out is not None:
+            require(fn, lens_out, "lens_out", "int32", self.num_seqs, dev)
+        elif slots is None:
+            lens_out = _empty((self.num_seqs,), torch.int32, dev, stream)
+        check(fn, lib().sift_cache_append(
+            self._h, self._kv(fn, kv), rows, _desc(fn, k, "k", dev), _desc(fn, v, "v", dev),
+            None if rotary is None else rotary.struct, _address(slots), _address(pos_out),
+            _address(lens_out), _stream_ptr(stream)))
+        return lens_out
 
     def accumulate(self, q, lse, kv, weights=None, decay=1.0, row_ptr=None, row_pos=None,
                    row_weight=None, scale=None, cap=0.0, slopes=None, out=None, stream=None):

@@ -1,6 +1,6 @@
 // C ABI of the page cache (include/sift_serve.h): the handle with its scratch,
 // and the host checks of its calls.  The kernels are in cache_attn.hip,
-// cache_weights.hip and cache_evict.hip.
+// cache_append.hip, cache_weights.hip and cache_evict.hip.
 
 #include <hip/hip_runtime.h>
 
@@ -11,6 +11,7 @@
 #include <limits>
 #include <new>
 
+#include "rotary_api.h"
 #include "score_api.h"
 #include "sift.h"
 #include "sift_internal.h"
@@ -48,14 +49,17 @@ sift_status check_tensor(const sift_tensor* t, int32_t tokens, int32_t heads, in
   if (t == nullptr) return SIFT_E_NULL;
   if (t->data == nullptr && static_cast<int64_t>(t->tokens) * t->heads * t->head_dim > 0)
     return SIFT_E_NULL;
-  if (t->dtype != SIFT_F32 && t->dtype != SIFT_BF16) return SIFT_E_UNSUPPORTED;
+  if (t->dtype != SIFT_F32 && t->dtype != SIFT_BF16 && t->dtype != SIFT_E4M3)
+    return SIFT_E_UNSUPPORTED;
   if (t->tokens != tokens || t->heads != heads || t->head_dim != dim) return SIFT_E_SHAPE;
   if (t->dtype != dtype || !aligned16(t->data)) return SIFT_E_UNSUPPORTED;
   return SIFT_OK;
 }
 
-// The cache's own arguments; a's device-side view of them.
-sift_status check_kv(const sift_cache* c, const sift_cache_kv* kv, sift::CacheArgs* a) {
+// The cache's own arguments; a's device-side view of them.  codes: the call takes pools
+// of e4m3.
+sift_status check_kv(const sift_cache* c, const sift_cache_kv* kv, sift::CacheArgs* a,
+                     bool codes = false) {
   if (c == nullptr || kv == nullptr || kv->k_pages == nullptr || kv->v_pages == nullptr)
     return SIFT_E_NULL;
   const int32_t rows = kv->k_pages->tokens, dtype = kv->k_pages->dtype;
@@ -64,6 +68,10 @@ sift_status check_kv(const sift_cache* c, const sift_cache_kv* kv, sift::CacheAr
   if ((st = check_tensor(kv->k_pages, rows, c->hkv, c->head_dim, dtype)) != SIFT_OK) return st;
   if ((st = check_tensor(kv->v_pages, rows, c->hkv, c->head_dim, dtype)) != SIFT_OK) return st;
   if (kv->page_table == nullptr || kv->lens == nullptr) return SIFT_E_NULL;
+  if (dtype == SIFT_E4M3) {
+    if (!codes) return SIFT_E_UNSUPPORTED;
+    if (kv->k_scales == nullptr || kv->v_scales == nullptr) return SIFT_E_NULL;
+  }
   if (!aligned16(kv->key_pos)) return SIFT_E_UNSUPPORTED;
   int dev = -1;
   if (hipGetDevice(&dev) != hipSuccess) return SIFT_E_HIP;
@@ -108,6 +116,9 @@ bool overlap(const void* p, const void* q, size_t n) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return q != nullptr && a < b + n && b < a + n;
 }
+
+// The type of a call's other tensors.
+int32_t type_beside(int32_t pools) { return pools == SIFT_E4M3 ? SIFT_BF16 : pools; }
 
 // Workgroups of the attention: two to a CU (one where its LDS allows no more).
 int32_t attn_groups(const sift_cache* c, bool bf16) {
@@ -227,6 +238,55 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   a.groups = attn_groups(cache, bf16);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   const hipError_t e = sift::launch_cache_attn(a, bf16, d, s);
+  cache->last_stream = s;
+  return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
+}
+
+sift_status sift_cache_append(sift_cache* cache, const sift_cache_kv* kv,
+                              const sift_cache_rows* new_rows, const sift_tensor* k,
+                              const sift_tensor* v, const sift_rotary* rotary,
+                              const int32_t* slots, int32_t* pos_out, int32_t* lens_out,
+                              void* stream) {
+  sift::CacheAppendArgs a{};
+  sift_status st;
+  if ((st = check_kv(cache, kv, &a.c, true)) != SIFT_OK) return st;
+  if (k == nullptr) return SIFT_E_NULL;
+  const int32_t rows = k->tokens, dtype = kv->k_pages->dtype;
+  if (rows < 0) return SIFT_E_SHAPE;
+  for (const sift_tensor* t : {k, v})
+    if ((st = check_tensor(t, rows, cache->hkv, cache->head_dim, type_beside(dtype))) != SIFT_OK)
+      return st;
+  a.c.row_ptr = new_rows != nullptr ? new_rows->row_ptr : nullptr;
+  a.c.row_pos = new_rows != nullptr ? new_rows->row_pos : nullptr;
+  if (a.c.row_ptr == nullptr && rows % cache->num_seqs != 0) return SIFT_E_SHAPE;
+  a.c.rows = a.c.max_rows = rows;
+  if (rotary != nullptr && (st = sift::make_rotary(rotary, cache->head_dim, &a.r)) != SIFT_OK)
+    return st;
+  if (slots != nullptr && (lens_out != nullptr || dtype == SIFT_E4M3)) return SIFT_E_UNSUPPORTED;
+  const size_t small = static_cast<size_t>(cache->num_seqs) * 4;
+  if (lens_out != kv->lens && overlap(lens_out, kv->lens, small)) return SIFT_E_UNSUPPORTED;
+  if (static_cast<int64_t>(rows) * cache->hkv >= int64_t(1) << 31 ||
+      sift::cache_append_units(a) >= int64_t(1) << 31)
+    return SIFT_E_CAPACITY;
+  a.d = cache->head_dim;
+  a.k = k->data;
+  a.v = v->data;
+  a.k_pages = kv->k_pages->data;
+  a.v_pages = kv->v_pages->data;
+  if (dtype == SIFT_E4M3) {
+    a.k_scales = kv->k_scales;
+    a.v_scales = kv->v_scales;
+  }
+  a.slots = slots;
+  a.pos_out = pos_out;
+  a.lens_out = lens_out;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = sift::launch_cache_append(
+      a,
+      dtype == SIFT_E4M3 ? sift::Pool::kE4m3
+      : dtype == SIFT_BF16 ? sift::Pool::kBf16
+                           : sift::Pool::kF32,
+      s);
   cache->last_stream = s;
   return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
 }

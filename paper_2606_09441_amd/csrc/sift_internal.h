@@ -517,6 +517,29 @@ int64_t cache_weights_steps(const CacheArgs& a);
 hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int cus,
                                 hipStream_t stream);
 
+// What the pools hold: numbers, or e4m3 codes with a scale for each page and kv head.
+enum class Pool { kF32, kBf16, kE4m3 };
+
+// New keys and values into the pages (cache_append.hip); c's q and max_rows are not the
+// caller's: a sequence may have all rows.
+struct CacheAppendArgs {
+  CacheArgs c;
+  RotaryArgs r;              // half 0: the keys do not turn
+  int32_t d;
+  const void* k;             // [rows][hkv][d]
+  const void* v;
+  void* k_pages;
+  void* v_pages;
+  float* k_scales;           // [num_pages][hkv], with codes
+  float* v_scales;
+  const int32_t* slots;      // [rows] or nullptr: lens[b] and on
+  int32_t* pos_out;          // [num_seqs][hkv][slots] or nullptr
+  int32_t* lens_out;         // [num_seqs] or nullptr, may be c.lens
+};
+// Pages and heads that rows may enter at most: fewer than 2^31.
+int64_t cache_append_units(const CacheAppendArgs& a);
+hipError_t launch_cache_append(CacheAppendArgs a, Pool pool, hipStream_t stream);
+
 // Eviction (cache_evict.hip): a selection per (sequence, kv head), then the
 // moves of the K and V rows that it lists.
 struct CacheEvictArgs {
