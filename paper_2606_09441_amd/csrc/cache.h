@@ -17,6 +17,11 @@ __device__ __forceinline__ int32_t scalar(const int32_t* p, int64_t i) {
   return ((ptr)p)[i];
 }
 
+__device__ __forceinline__ float scalar(const float* p, int64_t i) {
+  typedef const __attribute__((address_space(4))) float* ptr;
+  return ((ptr)p)[i];
+}
+
 struct Seq {
   int32_t len;   // slots
   int32_t row0;  // first new token

@@ -120,6 +120,12 @@ bool overlap(const void* p, const void* q, size_t n) {
 // The type of a call's other tensors.
 int32_t type_beside(int32_t pools) { return pools == SIFT_E4M3 ? SIFT_BF16 : pools; }
 
+sift::Pool pool_of(int32_t pools) {
+  return pools == SIFT_E4M3   ? sift::Pool::kE4m3
+         : pools == SIFT_BF16 ? sift::Pool::kBf16
+                              : sift::Pool::kF32;
+}
+
 // Workgroups of the attention: two to a CU (one where its LDS allows no more).
 int32_t attn_groups(const sift_cache* c, bool bf16) {
   return c->cus * (!bf16 && c->head_dim == 128 ? 1 : 2);
@@ -215,8 +221,8 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
                                  void* stream) {
   sift::CacheAttnArgs a{};
   sift_status st;
-  if ((st = check_kv(cache, kv, &a.c)) != SIFT_OK) return st;
-  const int32_t dtype = kv->k_pages->dtype;
+  if ((st = check_kv(cache, kv, &a.c, true)) != SIFT_OK) return st;
+  const int32_t pools = kv->k_pages->dtype, dtype = type_beside(pools);
   if ((st = check_rows(cache, new_rows, q, dtype, score, sift::kUnitLog2e, &a.c)) != SIFT_OK)
     return st;
   const int32_t rows = q->tokens, d = cache->head_dim;
@@ -234,10 +240,13 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   a.lse = lse;
   a.part_o = cache->part_o;
   a.part_ml = cache->part_ml;
-  const bool bf16 = dtype == SIFT_BF16;
-  a.groups = attn_groups(cache, bf16);
+  if (pools == SIFT_E4M3) {
+    a.k_scales = kv->k_scales;
+    a.v_scales = kv->v_scales;
+  }
+  a.groups = attn_groups(cache, dtype == SIFT_BF16);
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = sift::launch_cache_attn(a, bf16, d, s);
+  const hipError_t e = sift::launch_cache_attn(a, pool_of(pools), d, s);
   cache->last_stream = s;
   return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
 }
@@ -281,12 +290,7 @@ sift_status sift_cache_append(sift_cache* cache, const sift_cache_kv* kv,
   a.pos_out = pos_out;
   a.lens_out = lens_out;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const hipError_t e = sift::launch_cache_append(
-      a,
-      dtype == SIFT_E4M3 ? sift::Pool::kE4m3
-      : dtype == SIFT_BF16 ? sift::Pool::kBf16
-                           : sift::Pool::kF32,
-      s);
+  const hipError_t e = sift::launch_cache_append(a, pool_of(dtype), s);
   cache->last_stream = s;
   return e == hipSuccess ? SIFT_OK : SIFT_E_HIP;
 }

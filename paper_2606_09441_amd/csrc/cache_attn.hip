@@ -310,13 +310,14 @@ int64_t cache_attn_steps(const CacheArgs& a) {
   return units >= int64_t(1) << 31 ? units : units * steps;
 }
 
-hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream) {
+hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hipStream_t stream) {
   if (a.c.rows == 0) return hipSuccess;
   const int64_t items = static_cast<int64_t>(a.c.rows) * a.c.hq;
   if (items >= int64_t(1) << 24) return hipErrorInvalidValue;  // fewer than 2^32 threads
   const int64_t most = static_cast<int64_t>(std::min(a.c.rows, a.c.max_rows)) * (a.c.hq / a.c.hkv);
+  const bool codes = pool == Pool::kE4m3;
   const bool wide = cache_attn_wide(
-      bf16, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
+      pool == Pool::kBf16, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
@@ -332,17 +333,21 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hi
         return hipGetLastError();
       }
     }
-    {
+    hipError_t e;
+    if (codes) {
+      e = launch_cache_codes(a, D, stream);
+    } else {
       hipLaunchKernelGGL((cache_attn_kernel<T, D>), dim3(a.groups), block, 0, stream, a);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-      hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a, each);
+      e = hipGetLastError();
     }
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a, each);
     return hipGetLastError();
   };
   using D64 = std::integral_constant<int, 64>;
   using D128 = std::integral_constant<int, 128>;
-  if (bf16) return head_dim == 128 ? launch(__bf16{}, D128{}) : launch(__bf16{}, D64{});
+  if (pool != Pool::kF32)
+    return head_dim == 128 ? launch(__bf16{}, D128{}) : launch(__bf16{}, D64{});
   return head_dim == 128 ? launch(float{}, D128{}) : launch(float{}, D64{});
 }
 

@@ -476,8 +476,13 @@ struct CacheArgs {
   ScoreArgs sc;
 };
 
+// What the pools hold: numbers, or e4m3 codes with a scale for each page and kv head.
+enum class Pool { kF32, kBf16, kE4m3 };
+
 struct CacheAttnArgs {
   CacheArgs c;
+  const float* k_scales;     // [num_pages][hkv], with codes
+  const float* v_scales;
   const void* k_new;         // [rows][hkv][D]
   const void* v_new;
   const uint64_t* tree_mask; // [rows][mask_words] or nullptr: a row sees those up to itself
@@ -499,7 +504,8 @@ constexpr int kCacheRows = 32, kCacheWideRows = 128;
 bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys);
 int64_t cache_attn_steps(const CacheArgs& a);
 hipError_t launch_cache_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
-hipError_t launch_cache_attn(const CacheAttnArgs& a, bool bf16, int head_dim, hipStream_t stream);
+hipError_t launch_cache_codes(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
+hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hipStream_t stream);
 
 // Accumulated attention weights (cache_weights.hip); c.sc in the natural domain.
 struct CacheWeightArgs {
@@ -516,9 +522,6 @@ struct CacheWeightArgs {
 int64_t cache_weights_steps(const CacheArgs& a);
 hipError_t launch_cache_weights(CacheWeightArgs a, bool bf16, int head_dim, int cus,
                                 hipStream_t stream);
-
-// What the pools hold: numbers, or e4m3 codes with a scale for each page and kv head.
-enum class Pool { kF32, kBf16, kE4m3 };
 
 // New keys and values into the pages (cache_append.hip); c's q and max_rows are not the
 // caller's: a sequence may have all rows.

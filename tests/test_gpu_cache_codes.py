@@ -1,0 +1,354 @@
+"""GPU: attention over a paged cache held in e4m3 (sift_cache_attention with SIFT_E4M3
+pools) against the fp64 oracle on the numbers that the codes stand for.  Pool rows that
+hold no key are NaN codes.
+
+Codes and scales come as they are, so the errors are the bf16 attention's: the weights are
+rounded to bf16 in the numerator and in the denominator alike, each by 2^-8 of itself, and
+the output by 2^-8: |out| 2^-8 + 2 2^-8 sum w |v|, and 1e-5 for the fp32 sums and scores
+(1e-4 of the log sum, as of the other caches)."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from cache_helpers import Batch, random_tree, some_empty
+from gpu_helpers import device, max_abs, say
+from oracle import serve_oracle as S
+
+pytestmark = pytest.mark.gpu
+
+E4M3 = torch.float8_e4m3fn
+LSE_TOL = 1e-4
+
+
+class Codes(Batch):
+    """A Batch whose pools are e4m3 codes; k and v stay the numbers, for the oracle."""
+
+    def __init__(self, lens, new, hq, hkv, d, page=64, *a, powers=False, **kw):
+        super().__init__(lens, new, hq, hkv, d, "bf16", page, *a, **kw)
+        rng = np.random.default_rng(kw.get("seed", 0) + 100)
+        self.codes, self.scales = {}, {}
+        for name in "kv":
+            x = getattr(self, name).float().view(-1, page, hkv, d)
+            top = torch.nan_to_num(x.abs(), nan=0.0).amax((1, 3))
+            scale = torch.where(top > 0, top / 448, 1.0)
+            if powers:
+                scale = torch.exp2(torch.ceil(torch.log2(scale)))
+            else:   # some with more room than they need
+                more = torch.from_numpy(rng.uniform(1, 3, scale.shape).astype(np.float32))
+                scale = scale * more.to(scale.device)
+            codes = (x / scale[:, None, :, None]).to(E4M3)
+            self.codes[name] = codes.view(-1, hkv, d)
+            self.scales[name] = scale.contiguous()
+            setattr(self, name, (codes.float() * scale[:, None, :, None]).view(-1, hkv, d))
+
+    def pages(self):
+        from paper_2606_09441_amd import CachePages
+        return CachePages(self.codes["k"], self.codes["v"], self.t["table"], self.t["lens"],
+                          page_lens=self.t["page_lens"], key_pos=self.t["key_pos"],
+                          k_scales=self.scales["k"], v_scales=self.scales["v"])
+
+
+def check(x, cap=0.0, bias=False, scale=None, row_ptr=True, name=""):
+    slopes = (2.0 ** (-4.0 * np.arange(1, x.hq + 1) / x.hq)).astype(np.float32) if bias else None
+    lse = torch.full((x.rows, x.hq), 7.0, device=x.q.device)
+    out = torch.full_like(x.q, 7.0)
+    with x.cache() as cache:
+        cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"] if row_ptr else None,
+                        tree_mask=x.mask, row_pos=x.t["row_pos"], scale=scale, cap=cap,
+                        slopes=None if slopes is None else torch.from_numpy(slopes).to(x.q.device),
+                        out=out, lse=lse)
+        torch.cuda.synchronize()
+    ref, ref_lse = x.oracle(scale=scale, cap=cap, slopes=slopes)
+    v, v_new = x.v, x.v_new
+    x.v, x.v_new = v.abs(), v_new.abs()
+    size, _ = x.oracle(scale=scale, cap=cap, slopes=slopes)
+    x.v, x.v_new = v, v_new
+    out, lse = out.float().cpu().numpy(), lse.cpu().numpy()
+    none = np.isneginf(ref_lse)
+    assert np.array_equal(none, np.isneginf(lse))
+    assert not out[none].any()
+    bound = np.abs(ref) * 2.0 ** -8 + size * 2.0 ** -7 + 1e-5
+    e, el = float((np.abs(out - ref) / bound).max()), max_abs(lse[~none], ref_lse[~none])
+    say(f"[codes] {name}: {e:.2f} of the bound, lse {el:.2e}")
+    assert e <= 1 and el <= LSE_TOL
+    return out, lse
+
+
+LENS = [0, 1, 15, 16, 17, 31, 33, 64, 127, 129, 300, 700]
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+def test_single_tokens(d, page):
+    check(Codes(LENS, [1] * len(LENS), 8, 2, d, page), row_ptr=False)
+    check(Codes(LENS, [1] * len(LENS), 8, 2, d, page, gaps=True), cap=20.0)
+
+
+@pytest.mark.parametrize("d", [128, 64])
+@pytest.mark.parametrize("tree", [None, random_tree, some_empty])
+def test_trees(d, tree):
+    new = [5, 0, 1, 33, 3, 2, 64, 12, 0, 1, 20, 40]
+    for gaps, moved, cap, bias in [(False, False, 0.0, False), (True, True, 0.0, True),
+                                   (True, False, 30.0, False), (False, True, 20.0, True),
+                                   (False, False, 0.0, True)]:
+        check(Codes(LENS, new, 6, 2, d, 32, gaps, moved, tree, seed=3), cap, bias,
+              name=f"gaps {gaps} moved {moved} cap {cap} bias {bias}")
+
+
+def test_many_new_tokens():
+    check(Codes([40, 0, 513], [130, 65, 200], 4, 1, 128, tree=random_tree, seed=4))
+    check(Codes([40, 0], [150, 90], 4, 4, 64, seed=5))
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (8, 8), (5, 1), (12, 3), (64, 1), (40, 1), (20, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_head_layouts(hq, hkv, d):
+    check(Codes([200, 0, 77], [3, 1, 2], hq, hkv, d, seed=6), bias=d == 64)
+
+
+def test_many_sequences():
+    rng = np.random.default_rng(7)
+    lens = rng.integers(0, 90, 150).tolist()
+    for most, hq in ((3, 4), (12, 16)):
+        new = [int(rng.integers(0, most)) for _ in lens]
+        check(Codes(lens, new, hq, 2, 64, 16, tree=random_tree, seed=7))
+
+
+@pytest.mark.parametrize("powers", [False, True])
+def test_long_cache(powers):
+    """Every workgroup shares units with others."""
+    check(Codes([20000, 7], [1, 1], 4, 1, 128, 128, seed=8, powers=powers))
+    check(Codes([9000], [21], 8, 2, 64, 16, tree=random_tree, gaps=True, seed=9, powers=powers),
+          cap=50.0)
+
+
+# as those of the bf16 caches that go by units of 128 rows
+WIDE = ([9000, 300, 0], [100, 40, 3])
+MANY = [(None, False, False, 0.0, False), (random_tree, True, False, 0.0, False),
+        (some_empty, False, False, 30.0, False), (random_tree, False, True, 0.0, True),
+        (None, True, True, 20.0, True)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tree,gaps,moved,cap,bias", MANY)
+def test_many_rows_over_long_caches(d, tree, gaps, moved, cap, bias):
+    check(Codes(*WIDE, 8, 1, d, 128, gaps, moved, tree, seed=16, extra_pages=16), cap, bias)
+
+
+@pytest.mark.parametrize("hq,hkv,page", [(8, 2, 128), (9, 3, 32), (16, 8, 16)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tree,gaps,moved,cap,bias", MANY)
+def test_many_rows_of_several_kv_heads(hq, hkv, page, d, tree, gaps, moved, cap, bias):
+    check(Codes([5000, 300, 0], WIDE[1], hq, hkv, d, page, gaps, moved, tree, seed=21,
+                extra_pages=47 * 128 // page), cap, bias)
+
+
+@pytest.mark.parametrize("gaps,moved,cap,bias", [(False, False, 0.0, False), (True, False, 0.0, False),
+                                                 (False, True, 0.0, True), (False, False, 20.0, True)])
+def test_many_rows_of_many_sequences(gaps, moved, cap, bias):
+    rng = np.random.default_rng(22)
+    lens = rng.integers(0, 300, 70).tolist()
+    new = rng.integers(0, 21, 70).tolist()
+    lens[5], new[3], new[66] = 0, 20, 0
+    check(Codes(lens, new, 8, 2, 64, 128, gaps, moved, random_tree, seed=22, extra_pages=16), cap,
+          bias)
+
+
+def test_scales_far_apart():
+    """Pages of values 2^-60 to 2^60 beside each other, and one under a scale of 0."""
+    for rows in (2, 60):
+        x = Codes([600, 90], [rows, 3], 8, 2, 128, 64, seed=30, extra_pages=200)
+        for name in "kv":
+            s = x.scales[name]
+            by = torch.exp2(torch.randint(-60, 8 if name == "k" else 60, s.shape).float()).to(s.device)
+            if name == "k":
+                by[int(x.table[0, 2])] = 0
+            x.scales[name] = s * by
+            val = getattr(x, name).view(-1, 64, 2, 128) * by[:, None, :, None]
+            setattr(x, name, val.reshape(-1, 2, 128))
+        check(x, name="far apart")
+
+
+@pytest.mark.parametrize("value", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("many", [False, True])
+def test_unseen_new_tokens_do_not_matter(value, many):
+    """A drafted token with such values reaches the rows that see it and no other; NaN
+    codes of a cached key reach every row of their head."""
+    if many:
+        x = Codes(*WIDE, 8, 1, 64, 128, tree=random_tree, seed=17, extra_pages=16)
+    else:
+        x = Codes([70, 0], [9, 40], 4, 1, 128, tree=random_tree, seed=12)
+    for bad in (3, int(x.row_ptr[1]) + 20):
+        x.v_new[bad, 0, 5:9] = value
+    run = lambda cache: cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"],  # noqa: E731
+                                        tree_mask=x.mask).float().cpu().numpy()
+    with x.cache() as cache:
+        out = run(cache)
+        with np.errstate(all="ignore"):
+            ref, _ = x.oracle()
+        fine = np.isfinite(ref)
+        assert np.array_equal(fine, np.isfinite(out))
+        assert max_abs(out[fine], ref[fine]) <= 2e-2
+        at = int(x.table[0, 0]) * x.page
+        x.codes["v"].view(torch.uint8)[at, 0, 11] = 0x7f
+        out = run(cache)
+        first = slice(0, int(x.row_ptr[1]))
+        assert np.isnan(out[first, :, 11]).all()
+        assert np.array_equal(np.isfinite(out[first])[..., 12:], fine[first][..., 12:])
+
+
+def test_rows_left_out():
+    x = Codes([50, 60], [4, 4], 4, 2, 64, seed=11)
+    out = torch.full_like(x.q, 7.0)
+    with x.cache() as cache:
+        whole = cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=x.t["row_ptr"])
+        ptr = torch.tensor([0, 4, 6], dtype=torch.int32, device=x.q.device)
+        cache.attention(x.q, x.k_new, x.v_new, x.pages(), row_ptr=ptr, out=out)
+    assert torch.equal(out[:6], whole[:6]) and bool((out[6:] == 7).all())
+
+
+@pytest.mark.parametrize("many", [False, True])
+def test_streams_and_repeats(many):
+    """The same bits on another stream and in a captured graph, whose replays follow the
+    tables' and scales' present contents."""
+    if many:
+        x = Codes(*WIDE, 8, 1, 128, 128, tree=random_tree, seed=13, extra_pages=16)
+    else:
+        x = Codes([300, 41], [7, 7], 8, 2, 128, tree=random_tree, seed=13)
+    args = (x.q, x.k_new, x.v_new, x.pages())
+    with x.cache() as cache:
+        kw = dict(row_ptr=x.t["row_ptr"], tree_mask=x.mask)
+        first = cache.attention(*args, **kw)
+        torch.cuda.synchronize()
+        side = torch.cuda.Stream()
+        out = torch.zeros_like(first)
+        with torch.cuda.stream(side):
+            cache.attention(*args, out=out, **kw)
+        side.synchronize()
+        assert torch.equal(out, first)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            cache.attention(*args, out=out, **kw)
+        keep = x.scales["v"].clone()
+        for n, by in ((300, 1), (200, 2), (0, 1), (300, 0.5), (300, 1)):
+            x.t["lens"][0] = n
+            x.scales["v"].copy_(keep * by)
+            out.zero_()
+            graph.replay()
+            got = out.clone()
+            assert torch.equal(got, cache.attention(*args, **kw))
+        x.t["lens"][0] = int(x.lens[0])
+        assert torch.equal(first, cache.attention(*args, **kw))
+
+
+def test_offsets_beyond_32_bits():
+    """Pages at the far end of pools of more than 2^32 bytes: the same bits."""
+    from paper_2606_09441_amd import CachePages
+    x = Codes([300, 41], [3, 3], 16, 8, 128, 64, seed=15)
+    page, rows = x.page, (1 << 32) // (8 * 128) + 64 * 32
+    rows -= rows % page
+    far = rows // page - 1 - torch.arange(x.B * x.max_pages, device=x.q.device).view(x.B, -1)
+    near = x.t["table"].long().clamp(0, x.k.shape[0] // page - 1)
+    at = lambda t: (t.long()[..., None] * page + torch.arange(page, device=t.device)).flatten()  # noqa: E731
+    pools, scales = {}, {}
+    for n in "kv":
+        p = torch.empty(rows, 8, 128, dtype=torch.uint8, device=x.q.device)
+        p[at(far)] = x.codes[n].view(torch.uint8)[at(near)]
+        s = torch.zeros(rows // page, 8, device=x.q.device)
+        s[far.flatten()] = x.scales[n][near.flatten()]
+        pools[n], scales[n] = p.view(E4M3), s
+    big = CachePages(pools["k"], pools["v"], far.int().contiguous(), x.t["lens"],
+                     k_scales=scales["k"], v_scales=scales["v"])
+    with x.cache() as cache:
+        res = [cache.attention(x.q, x.k_new, x.v_new, kv, row_ptr=x.t["row_ptr"])
+               for kv in (x.pages(), big)]
+        torch.cuda.synchronize()
+    assert torch.equal(*res)
+
+
+def test_after_appends():
+    """Rotated keys appended to e4m3 pages, a prompt and then token by token, and attended
+    to: against the attention over the same keys in bf16 pages, to what the codes lose.
+
+    K is off by 2^-4 of itself at most, a score by sum |q k| 2^-4 scale < 0.2 for these
+    (|q| = |k| = sqrt(D) and the errors of unlike sign: a tenth of that at most); the
+    weights by a factor, V by 2^-4: a bound of 0.25 of the values' spread holds with room."""
+    from paper_2606_09441_amd import Cache, CachePages, Rotary
+    dev = device()
+    hq, hkv, d, page, pages = 8, 2, 128, 64, 6
+    gen = torch.Generator(dev).manual_seed(1)
+    normal = lambda n, h: torch.randn(n, h, d, generator=gen, device=dev).bfloat16()  # noqa: E731
+    rotary = Rotary((10000.0 ** (-torch.arange(64, device=dev, dtype=torch.float64) / 64)).float())
+    table = torch.randperm(2 * pages, device=dev, generator=gen).int().view(2, pages)
+    made = {}
+    for dt in (torch.bfloat16, E4M3):
+        pool = lambda: torch.zeros(2 * pages * page, hkv, d, device=dev).to(dt)  # noqa: E731
+        sc = lambda: torch.zeros(2 * pages, hkv, device=dev) if dt is E4M3 else None  # noqa: E731
+        made[dt] = CachePages(pool(), pool(), table, torch.zeros(2, dtype=torch.int32, device=dev),
+                              k_scales=sc(), v_scales=sc())
+    ptr = torch.tensor([0, 200, 290], dtype=torch.int32, device=dev)
+    k, v = normal(290, hkv), normal(290, hkv)
+    with Cache(2, hq, hkv, d, page=page, max_pages=pages) as cache:
+        for kv in made.values():
+            cache.append(kv, k, v, row_ptr=ptr, rotary=rotary, lens_out=kv.lens)
+        for step in range(70):
+            q, kn, vn = normal(2, hq), normal(2, hkv), normal(2, hkv)
+            pos = made[E4M3].lens.clone()
+            qr, kr = rotary.rotate(q, kn, pos)
+            outs = [cache.attention(qr, kr, vn, kv).float() for kv in made.values()]
+            for kv in made.values():
+                cache.append(kv, kn, vn, rotary=rotary, lens_out=kv.lens)
+            assert (outs[0] - outs[1]).abs().max() <= 0.25
+            # the same on the numbers that the codes stand for, to the attention's own errors
+            if step % 23 == 0:
+                kv = made[E4M3]
+                num = [(p.float().view(-1, page, hkv, d) * s[:, None, :, None]).view(-1, hkv, d)
+                       for p, s in ((kv.k_pages, kv.k_scales), (kv.v_pages, kv.v_scales))]
+                f = lambda t: t.float().cpu().numpy()  # noqa: E731
+                host = S.Pages(f(num[0]), f(num[1]), table.cpu().numpy(), pos.cpu().numpy(), page)
+                ref, _ = S.cache_attention(f(qr), f(kr), f(vn), host, np.array([0, 1, 2]))
+                assert max_abs(outs[1].cpu().numpy(), ref) <= 2e-2
+        assert made[E4M3].lens.tolist() == [270, 160]
+
+
+def test_refusals():
+    from paper_2606_09441_amd import CachePages, SiftError
+    x = Codes([100, 30], [2, 2], 4, 2, 128, seed=14)
+    kv = x.pages()
+
+    def refused(status, fn, *a, **kw):
+        with pytest.raises(SiftError) as e:
+            fn(*a, **kw)
+        assert e.value.status == status
+
+    w = torch.zeros(2, 2, x.slots, device=x.q.device)
+    lse = torch.zeros(4, 4, device=x.q.device)
+    with x.cache() as cache:
+        f = cache.attention
+        refused(4, f, x.q.float(), x.k_new.float(), x.v_new.float(), kv)
+        refused(4, f, x.q, x.k_new.float(), x.v_new, kv)
+        refused(4, cache.accumulate, x.q, lse, kv)
+        refused(4, cache.evict, kv, w, 8)
+        small = CachePages(x.codes["k"], x.codes["v"], x.t["table"], x.t["lens"],
+                           k_scales=x.scales["k"][:-1], v_scales=x.scales["v"])
+        refused(5, f, x.q, x.k_new, x.v_new, small)
+        refused(5, cache.append, small, x.k_new, x.v_new)
+        refused(4, cache.append, kv, x.k_new.float(), x.v_new.float())
+        refused(4, cache.append, kv, x.k_new, x.v_new, slots=torch.zeros(4, dtype=torch.int32,
+                                                                        device=x.q.device))
+        refused(2, cache.append, kv, x.k_new[:3], x.v_new[:3])
+        refused(2, cache.append, kv, x.k_new, x.v_new[:3])
+        refused(5, cache.append, kv, x.k_new, x.v_new, row_pos=x.t["lens"])
+        both = torch.cat([x.t["lens"], x.t["lens"]])
+        odd = CachePages(x.codes["k"], x.codes["v"], x.t["table"], both[:2], k_scales=x.scales["k"],
+                         v_scales=x.scales["v"])
+        refused(4, cache.append, odd, x.k_new, x.v_new, lens_out=both[1:3])
+        mixed = CachePages(x.codes["k"], x.v.bfloat16(), x.t["table"], x.t["lens"],
+                           k_scales=x.scales["k"], v_scales=x.scales["v"])
+        refused(4, f, x.q, x.k_new, x.v_new, mixed)
+    refused(1, CachePages, x.codes["k"], x.codes["v"], x.t["table"], x.t["lens"])
+    refused(4, CachePages, x.codes["k"], x.codes["v"], x.t["table"], x.t["lens"],
+            k_scales=x.scales["k"].half(), v_scales=x.scales["v"])
