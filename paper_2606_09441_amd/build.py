@@ -22,7 +22,7 @@ LIB_PATH = os.path.join(HERE, "libsift.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 
 SOURCES = ["decode.hip", "attn_bf16.hip", "attn_f32.hip", "attn_dense.hip", "cache_attn.hip", "cache_wide.hip",
-           "cache_append.hip", "cache_codes.hip", "cache_weights.hip", "cache_evict.hip", "extract.hip", "rope.hip",
+           "cache_append.hip", "cache_codes.hip", "codes_wide.hip", "cache_weights.hip", "cache_evict.hip", "extract.hip", "rope.hip",
            "rotary.hip", "layer_ops.hip", "sift_api.cpp",
            "extract_api.cpp", "layer_api.cpp", "cache_api.cpp"]
 # Per-source extra flags.  The bf16 attention kernel takes row maxima of MFMA

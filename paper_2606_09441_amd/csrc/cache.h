@@ -157,10 +157,15 @@ struct Split {
 struct Narrow {  // four 32-key tiles a step
   static constexpr int kRows = 32;
   static constexpr int kTileKeys = 32, kStepTiles = 4;
+  static constexpr int kLead = 0;  // steps of a unit that are none: what beginning it costs
 };
 struct Wide {    // a 64-key tile a step
   static constexpr int kRows = 128;
   static constexpr int kTileKeys = 64, kStepTiles = 1;
+  static constexpr int kLead = 0;
+};
+struct NarrowCodes : Narrow {
+  static constexpr int kLead = 2;
 };
 template <typename U>
 struct UnitCost {
@@ -175,7 +180,7 @@ struct UnitCost {
     return cached_tiles(s) + (s.n + U::kTileKeys - 1) / U::kTileKeys;
   }
   static __device__ __forceinline__ int steps(const Seq& s) {
-    return (tiles(s) + U::kStepTiles - 1) / U::kStepTiles;
+    return U::kLead + (tiles(s) + U::kStepTiles - 1) / U::kStepTiles;
   }
   __device__ __forceinline__ int operator()(const Seq& s) const {
     return hkv * blocks(s) * steps(s);

@@ -230,7 +230,7 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
   if ((st = check_tensor(v_new, rows, cache->hkv, d, dtype)) != SIFT_OK) return st;
   if ((st = check_tensor(out, rows, cache->hq, d, dtype)) != SIFT_OK) return st;
   if (tree_mask != nullptr && mask_words < (cache->max_rows + 63) / 64) return SIFT_E_CAPACITY;
-  if (sift::cache_attn_steps(a.c) >= int64_t(1) << 31) return SIFT_E_CAPACITY;
+  if (sift::cache_attn_steps(a.c, pools == SIFT_E4M3) >= int64_t(1) << 31) return SIFT_E_CAPACITY;
   if (rows == 0) return SIFT_OK;
   a.k_new = k_new->data;
   a.v_new = v_new->data;

@@ -298,7 +298,7 @@ bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys) {
   return bf16 && rows_of_kv > kRows && rows_of_kv >= (kNarrowMost + keys - 1) / keys;
 }
 
-int64_t cache_attn_steps(const CacheArgs& a) {
+int64_t cache_attn_steps(const CacheArgs& a, bool codes) {
   // as if every sequence had the most rows, which row pointers may say whatever they
   // add up to; of the narrow units: the wide ones are no more, and take twice the steps
   // where there are half as many
@@ -306,7 +306,7 @@ int64_t cache_attn_steps(const CacheArgs& a) {
   const int64_t units = static_cast<int64_t>(a.num_seqs) * a.hkv *
                         ((rows * (a.hq / a.hkv) + kRows - 1) / kRows);
   const int64_t keys = (static_cast<int64_t>(a.max_pages) << a.page_shift) + rows + 4 * kTileKeys;
-  const int64_t steps = keys / (kTileKeys * kStepTiles) + 1;
+  const int64_t steps = keys / (kTileKeys * kStepTiles) + 1 + (codes ? NarrowCodes::kLead : 0);
   return units >= int64_t(1) << 31 ? units : units * steps;
 }
 
@@ -317,7 +317,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hi
   const int64_t most = static_cast<int64_t>(std::min(a.c.rows, a.c.max_rows)) * (a.c.hq / a.c.hkv);
   const bool codes = pool == Pool::kE4m3;
   const bool wide = cache_attn_wide(
-      pool == Pool::kBf16, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
+      pool != Pool::kF32, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;
@@ -327,7 +327,8 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hi
     const dim3 grid(static_cast<unsigned>((items + each - 1) / each)), block(256);
     if constexpr (Tile<T, D>::kBf16) {
       if (wide) {
-        const hipError_t e = launch_cache_wide(a, D, stream);
+        const hipError_t e =
+            codes ? launch_codes_wide(a, D, stream) : launch_cache_wide(a, D, stream);
         if (e != hipSuccess) return e;
         hipLaunchKernelGGL((cache_merge_kernel<Wide, T, D>), grid, block, 0, stream, a, each);
         return hipGetLastError();
@@ -341,7 +342,10 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hi
       e = hipGetLastError();
     }
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a, each);
+    if (codes)
+      hipLaunchKernelGGL((cache_merge_kernel<NarrowCodes, T, D>), grid, block, 0, stream, a, each);
+    else
+      hipLaunchKernelGGL((cache_merge_kernel<Narrow, T, D>), grid, block, 0, stream, a, each);
     return hipGetLastError();
   };
   using D64 = std::integral_constant<int, 64>;

@@ -25,10 +25,12 @@ constexpr int kRows = Narrow::kRows;
 // A tile of cached keys: its two groups of 16 rows, and their scales.
 struct CodeRows {
   Rows16 r[2];
-  float ks[2], vs[2];
+};
+struct Scales {
+  float k[2], v[2];
 };
 
-template <int D>
+template <int D, bool kCap, bool kBias>
 __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
   using T = __bf16;
   using G = Tile<T, D>;       // of the new tokens' keys
@@ -40,7 +42,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
   __shared__ float part[4][kRows][3];
   const CacheArgs& a = p.c;
   const int g = a.hq / a.hkv;
-  const UnitCost<Narrow> cost{g, a.hkv};
+  const UnitCost<NarrowCodes> cost{g, a.hkv};
   int group, x, xend;
   Place pl;
   Seq s;
@@ -64,8 +66,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
   const int klane = C::lane_k(l32, hf), vlane = C::lane_v(lane, hf);
   const int koff = C::template dma_lane<false>(lane, stride);
   const int voff = C::template dma_lane<true>(lane, stride);
-  const float c = score_factor(a.sc);
-  const bool bent = a.sc.x != 0.f || a.sc.slopes != nullptr;  // not the products alone
+  const float c = kCap || kBias ? 1.f : a.sc.c;  // score_factor
 
   while (x < xend && pl.b < a.num_seqs) {
     // the unit that holds step x
@@ -86,21 +87,26 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
     CodeQ<D> q;
     q.load(static_cast<const T*>(a.q) + (static_cast<int64_t>(row0 + node) * a.hq + h) * D, hf,
            live);
-    const float slope = a.sc.slopes != nullptr ? a.sc.slopes[h] * kLog2e : 0.f;
-    const int my_pos = a.sc.slopes == nullptr ? 0
-                       : a.row_pos != nullptr ? a.row_pos[row0 + node]
-                                              : len + node;
+    const float slope = kBias ? a.sc.slopes[h] * kLog2e : 0.f;
+    const int my_pos = !kBias ? 0 : a.row_pos != nullptr ? a.row_pos[row0 + node] : len + node;
 
     const auto rows_of = [&](int t) {
       CodeRows y;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         y.r[i] = cached_rows(a, b, len, t * kTileKeys + 16 * i);
-        const int64_t at = (y.r[i].row >> a.page_shift) * a.hkv + kvh;
-        y.ks[i] = scalar(p.k_scales, at);
-        y.vs[i] = scalar(p.v_scales, at);
       }
       return y;
+    };
+    const auto scales_of = [&](const CodeRows& y) {
+      Scales z;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int64_t at = (y.r[i].row >> a.page_shift) * a.hkv + kvh;
+        z.k[i] = scalar(p.k_scales, at);
+        z.v[i] = scalar(p.v_scales, at);
+      }
+      return z;
     };
     const auto fetch = [&](const CodeRows& y, int slot, auto v) {
       constexpr bool kV = decltype(v)::value;
@@ -122,30 +128,32 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
     // of whose keys this row sees `bits`, to the exponents' form, and the reference moved:
     // what is left is c (times K's scales) and the returned offset.
     const auto shape = [&](f32x16& sc, uint32_t bits, bool fresh, int j0, float (&f)[2]) {
-      if (a.sc.x != 0.f) cap_scores(a.sc, sc);
+      if constexpr (kCap) cap_scores(a.sc, sc);
       if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(sc, bits >> (4 * hf));
       float off = 0.f;
-      const auto bias = [&](auto far) {
-        off = half_max(largest_bias(sc, slope, far));
-        if (off == -INFINITY) off = 0.f;
-        add_bias(a.sc, sc, slope, off, far);
-      };
-      if (a.sc.slopes != nullptr && (fresh ? a.row_pos : a.key_pos) != nullptr) {
-        float dist[16];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int j = j0 + 4 * hf + key_of(v);
-          const int pos =
-              fresh ? a.row_pos[row0 + min(j, n - 1)]
-                    : a.key_pos[((static_cast<int64_t>(b) * a.hkv + kvh) * a.max_pages
-                                 << a.page_shift) +
-                                min(j, (a.max_pages << a.page_shift) - 1)];
-          dist[v] = fabsf(static_cast<float>(my_pos - pos));
+      if constexpr (kBias) {
+        const auto bias = [&](auto far) {
+          off = half_max(largest_bias(sc, slope, far));
+          if (off == -INFINITY) off = 0.f;
+          add_bias(a.sc, sc, slope, off, far);
+        };
+        if ((fresh ? a.row_pos : a.key_pos) != nullptr) {
+          float dist[16];
+  #pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int j = j0 + 4 * hf + key_of(v);
+            const int pos =
+                fresh ? a.row_pos[row0 + min(j, n - 1)]
+                      : a.key_pos[((static_cast<int64_t>(b) * a.hkv + kvh) * a.max_pages
+                                   << a.page_shift) +
+                                  min(j, (a.max_pages << a.page_shift) - 1)];
+            dist[v] = fabsf(static_cast<float>(my_pos - pos));
+          }
+          bias([&](int v) { return dist[v]; });
+        } else {
+          const float d0 = static_cast<float>(my_pos - (fresh ? len : 0) - j0 - 4 * hf);
+          bias([&](int v) { return fabsf(d0 - static_cast<float>(key_of(v))); });
         }
-        bias([&](int v) { return dist[v]; });
-      } else if (a.sc.slopes != nullptr) {
-        const float d0 = static_cast<float>(my_pos - (fresh ? len : 0) - j0 - 4 * hf);
-        bias([&](int v) { return fabsf(d0 - static_cast<float>(key_of(v))); });
       }
       float m0 = sc[0], m1 = sc[8];
 #pragma unroll
@@ -157,19 +165,21 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
       return off;
     };
 
-    const int tend = min(tiles, s1 * kStepTiles);
+    // (of the unit's steps the first kLead are none)
+    const int first = max(s0 - NarrowCodes::kLead, 0), last = max(s1 - NarrowCodes::kLead, 0);
+    const int tend = min(tiles, last * kStepTiles);
     const int cend = min(ct, tend);
-    int t = s0 * kStepTiles + wave;
+    int t = first * kStepTiles + wave;
     if (t < cend) {
-      // rows (of this tile, and of the next)
-      CodeRows now = rows_of(t), next{};
+      // of this tile and of the next; the scales are asked for behind the rows
+      CodeRows now = rows_of(t), next = rows_of(min(t + kStepTiles, cend - 1));
       fetch(now, 0, kK);
       fetch(now, 0, kV);
       if (t + kStepTiles < cend) {
-        next = rows_of(t + kStepTiles);
         fetch(next, 1, kK);
         fetch(next, 1, kV);
       }
+      Scales mine = scales_of(now);
       int slot = 0;
       for (; t < cend; t += kStepTiles, slot ^= 1) {
         const bool one = t + kStepTiles < cend, two = t + 2 * kStepTiles < cend;
@@ -177,6 +187,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
                               static_cast<uint32_t>(low_bits(now.r[1].n)) << 16;
         CodeRows after{};
         if (two) after = rows_of(t + 2 * kStepTiles);
+        const Scales then = scales_of(next);
         if (one)
           wait_vm<3 * kDmas>();  // K is there, V and the next tile may still be on their way
         else
@@ -187,9 +198,9 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         float f[2], base[2], undo[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const float ks = usable_scale(now.ks[i]), vs = usable_scale(now.vs[i]);
+          const float ks = usable_scale(mine.k[i]), vs = usable_scale(mine.v[i]);
           f[i] = ks * c;
-          if (bent) {
+          if constexpr (kCap || kBias) {
 #pragma unroll
             for (int v = 8 * i; v < 8 * i + 8; ++v) sc[v] *= ks;
             f[i] = c;
@@ -212,6 +223,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         if (two) fetch(after, slot, kV);
         now = next;
         next = after;
+        mine = then;
       }
     }
     // the new tokens' own
@@ -281,10 +293,23 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
 }  // namespace
 
 hipError_t launch_cache_codes(const CacheAttnArgs& a, int head_dim, hipStream_t stream) {
+  const auto launch = [&](auto dim, auto cap, auto bias) {
+    hipLaunchKernelGGL(
+        (cache_codes_kernel<decltype(dim)::value, decltype(cap)::value, decltype(bias)::value>),
+        dim3(a.groups), dim3(256), 0, stream, a);
+  };
+  const auto of = [&](auto dim) {
+    const std::true_type yes;
+    const std::false_type no;
+    if (a.c.sc.x != 0.f)
+      a.c.sc.slopes != nullptr ? launch(dim, yes, yes) : launch(dim, yes, no);
+    else
+      a.c.sc.slopes != nullptr ? launch(dim, no, yes) : launch(dim, no, no);
+  };
   if (head_dim == 128)
-    hipLaunchKernelGGL((cache_codes_kernel<128>), dim3(a.groups), dim3(256), 0, stream, a);
+    of(std::integral_constant<int, 128>{});
   else
-    hipLaunchKernelGGL((cache_codes_kernel<64>), dim3(a.groups), dim3(256), 0, stream, a);
+    of(std::integral_constant<int, 64>{});
   return hipGetLastError();
 }
 

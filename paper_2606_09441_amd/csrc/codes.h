@@ -80,10 +80,10 @@ struct CodeTile {
     const int row = 4 * hf + (z & 3) + 8 * (z >> 2);
     return row * kRow + 16 * (((lane >> 4) & 1) ^ swz_v(row)) + 8 * (lane & 1);
   }
-  static __device__ __forceinline__ bf16x8 v_frag(int addr, int db, int st) {
+  static __device__ __forceinline__ u32x2 v_codes(int addr, int db, int st) {
     const i32x2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<lds_i32x2*>(
         static_cast<size_t>((addr ^ (db << 5)) + 16 * st * kRow)));
-    return code_values(__builtin_bit_cast(u32x2, v));
+    return __builtin_bit_cast(u32x2, v);
   }
 };
 
@@ -145,8 +145,8 @@ __device__ __forceinline__ void pv_codes(int addr, const f32x16& p, f32x16 (&o)[
     for (int i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(p[8 * st + i]);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
-      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(CodeTile<D>::v_frag(addr, db, st), b, o[db],
-                                                      0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code_values(CodeTile<D>::v_codes(addr, db, st)), b,
+                                                      o[db], 0, 0, 0);
   }
 }
 
