@@ -488,7 +488,10 @@ def _empty(shape, dtype, device, stream):
 def _desc(fn, t, name, device) -> SiftTensor:
     if getattr(t, "device", None) != device:
         raise SiftError(fn, 7, f"{name} is not on {device}")
-    return tensor_desc(t)
+    shape, kind = t.shape, _kinds.get(t.dtype)
+    if kind is None or len(shape) != 3 or not t.is_contiguous():
+        return tensor_desc(t)   # says what is wrong
+    return SiftTensor(t.data_ptr(), kind, shape[0], shape[1], shape[2])
 
 
 def _address(t):
@@ -750,17 +753,22 @@ class Rotary:
         call.  The outputs are new, or given, and may be the inputs."""
         fn, dev = "sift_rotate", self.device
         _current(fn, dev)
-        if k is None and k_out is not None:
-            raise SiftError(fn, 1, "k_out without k")
-        require(fn, positions, "positions", "int32", q.shape[0], dev)
+        qd, kd, ko = _desc(fn, q, "q", dev), None, None
+        require(fn, positions, "positions", "int32", qd.tokens, dev)
         if q_out is None:
             q_out = _empty_like(q, stream)
-        if k is not None and k_out is None:
-            k_out = _empty_like(k, stream)
-        check(fn, lib().sift_rotate(
-            _desc(fn, q, "q", dev), None if k is None else _desc(fn, k, "k", dev),
-            positions.data_ptr(), self.struct, back, _desc(fn, q_out, "q_out", dev),
-            None if k is None else _desc(fn, k_out, "k_out", dev), _stream_ptr(stream)))
+        qo = _desc(fn, q_out, "q_out", dev)
+        if k is not None:
+            kd = _desc(fn, k, "k", dev)
+            if k_out is None:
+                k_out = _empty_like(k, stream)
+            ko = _desc(fn, k_out, "k_out", dev)
+        elif k_out is not None:
+            raise SiftError(fn, 1, "k_out without k")
+        st = lib().sift_rotate(qd, kd, positions.data_ptr(), self.struct, back, qo, ko,
+                               _stream_ptr(stream))
+        if st:
+            check(fn, st)
         return q_out, k_out
 
     def rotate_(self, q, k, positions, back=False, stream=None):
@@ -793,8 +801,11 @@ def _turn_function():
             def backward(ctx, dq, dk):
                 positions, = ctx.saved_tensors
                 # (a gradient may be a view, or expanded)
-                dq, dk = _turn_class.apply(dq.contiguous(), dk.contiguous() if ctx.pair else None,
-                                           positions, ctx.rotary, not ctx.back)
+                args = (dq.contiguous(), dk.contiguous() if ctx.pair else None, positions)
+                if torch.is_grad_enabled():   # a gradient of the gradient may be asked for
+                    dq, dk = _turn_class.apply(*args, ctx.rotary, not ctx.back)
+                else:
+                    dq, dk = ctx.rotary.rotate(*args, not ctx.back)
                 return dq, dk, None, None, None
 
         _turn_class = Turn
@@ -887,6 +898,7 @@ class CachePages:
                       v_scales)
         self.sizes = (dev, *(None if t is None else (t.numel(), t.shape)
                              for t in (page_table, lens, page_lens, key_pos)))
+        self.fits = None   # the sizes of the Cache that took these last
         ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
                                   lens.data_ptr(), ptr(page_lens), ptr(key_pos), ptr(k_scales),
@@ -920,7 +932,7 @@ class Cache:
         self._slot_sizes = (num_seqs, num_kv_heads, self.slots)
         sizes = (("page_table", (num_seqs, max_pages)), ("lens", (num_seqs,)),
                  ("page_lens", (num_seqs, max_pages)), ("key_pos", self._slot_sizes))
-        self._tables = tuple((name, math.prod(x), x) for name, x in sizes)
+        self._tables = tuple((name, math.prod(x), x) for name, x in sizes)  # (of this handle alone)
 
     def close(self):
         if self._h is not None:
@@ -941,6 +953,8 @@ class Cache:
 
     def _kv(self, fn, kv):
         """The tables' sizes, which the library cannot see."""
+        if kv.fits is self._tables:   # as of the last call
+            return kv.struct
         device, *have = kv.sizes
         if device != self.device:
             raise SiftError(fn, 7, f"the pages are on {device}, the cache on {self.device}")
@@ -953,8 +967,8 @@ class Cache:
         if kv.k_scales is not None:
             sizes = (kv.k_pages.shape[0] // self.page, self.hkv)
             for name, t in (("k_scales", kv.k_scales), ("v_scales", kv.v_scales)):
-                if t.shape != sizes:
-                    require_laid_out(fn, t, name, "float32", sizes, self.device)
+                require_laid_out(fn, t, name, "float32", sizes, self.device)
+        kv.fits = self._tables
         return kv.struct
 
     def _rows(self, fn, q, row_ptr, row_pos):
@@ -1008,6 +1022,7 @@ class Cache:
         receives the positions, kv.key_pos when None."""
         torch = _torch()
         fn, dev = "sift_cache_append", self.device
+        kd, vd = _desc(fn, k, "k", dev), _desc(fn, v, "v", dev)
         rows = self._rows(fn, k, row_ptr, row_pos)
         if rotary is not None and rotary.device != dev:
             raise SiftError(fn, 7, f"the rotary is on {rotary.device}, the cache on {dev}")
@@ -1021,10 +1036,11 @@ class Cache:
             require(fn, lens_out, "lens_out", "int32", self.num_seqs, dev)
         elif slots is None:
             lens_out = _empty((self.num_seqs,), torch.int32, dev, stream)
-        check(fn, lib().sift_cache_append(
-            self._h, self._kv(fn, kv), rows, _desc(fn, k, "k", dev), _desc(fn, v, "v", dev),
-            None if rotary is None else rotary.struct, _address(slots), _address(pos_out),
-            _address(lens_out), _stream_ptr(stream)))
+        st = lib().sift_cache_append(
+            self._h, self._kv(fn, kv), rows, kd, vd, None if rotary is None else rotary.struct,
+            _address(slots), _address(pos_out), _address(lens_out), _stream_ptr(stream))
+        if st:
+            check(fn, st)
         return lens_out
 
     def accumulate(self, q, lse, kv, weights=None, decay=1.0, row_ptr=None, row_pos=None,
