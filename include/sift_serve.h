@@ -220,8 +220,8 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
  * changed.  The pages that rows enter must be the sequence's own.
  * SIFT_E4M3: a page's scale becomes the least power of two (2^-100 at least) such that
  *   448 times it holds max |x| of the page's new rows of the head (of dims that turn,
- *   sqrt(2) times that and the magnitude), or stays where the page held keys under a
- *   larger one.  Where it grows the codes of the keys held are rounded again.  Values
+ *   sqrt(2) times that and the magnitude), and that is not below the scale under which
+ *   the page held keys.  Where it grows the codes of the keys held are rounded again.  Values
  *   that are not finite are held as NaN and take no part in the scale.  The first row
  *   that enters a page begins it: whatever else it holds, and its scale, is forgotten.
  * Errors: SIFT_E_NULL, SIFT_E_SHAPE, SIFT_E_UNSUPPORTED (dtypes, alignment, magnitude;

@@ -162,35 +162,62 @@ __device__ __forceinline__ float scale_for(float size) {
   const int e = static_cast<int>(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
   return __builtin_bit_cast(float, static_cast<uint32_t>(max(e, kLeastScale) + 127) << 23);
 }
-
-// Eight numbers as codes, rounded to the nearest; what is not finite (or beyond what
-// rounds to 448) as NaN, which e4m3 has in place of infinities.
-__device__ __forceinline__ u32x2 encode(const float (&x)[8], float by) {
-  float y[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float z = x[i] * by;
-    y[i] = fabsf(z) < 464.f ? z : __builtin_nanf("");
-  }
-  int lo = 0, hi = 0;
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], lo, false);
-  lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], hi, false);
-  hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
-  return u32x2{static_cast<uint32_t>(lo), static_cast<uint32_t>(hi)};
+// The least power of two that is not below x.
+__device__ __forceinline__ float power_from(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  return __builtin_bit_cast(float, (u + 0x7fffffu) & 0xff800000u);
 }
 
-__device__ __forceinline__ void decode(u32x2 v, float (&x)[8]) {
+// Sizes of bf16 numbers as their bits, which order them: the largest of each half of words.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 larger_bits(u16x2 m, uint32_t w) {
+  return __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w & 0x7fff7fffu));
+}
+// The larger half as a number; infinity where it is none.
+__device__ __forceinline__ float size_of(u16x2 m) {
+  const uint32_t u = m[0] > m[1] ? m[0] : m[1];
+  return u >= 0x7f80u ? INFINITY : __builtin_bit_cast(float, u << 16);
+}
+
+// Eight numbers as codes of `scale` (a power of two), rounded to the nearest; what is
+// not finite, or rounds to more than 448, becomes NaN, which e4m3 has in place of
+// infinities.
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2 encode(const float (&x)[8], float scale) {
+  u32x2 v;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i], x[4 * i + 1], scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i + 2], x[4 * i + 3], scale, true);
+    v[i] = __builtin_bit_cast(uint32_t, w);
+  }
+  return v;
+}
+__device__ __forceinline__ u32x2 encode(u32x4 x, float scale) {  // of bf16
+  u32x2 v;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t a = x[2 * i], b = x[2 * i + 1];
+    s16x2 w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, a), scale, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2, b), scale, true);
+    v[i] = __builtin_bit_cast(uint32_t, w);
+  }
+  return v;
+}
+
+__device__ __forceinline__ void decode(u32x2 v, float scale, float (&x)[8]) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int w = static_cast<int>(v[i]);
     const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
     const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-    x[4 * i] = a[0];
-    x[4 * i + 1] = a[1];
-    x[4 * i + 2] = b[0];
-    x[4 * i + 3] = b[1];
+    x[4 * i] = a[0] * scale;
+    x[4 * i + 1] = a[1] * scale;
+    x[4 * i + 2] = b[0] * scale;
+    x[4 * i + 3] = b[1] * scale;
   }
 }
 
@@ -260,25 +287,47 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     const float old_k = begun ? p.k_scales[sc] : 0.f, old_v = begun ? p.v_scales[sc] : 0.f;
 
     // their largest sizes
-    float mr = 0.f, mk = 0.f, mv = 0.f;  // of dims that turn, of those that stay, of V
+    const float grow = kRoot2 * p.r.magnitude;  // of dims that turn
+    float mk, mv;
+    {
+      u16x2 r = {0, 0}, k = {0, 0}, v = {0, 0};  // of dims that turn, that stay, of V
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i)
+      for (int i = 0; i < kPasses; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        C k, v;
-        k.set(kx[i][j]);
-        v.set(vx[i][j]);
-        const int d0 = 8 * (j ? c1 : c0);
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          mv = larger(mv, v.x[e]);
-          if (kTurns != kNone && d0 + e < 2 * p.r.half)
-            mr = larger(mr, k.x[e]);
-          else
-            mk = larger(mk, k.x[e]);
+          for (int e = 0; e < 4; ++e) {
+            v = larger_bits(v, vx[i][j][e]);
+            if (kTurns != kNone && 4 * (j ? c1 : c0) + e < p.r.half)
+              r = larger_bits(r, kx[i][j][e]);
+            else
+              k = larger_bits(k, kx[i][j][e]);
+          }
+      mk = size_of(k);
+      mv = size_of(v);
+      if (kTurns != kNone) mk = fmaxf(mk, size_of(r) * grow);
+    }
+    if (__syncthreads_or(mk == INFINITY || mv == INFINITY)) {  // without what is not finite
+      float r = 0.f;
+      mk = mv = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          C k, v;
+          k.set(kx[i][j]);
+          v.set(vx[i][j]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            mv = larger(mv, v.x[e]);
+            if (kTurns != kNone && 4 * (j ? c1 : c0) + e / 2 < p.r.half)
+              r = larger(r, k.x[e]);
+            else
+              mk = larger(mk, k.x[e]);
+          }
         }
-      }
-    if (kTurns != kNone) mk = fmaxf(mk, mr * kRoot2 * p.r.magnitude);
+      if (kTurns != kNone) mk = fmaxf(mk, r * grow);
+    }
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
       mk = fmaxf(mk, __shfl_xor(mk, d));
@@ -293,7 +342,8 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
       mk = fmaxf(mk, part[0][w]);
       mv = fmaxf(mv, part[1][w]);
     }
-    const float new_k = fmaxf(old_k, scale_for(mk)), new_v = fmaxf(old_v, scale_for(mv));
+    const float new_k = fmaxf(power_from(old_k), scale_for(mk));
+    const float new_v = fmaxf(power_from(old_v), scale_for(mv));
     __syncthreads();  // the maxima and the old scales are read
     if (threadIdx.x == 0) {
       p.k_scales[sc] = new_k;
@@ -302,31 +352,27 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     uint8_t* const ko = static_cast<uint8_t*>(p.k_pages);
     uint8_t* const vo = static_cast<uint8_t*>(p.v_pages);
     // rows that the page held
-    const auto again = [&](uint8_t* pool, float by) {
+    const auto again = [&](uint8_t* pool, float was, float is) {
       for (int r = r0; r < lo; r += each)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           u32x2* q = reinterpret_cast<u32x2*>(pool + ((row + r) * a.hkv + h) * D + 8 * (j ? c1 : c0));
           float y[8];
-          decode(*q, y);
-          *q = encode(y, by);
+          decode(*q, was, y);
+          *q = encode(y, is);
         }
     };
-    if (begun && new_k != old_k) again(ko, old_k / new_k);
-    if (begun && new_v != old_v) again(vo, old_v / new_v);
+    if (begun && new_k != old_k) again(ko, old_k, new_k);
+    if (begun && new_v != old_v) again(vo, old_v, new_v);
     // the new ones
-    const float by_k = 1.f / new_k, by_v = 1.f / new_v;
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
       const int r = r0 + i * each;
       if (r < lo || r >= hi) continue;
       const int pos = a.row_pos != nullptr ? a.row_pos[src + r] : base + r;
-      C k[2], v[2];
+      C k[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        k[j].set(kx[i][j]);
-        v[j].set(vx[i][j]);
-      }
+      for (int j = 0; j < 2; ++j) k[j].set(kx[i][j]);
       if constexpr (kTurns == kHalves) {
         if (8 * c0 < p.r.half) {
           rotary::Item<__bf16, false> it;
@@ -363,8 +409,9 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int64_t c = at + 8 * (j ? c1 : c0);
-        *reinterpret_cast<u32x2*>(ko + c) = encode(k[j].x, by_k);
-        *reinterpret_cast<u32x2*>(vo + c) = encode(v[j].x, by_v);
+        *reinterpret_cast<u32x2*>(ko + c) =
+            kTurns == kNone ? encode(kx[i][j], new_k) : encode(k[j].x, new_k);
+        *reinterpret_cast<u32x2*>(vo + c) = encode(vx[i][j], new_v);
       }
       if (item == 0 && p.pos_out != nullptr)
         p.pos_out[(static_cast<int64_t>(pl.b) * a.hkv + h) * slots + base + r] = pos;

@@ -384,6 +384,29 @@ def test_growing_scales_keep_what_is_held():
     assert ((got - x).abs() <= torch.maximum(x.abs() * 2.0 ** -4, torch.tensor(4 * s * 2.0 ** -10))).all()
 
 
+def test_pages_under_scales_that_are_no_powers():
+    """Pages that another program filled: their scale becomes the next power of two, and
+    what they hold is rounded again, by half a step."""
+    c = Case([5, 20], [3, 2], 2, 64, 16, "e4m3", 32)
+    for t in (c.k_scales, c.v_scales):
+        t.mul_(1.37)
+    before = c.snapshot()
+    with c.cache() as cache:
+        cache.append(c.kv(), c.k, c.v, row_ptr=c.t["row_ptr"], row_pos=c.t["row_pos"],
+                     rotary=c.rotary())
+    torch.cuda.synchronize()
+    after = c.snapshot()
+    for b, n in ((0, 5), (1, 4)):
+        page = int(c.table[b, c.lens[b] // 16])
+        for name in "kv":
+            was, now = (x[name].view(DTYPES["e4m3"]).double()[page * 16:page * 16 + n] *
+                        x[name + "s"].double()[page][:, None] for x in (before, after))
+            s = after[name + "s"].double()[page]
+            assert torch.equal(s.log2(), s.log2().round()) and (s >= before[name + "s"][page]).all()
+            half = torch.maximum(was.abs() * 2.0 ** -4, s[:, None] * 2.0 ** -10)
+            assert ((now - was).abs() <= half).all()
+
+
 def test_another_stream():
     c = Case([5, 6], [70, 3], 2, 128, 64, "e4m3", 128)
     before = c.snapshot()
