@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
             f[i] = c;
           }
           base[i] = -__builtin_amdgcn_logf(vs);
-          undo[i] = 1.f / vs;
+          undo[i] = __builtin_amdgcn_rcpf(vs);
         }
         const float off = shape(sc, bits, false, t * kTileKeys, f);
 #pragma unroll

@@ -18,15 +18,32 @@ namespace flash {
 
 constexpr int kGroups = kKeys / 16;
 
+// A tile: this wavefront's 16 rows, and its groups' pages.
+struct CodeWhere {
+  int64_t row;
+  int32_t n;
+  int32_t page[kGroups];
+};
+struct CodeScales {
+  float k[kGroups], v[kGroups];
+};
 // A tile's V scales as the weights take them: 2^-lift, and one over the scale.
 struct Lift {
   float lift[kGroups], undo[kGroups];
+  __device__ __forceinline__ void set(const CodeScales& z) {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const float s = usable_scale(z.v[g]);
+      lift[g] = -__builtin_amdgcn_logf(s);
+      undo[g] = __builtin_amdgcn_rcpf(s);
+    }
+  }
 };
 
 // Src: what the tiles are.
 //   int steps               of the workgroup;  int mine: of this wavefront, the first ones
-//   rows<kV>(i)             this wavefront's 16 rows of step i's K or V tile
-//   k_scales(i, float (&)[4]), lift(i): of step i's tile
+//   where(i)                step i's tile, no rows of it past the last step
+//   rows<kV>(where), scales(where): this wavefront's rows of K or V; the tile's scales
 //   take(i, s0, s1, mx, mn, form) -> bound   as take_tile, of scaled products
 template <int D, bool kCap, typename Src>
 __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowState<D>& st,
@@ -126,10 +143,10 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
     }
   };
 
-  const i32x4 none = i32x4{0, 0, 0, kBufferWord3};
-  const auto k_rows = [&](int i) { return i < src.steps ? src.template rows<false>(i) : none; };
-  const auto v_rows = [&](int i) { return i < src.steps ? src.template rows<true>(i) : none; };
-
+  // Of steps i + 2 and i + 3; the scales of step i + 1.  Tables and scales are asked for
+  // a step before they are used.
+  CodeWhere in2 = src.where(2), in3 = src.where(3);
+  CodeScales next;
   // Slots (byte offsets) of K of steps i, i + 1 and i + 2, and of V's.
   int k0 = 0, k1 = kTile, k2 = 2 * kTile, v0 = 0, v1 = kTile, v2 = 2 * kTile;
   Form f;
@@ -139,7 +156,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
     // addresses made anew in every step: kept, each would hold a register
     asm volatile("" : "+v"(kaddr), "+v"(vaddr));
     // K of step i + 3 and V of step i + 2 (past the last step zeros, from nowhere)
-    const i32x4 krs = k_rows(i + 3), vrs = v_rows(i + 2);
+    const i32x4 krs = src.template rows<false>(in3), vrs = src.template rows<true>(in2);
     const auto issue = [&](int s) {
       if (s < kDmas)
         dma_b128(own + k0 + s * 1024, C::template dma_off<false>(koff, s, stride), krs);
@@ -147,11 +164,13 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
         dma_b128(own + 3 * kTile + v2 + (s - kDmas) * 1024,
                  C::template dma_off<true>(voff, s - kDmas, stride), vrs);
     };
+    const CodeScales now = next;
     if (i < src.mine) {
-      float ks[kGroups];
-      src.k_scales(min(i + 1, src.steps - 1), ks);
       // (past the last tile a body like the others: its scores go nowhere)
       qk_and_weigh(k1, n0, n1, c0, c1, f, w, issue);
+      float ks[kGroups];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(now.k[g]);
       float mx = -INFINITY, mn = INFINITY;
       pv_and(v0, [&](int e) {
 #pragma unroll
@@ -167,12 +186,15 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
       });
       if (i + 1 < src.mine) {
         st.rescale(src.take(i + 1, n0, n1, mx, mn, f));
-        w = src.lift(i + 1);
+        w.set(now);
       }
     } else {
 #pragma unroll
       for (int s = 0; s < 2 * kDmas; ++s) issue(s);
     }
+    next = src.scales(in2);
+    in2 = in3;
+    in3 = src.where(i + 4);
     wait_vm<2 * kDmas>();  // but for those of this step
     __syncthreads();
     const int a = k0, b = v0;
@@ -180,23 +202,30 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
     v0 = v1, v1 = v2, v2 = b;
   };
 
-  const auto bring_k = [&](int slot, int i) {
-    C::template dma_rows<false>(own + slot * kTile, k_rows(i), koff, stride);
+  const auto bring_k = [&](int slot, const CodeWhere& y) {
+    C::template dma_rows<false>(own + slot * kTile, src.template rows<false>(y), koff, stride);
   };
-  const auto bring_v = [&](int slot, int i) {
-    C::template dma_rows<true>(own + (3 + slot) * kTile, v_rows(i), voff, stride);
+  const auto bring_v = [&](int slot, const CodeWhere& y) {
+    C::template dma_rows<true>(own + (3 + slot) * kTile, src.template rows<true>(y), voff, stride);
   };
-  bring_k(0, 0);
-  bring_v(0, 0);
-  bring_k(1, 1);
-  bring_k(2, 2);
-  bring_v(1, 1);
+  CodeScales first;
+  {
+    const CodeWhere in0 = src.where(0), in1 = src.where(1);
+    bring_k(0, in0);
+    bring_v(0, in0);
+    bring_k(1, in1);
+    bring_k(2, in2);
+    bring_v(1, in1);
+    first = src.scales(in0);
+    next = src.scales(in1);
+  }
   wait_vm<2 * kDmas>();
   __syncthreads();
   f32x16 a0{}, a1{}, b0{}, b1{};
   if (src.mine > 0) {
     float ks[kGroups];
-    src.k_scales(0, ks);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(first.k[g]);
     a0 = qk_codes<D>(kaddr, q);
     a1 = qk_codes<D>(kaddr + 32 * C::kRow, q);
     float mx = -INFINITY, mn = INFINITY;
@@ -208,7 +237,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
       mn = fminf(fminf(mn, a0[v]), a1[v]);
     }
     st.rescale(src.take(0, a0, a1, mx, mn, f));
-    w = src.lift(0);
+    w.set(first);
   }
   __syncthreads();  // K slot 0 is refilled by step 0
   for (int i = 0; i < src.steps; i += 2) {

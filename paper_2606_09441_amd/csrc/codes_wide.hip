@@ -28,35 +28,45 @@ struct CodeTiles {
     const int j = i + turn;
     return s0 + (j < steps ? j : j - steps);
   }
-  template <bool kV>
-  __device__ __forceinline__ i32x4 rows(int i) const {
-    using C = CodeTile<D>;
+  // Step i's tile (past the last step none of its rows).
+  __device__ __forceinline__ CodeWhere where(int i) const {
     const CacheArgs& a = p.c;
-    const Rows16 r = cached_rows(a, b, len, tile(i) * kKeys + 16 * wave);
-    return rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
-                         (r.row * a.hkv + kvh) * C::kRow,
-                     r.n, a.hkv * C::kRow, C::kRow);
-  }
-  __device__ __forceinline__ int64_t scale_at(int i, int g) const {
-    const CacheArgs& a = p.c;
-    const int pi = min((tile(i) * kKeys + 16 * g) >> a.page_shift, a.max_pages - 1);
-    const int page =
-        within(scalar(a.table, static_cast<int64_t>(b) * a.max_pages + pi), a.num_pages - 1);
-    return static_cast<int64_t>(page) * a.hkv + kvh;
-  }
-  __device__ __forceinline__ void k_scales(int i, float (&s)[kGroups]) const {
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) s[g] = usable_scale(scalar(p.k_scales, scale_at(i, g)));
-  }
-  __device__ __forceinline__ Lift lift(int i) const {
-    Lift w;
+    const int slot = tile(min(i, steps - 1)) * kKeys;
+    const Rows16 r = cached_rows(a, b, len, slot + 16 * wave);
+    CodeWhere y;
+    y.row = r.row;
+    y.n = i < steps ? r.n : 0;
+    y.page[0] = static_cast<int32_t>(r.row >> a.page_shift);
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
-      const float s = usable_scale(scalar(p.v_scales, scale_at(i, g)));
-      w.lift[g] = -__builtin_amdgcn_logf(s);
-      w.undo[g] = 1.f / s;
+      if (a.page_shift >= 6) {  // one page
+        y.page[g] = y.page[0];
+        continue;
+      }
+      const int pi = min((slot + 16 * g) >> a.page_shift, a.max_pages - 1);
+      y.page[g] =
+          within(scalar(a.table, static_cast<int64_t>(b) * a.max_pages + pi), a.num_pages - 1);
     }
-    return w;
+    return y;
+  }
+  template <bool kV>
+  __device__ __forceinline__ i32x4 rows(const CodeWhere& y) const {
+    using C = CodeTile<D>;
+    const CacheArgs& a = p.c;
+    return rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
+                         (y.row * a.hkv + kvh) * C::kRow,
+                     y.n, a.hkv * C::kRow, C::kRow);
+  }
+  // As they are.
+  __device__ __forceinline__ CodeScales scales(const CodeWhere& y) const {
+    CodeScales z;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int64_t at = static_cast<int64_t>(y.page[g]) * p.c.hkv + kvh;
+      z.k[g] = scalar(p.k_scales, at);
+      z.v[g] = scalar(p.v_scales, at);
+    }
+    return z;
   }
   // One bit a key of tile t.
   __device__ __forceinline__ uint64_t bits(int t) const {
