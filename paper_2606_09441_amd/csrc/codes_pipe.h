@@ -6,8 +6,9 @@
 // read the same tiles from, and room for three tiles of K and of V: the DMA of a tile has
 // two steps to arrive in.
 //
-// A tile's four groups of 16 keys have scales of their own.  K's are multiplied into the
-// scores beside PV, V's are part of the exponents (codes.h).
+// A tile's four groups of 16 keys have scales of their own.  V's are part of the exponents
+// (codes.h), K's a factor of them; where scores are capped or biased K's are multiplied
+// into the scores beside PV.
 #pragma once
 
 #include "codes.h"
@@ -44,8 +45,9 @@ struct Lift {
 //   int steps               of the workgroup;  int mine: of this wavefront, the first ones
 //   where(i)                step i's tile, no rows of it past the last step
 //   rows<kV>(where), scales(where): this wavefront's rows of K or V; the tile's scales
-//   take(i, s0, s1, mx, mn, form) -> bound   as take_tile, of scaled products
-template <int D, bool kCap, typename Src>
+//   take(i, s0, s1, mx, mn, form) -> bound   as take_tile, of scaled products; kPlain:
+//   mask(i, s0, s1, mx), which only hides what a row does not see, and corrects mx
+template <int D, bool kCap, bool kPlain, typename Src>
 __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowState<D>& st,
                                               int lds0, int lane, int stride) {
   using C = CodeTile<D>;
@@ -64,16 +66,23 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
   const int voff = C::template dma_lane<true>(lane, stride);
   const bf16x2 ones = bf16x2{static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
+  Form f;
+  float fk[kGroups];  // kPlain: K's scales and the scores'
+  Lift w;
+  // The bound of a tile's scores from its groups' largest products.
+  const auto largest = [&](const float (&m)[kGroups]) {
+    return half_max(fmaxf(fmaxf(m[0] * fk[0], m[1] * fk[1]), fmaxf(m[2] * fk[2], m[3] * fk[3])));
+  };
   // The weight of score e (0 .. 31) of a tile, with its neighbour, into pb.
   bf16x8 pb[kGroups];
-  const auto weigh = [&](int e, const f32x16& s0, const f32x16& s1, const Form& f, float base,
-                         float& sum, float& le) {
+  const auto weigh = [&](int e, const f32x16& s0, const f32x16& s1, const Form& f, float p0,
+                         float base, float& sum, float& le) {
     const int i = e >> 3, v = 8 * (i & 1) + (e & 7);
     float p[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const float z = i < 2 ? s0[v + u] : s1[v + u];
-      float pz = f.p0;
+      float pz = p0;
       if constexpr (kCap) {
         const float y = z * z;
         pz = fmaf(y, fmaf(y, fmaf(y, f.p3, f.p2), f.p1), f.p0);
@@ -110,7 +119,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 #pragma unroll
       for (int u = 0; u < kEach; u += 2) {
         const int e = s * kEach + u, i = e >> 3;
-        weigh(e, c0, c1, f, base + w.lift[i], sum, le);
+        weigh(e, c0, c1, f, kPlain ? fk[i] : f.p0, base + w.lift[i], sum, le);
         if ((e & 7) == 6) {  // the group's last
           st.l = fmaf(sum, w.undo[i], st.l);
           st.le = fmaf(le, w.undo[i], st.le);
@@ -149,8 +158,6 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
   CodeScales next;
   // Slots (byte offsets) of K of steps i, i + 1 and i + 2, and of V's.
   int k0 = 0, k1 = kTile, k2 = 2 * kTile, v0 = 0, v1 = kTile, v2 = 2 * kTile;
-  Form f;
-  Lift w;
   // step i: its tile's scores in c0, c1 with form f; leaves the next in n0, n1
   const auto step = [&](int i, f32x16& c0, f32x16& c1, f32x16& n0, f32x16& n1) {
     // addresses made anew in every step: kept, each would hold a register
@@ -172,20 +179,34 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(now.k[g]);
       float mx = -INFINITY, mn = INFINITY;
+      float mg[kGroups] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       pv_and(v0, [&](int e) {
 #pragma unroll
         for (int u = 0; u < kDone; u += 2) {
           const int x = e * kDone + u, v = x & 15;
           f32x16& n = x < 16 ? n0 : n1;
-          n[v] *= ks[x >> 3];
-          n[v + 1] *= ks[x >> 3];
-          mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
-          if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
+          if constexpr (kPlain) {
+            float& m = mg[x >> 3];
+            m = fmaxf(fmaxf(m, n[v]), n[v + 1]);
+            asm volatile("" : "+v"(m));  // here, not where it is used
+          } else {
+            n[v] *= ks[x >> 3];
+            n[v + 1] *= ks[x >> 3];
+            mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
+            if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
+          }
         }
-        asm volatile("" : "+v"(mx), "+v"(mn));  // here, not where they are used
+        if constexpr (!kPlain) asm volatile("" : "+v"(mx), "+v"(mn));
       });
       if (i + 1 < src.mine) {
-        st.rescale(src.take(i + 1, n0, n1, mx, mn, f));
+        if constexpr (kPlain) {
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) fk[g] = ks[g] * src.factor();
+          src.mask(i + 1, n0, n1, mg);
+          st.rescale(largest(mg));
+        } else {
+          st.rescale(src.take(i + 1, n0, n1, mx, mn, f));
+        }
         w.set(now);
       }
     } else {
@@ -228,15 +249,28 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
     for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(first.k[g]);
     a0 = qk_codes<D>(kaddr, q);
     a1 = qk_codes<D>(kaddr + 32 * C::kRow, q);
-    float mx = -INFINITY, mn = INFINITY;
+    if constexpr (kPlain) {
+      float mg[kGroups] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      a0[v] *= ks[v >> 3];
-      a1[v] *= ks[2 + (v >> 3)];
-      mx = fmaxf(fmaxf(mx, a0[v]), a1[v]);
-      mn = fminf(fminf(mn, a0[v]), a1[v]);
+      for (int v = 0; v < 16; ++v) {
+        mg[v >> 3] = fmaxf(mg[v >> 3], a0[v]);
+        mg[2 + (v >> 3)] = fmaxf(mg[2 + (v >> 3)], a1[v]);
+      }
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) fk[g] = ks[g] * src.factor();
+      src.mask(0, a0, a1, mg);
+      st.rescale(largest(mg));
+    } else {
+      float mx = -INFINITY, mn = INFINITY;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        a0[v] *= ks[v >> 3];
+        a1[v] *= ks[2 + (v >> 3)];
+        mx = fmaxf(fmaxf(mx, a0[v]), a1[v]);
+        mn = fminf(fminf(mn, a0[v]), a1[v]);
+      }
+      st.rescale(src.take(0, a0, a1, mx, mn, f));
     }
-    st.rescale(src.take(0, a0, a1, mx, mn, f));
     w.set(first);
   }
   __syncthreads();  // K slot 0 is refilled by step 0

@@ -78,6 +78,20 @@ struct CodeTiles {
       m |= low_bits(cached_rows(a, b, len, t * kKeys + 16 * i).n) << (16 * i);
     return m;
   }
+  __device__ __forceinline__ float factor() const { return p.c.sc.c; }
+  __device__ __forceinline__ void mask(int i, f32x16& s0_, f32x16& s1_, float (&mg)[kGroups]) const {
+    const uint64_t m = bits(tile(i));
+    if (m == ~uint64_t(0)) return;
+    mask_block(s0_, static_cast<uint32_t>(m >> (4 * hf)));
+    mask_block(s1_, static_cast<uint32_t>(m >> (32 + 4 * hf)));
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const f32x16& z = g < 2 ? s0_ : s1_;
+      mg[g] = z[8 * (g & 1)];
+#pragma unroll
+      for (int v = 1; v < 8; ++v) mg[g] = fmaxf(mg[g], z[8 * (g & 1) + v]);
+    }
+  }
   __device__ __forceinline__ float take(int i, f32x16& s0_, f32x16& s1_, float mx, float mn,
                                         Form& f) const {
     const CacheArgs& a = p.c;
@@ -165,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void codes_wide_kernel(CacheAttnArgs p) {
                                     turn < c1 - s0 ? turn : 0,
                                     wave,   hf,
                                     slope,  pos};
-      run_code_pipe<D, kCap>(src, q, st, lds0, lane, a.hkv * C::kRow);
+      run_code_pipe<D, kCap, !kCap && !kBias>(src, q, st, lds0, lane, a.hkv * C::kRow);
     }
     // the new tokens' own
     bool cleaned = false;
