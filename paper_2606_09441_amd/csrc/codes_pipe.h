@@ -19,21 +19,25 @@ namespace flash {
 
 constexpr int kGroups = kKeys / 16;
 
-// A tile: this wavefront's 16 rows, and its groups' pages.
+// kPages: 1 where a tile lies in one page, else as many as it has groups.
+// A tile: this wavefront's 16 rows, and its pages.
+template <int kPages>
 struct CodeWhere {
   int64_t row;
   int32_t n;
-  int32_t page[kGroups];
+  int32_t page[kPages];
 };
+template <int kPages>
 struct CodeScales {
-  float k[kGroups], v[kGroups];
+  float k[kPages], v[kPages];
 };
 // A tile's V scales as the weights take them: 2^-lift, and one over the scale.
+template <int kPages>
 struct Lift {
-  float lift[kGroups], undo[kGroups];
-  __device__ __forceinline__ void set(const CodeScales& z) {
+  float lift[kPages], undo[kPages];
+  __device__ __forceinline__ void set(const CodeScales<kPages>& z) {
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int g = 0; g < kPages; ++g) {
       const float s = usable_scale(z.v[g]);
       lift[g] = -__builtin_amdgcn_logf(s);
       undo[g] = __builtin_amdgcn_rcpf(s);
@@ -47,10 +51,12 @@ struct Lift {
 //   rows<kV>(where), scales(where): this wavefront's rows of K or V; the tile's scales
 //   take(i, s0, s1, mx, mn, form) -> bound   as take_tile, of scaled products; kPlain:
 //   mask(i, s0, s1, mx), which only hides what a row does not see, and corrects mx
-template <int D, bool kCap, bool kPlain, typename Src>
+template <int D, int kPages, bool kCap, bool kPlain, typename Src>
 __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowState<D>& st,
                                               int lds0, int lane, int stride) {
   using C = CodeTile<D>;
+  static_assert(kPages == 1 || kPages == kGroups, "");
+  constexpr int kSame = kGroups / kPages;   // groups of a page
   constexpr int kTile = kKeys * C::kRow;
   constexpr int kSteps = D / 16;            // of QK^T: 16 dims each
   constexpr int kEach = 32 / kSteps;        // present scores that go with one
@@ -67,11 +73,14 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
   const bf16x2 ones = bf16x2{static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};
 
   Form f;
-  float fk[kGroups];  // kPlain: K's scales and the scores'
-  Lift w;
-  // The bound of a tile's scores from its groups' largest products.
-  const auto largest = [&](const float (&m)[kGroups]) {
-    return half_max(fmaxf(fmaxf(m[0] * fk[0], m[1] * fk[1]), fmaxf(m[2] * fk[2], m[3] * fk[3])));
+  float fk[kPages];  // kPlain: K's scales and the scores'
+  Lift<kPages> w;
+  // The bound of a tile's scores from its pages' largest products.
+  const auto largest = [&](const float (&m)[kPages]) {
+    float x = m[0] * fk[0];
+#pragma unroll
+    for (int g = 1; g < kPages; ++g) x = fmaxf(x, m[g] * fk[g]);
+    return half_max(x);
   };
   // The weight of score e (0 .. 31) of a tile, with its neighbour, into pb.
   bf16x8 pb[kGroups];
@@ -98,7 +107,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 
   // n0, n1 = K Q^T from K slot `slot`, beside the weights of the tile c0, c1 and issue(s)
   const auto qk_and_weigh = [&](int slot, f32x16& n0, f32x16& n1, const f32x16& c0,
-                                const f32x16& c1, const Form& f, const Lift& w, auto issue) {
+                                const f32x16& c1, const Form& f, const Lift<kPages>& w, auto issue) {
     const float base = st.base();
     float sum = 0.f, le = 0.f;
     u32x4 x[2][2];
@@ -118,9 +127,9 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
                                                    __builtin_bit_cast(bf16x8, q.x[s]), n1, 0, 0, 0);
 #pragma unroll
       for (int u = 0; u < kEach; u += 2) {
-        const int e = s * kEach + u, i = e >> 3;
+        const int e = s * kEach + u, i = (e >> 3) / kSame;
         weigh(e, c0, c1, f, kPlain ? fk[i] : f.p0, base + w.lift[i], sum, le);
-        if ((e & 7) == 6) {  // the group's last
+        if (e % (8 * kSame) == 8 * kSame - 2) {  // the page's last
           st.l = fmaf(sum, w.undo[i], st.l);
           st.le = fmaf(le, w.undo[i], st.le);
           sum = le = 0.f;
@@ -154,8 +163,8 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 
   // Of steps i + 2 and i + 3; the scales of step i + 1.  Tables and scales are asked for
   // a step before they are used.
-  CodeWhere in2 = src.where(2), in3 = src.where(3);
-  CodeScales next;
+  CodeWhere<kPages> in2 = src.where(2), in3 = src.where(3);
+  CodeScales<kPages> next;
   // Slots (byte offsets) of K of steps i, i + 1 and i + 2, and of V's.
   int k0 = 0, k1 = kTile, k2 = 2 * kTile, v0 = 0, v1 = kTile, v2 = 2 * kTile;
   // step i: its tile's scores in c0, c1 with form f; leaves the next in n0, n1
@@ -171,27 +180,29 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
         dma_b128(own + 3 * kTile + v2 + (s - kDmas) * 1024,
                  C::template dma_off<true>(voff, s - kDmas, stride), vrs);
     };
-    const CodeScales now = next;
+    const CodeScales<kPages> now = next;
     if (i < src.mine) {
       // (past the last tile a body like the others: its scores go nowhere)
       qk_and_weigh(k1, n0, n1, c0, c1, f, w, issue);
-      float ks[kGroups];
+      float ks[kPages];
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(now.k[g]);
+      for (int g = 0; g < kPages; ++g) ks[g] = usable_scale(now.k[g]);
       float mx = -INFINITY, mn = INFINITY;
-      float mg[kGroups] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float mg[kPages];
+#pragma unroll
+      for (float& m : mg) m = -INFINITY;
       pv_and(v0, [&](int e) {
 #pragma unroll
         for (int u = 0; u < kDone; u += 2) {
           const int x = e * kDone + u, v = x & 15;
           f32x16& n = x < 16 ? n0 : n1;
           if constexpr (kPlain) {
-            float& m = mg[x >> 3];
+            float& m = mg[(x >> 3) / kSame];
             m = fmaxf(fmaxf(m, n[v]), n[v + 1]);
             asm volatile("" : "+v"(m));  // here, not where it is used
           } else {
-            n[v] *= ks[x >> 3];
-            n[v + 1] *= ks[x >> 3];
+            n[v] *= ks[(x >> 3) / kSame];
+            n[v + 1] *= ks[(x >> 3) / kSame];
             mx = fmaxf(fmaxf(mx, n[v]), n[v + 1]);
             if constexpr (kCap) mn = fminf(fminf(mn, n[v]), n[v + 1]);
           }
@@ -201,7 +212,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
       if (i + 1 < src.mine) {
         if constexpr (kPlain) {
 #pragma unroll
-          for (int g = 0; g < kGroups; ++g) fk[g] = ks[g] * src.factor();
+          for (int g = 0; g < kPages; ++g) fk[g] = ks[g] * src.factor();
           src.mask(i + 1, n0, n1, mg);
           st.rescale(largest(mg));
         } else {
@@ -223,15 +234,15 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
     v0 = v1, v1 = v2, v2 = b;
   };
 
-  const auto bring_k = [&](int slot, const CodeWhere& y) {
+  const auto bring_k = [&](int slot, const CodeWhere<kPages>& y) {
     C::template dma_rows<false>(own + slot * kTile, src.template rows<false>(y), koff, stride);
   };
-  const auto bring_v = [&](int slot, const CodeWhere& y) {
+  const auto bring_v = [&](int slot, const CodeWhere<kPages>& y) {
     C::template dma_rows<true>(own + (3 + slot) * kTile, src.template rows<true>(y), voff, stride);
   };
-  CodeScales first;
+  CodeScales<kPages> first;
   {
-    const CodeWhere in0 = src.where(0), in1 = src.where(1);
+    const CodeWhere<kPages> in0 = src.where(0), in1 = src.where(1);
     bring_k(0, in0);
     bring_v(0, in0);
     bring_k(1, in1);
@@ -244,28 +255,31 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
   __syncthreads();
   f32x16 a0{}, a1{}, b0{}, b1{};
   if (src.mine > 0) {
-    float ks[kGroups];
+    float ks[kPages];
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) ks[g] = usable_scale(first.k[g]);
+    for (int g = 0; g < kPages; ++g) ks[g] = usable_scale(first.k[g]);
     a0 = qk_codes<D>(kaddr, q);
     a1 = qk_codes<D>(kaddr + 32 * C::kRow, q);
     if constexpr (kPlain) {
-      float mg[kGroups] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float mg[kPages];
+#pragma unroll
+      for (float& m : mg) m = -INFINITY;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        mg[v >> 3] = fmaxf(mg[v >> 3], a0[v]);
-        mg[2 + (v >> 3)] = fmaxf(mg[2 + (v >> 3)], a1[v]);
+        float &m0 = mg[(v >> 3) / kSame], &m1 = mg[(2 + (v >> 3)) / kSame];
+        m0 = fmaxf(m0, a0[v]);
+        m1 = fmaxf(m1, a1[v]);
       }
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) fk[g] = ks[g] * src.factor();
+      for (int g = 0; g < kPages; ++g) fk[g] = ks[g] * src.factor();
       src.mask(0, a0, a1, mg);
       st.rescale(largest(mg));
     } else {
       float mx = -INFINITY, mn = INFINITY;
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
-        a0[v] *= ks[v >> 3];
-        a1[v] *= ks[2 + (v >> 3)];
+        a0[v] *= ks[(v >> 3) / kSame];
+        a1[v] *= ks[(2 + (v >> 3)) / kSame];
         mx = fmaxf(fmaxf(mx, a0[v]), a1[v]);
         mn = fminf(fminf(mn, a0[v]), a1[v]);
       }

@@ -12,7 +12,7 @@ namespace {
 using namespace cache;
 
 // Cached tiles s0 .. of a unit.
-template <int D, bool kCap, bool kBias>
+template <int D, int kPages, bool kCap, bool kBias>
 struct CodeTiles {
   const CacheAttnArgs& p;
   int b, len, kvh;
@@ -29,20 +29,19 @@ struct CodeTiles {
     return s0 + (j < steps ? j : j - steps);
   }
   // Step i's tile (past the last step none of its rows).
-  __device__ __forceinline__ CodeWhere where(int i) const {
+  __device__ __forceinline__ CodeWhere<kPages> where(int i) const {
     const CacheArgs& a = p.c;
     const int slot = tile(min(i, steps - 1)) * kKeys;
     const Rows16 r = cached_rows(a, b, len, slot + 16 * wave);
-    CodeWhere y;
+    CodeWhere<kPages> y;
     y.row = r.row;
     y.n = i < steps ? r.n : 0;
-    y.page[0] = static_cast<int32_t>(r.row >> a.page_shift);
+    if constexpr (kPages == 1) {
+      y.page[0] = static_cast<int32_t>(r.row >> a.page_shift);
+      return y;
+    }
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      if (a.page_shift >= 6) {  // one page
-        y.page[g] = y.page[0];
-        continue;
-      }
+    for (int g = 0; g < kPages; ++g) {
       const int pi = min((slot + 16 * g) >> a.page_shift, a.max_pages - 1);
       y.page[g] =
           within(scalar(a.table, static_cast<int64_t>(b) * a.max_pages + pi), a.num_pages - 1);
@@ -50,7 +49,7 @@ struct CodeTiles {
     return y;
   }
   template <bool kV>
-  __device__ __forceinline__ i32x4 rows(const CodeWhere& y) const {
+  __device__ __forceinline__ i32x4 rows(const CodeWhere<kPages>& y) const {
     using C = CodeTile<D>;
     const CacheArgs& a = p.c;
     return rows_rsrc(reinterpret_cast<unsigned long long>(kV ? a.v : a.k) +
@@ -58,10 +57,10 @@ struct CodeTiles {
                      y.n, a.hkv * C::kRow, C::kRow);
   }
   // As they are.
-  __device__ __forceinline__ CodeScales scales(const CodeWhere& y) const {
-    CodeScales z;
+  __device__ __forceinline__ CodeScales<kPages> scales(const CodeWhere<kPages>& y) const {
+    CodeScales<kPages> z;
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
+    for (int g = 0; g < kPages; ++g) {
       const int64_t at = static_cast<int64_t>(y.page[g]) * p.c.hkv + kvh;
       z.k[g] = scalar(p.k_scales, at);
       z.v[g] = scalar(p.v_scales, at);
@@ -79,17 +78,17 @@ struct CodeTiles {
     return m;
   }
   __device__ __forceinline__ float factor() const { return p.c.sc.c; }
-  __device__ __forceinline__ void mask(int i, f32x16& s0_, f32x16& s1_, float (&mg)[kGroups]) const {
+  __device__ __forceinline__ void mask(int i, f32x16& s0_, f32x16& s1_, float (&mg)[kPages]) const {
     const uint64_t m = bits(tile(i));
     if (m == ~uint64_t(0)) return;
     mask_block(s0_, static_cast<uint32_t>(m >> (4 * hf)));
     mask_block(s1_, static_cast<uint32_t>(m >> (32 + 4 * hf)));
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const f32x16& z = g < 2 ? s0_ : s1_;
-      mg[g] = z[8 * (g & 1)];
+    for (float& m : mg) m = -INFINITY;
 #pragma unroll
-      for (int v = 1; v < 8; ++v) mg[g] = fmaxf(mg[g], z[8 * (g & 1) + v]);
+    for (int v = 0; v < 32; ++v) {
+      float& m = mg[(v >> 3) * kPages / kGroups];
+      m = fmaxf(m, v < 16 ? s0_[v & 15] : s1_[v & 15]);
     }
   }
   __device__ __forceinline__ float take(int i, f32x16& s0_, f32x16& s1_, float mx, float mn,
@@ -114,7 +113,7 @@ struct CodeTiles {
   }
 };
 
-template <int D, bool kCap, bool kBias>
+template <int D, int kPages, bool kCap, bool kBias>
 __global__ __launch_bounds__(256, 2) void codes_wide_kernel(CacheAttnArgs p) {
   using T = __bf16;
   using G = Tile<T, D>;
@@ -172,14 +171,14 @@ __global__ __launch_bounds__(256, 2) void codes_wide_kernel(CacheAttnArgs p) {
       // of the same keys read each tile at about the same time (cache_wide.hip).
       const int over = s0 - Split::quotient(s0, run) * run;
       const int turn = over > 0 ? run - over : 0;
-      CodeTiles<D, kCap, kBias> src{p,      b,
+      CodeTiles<D, kPages, kCap, kBias> src{p,      b,
                                     len,    kvh,
                                     s0,     c1 - s0,
                                     any ? c1 - s0 : 0,
                                     turn < c1 - s0 ? turn : 0,
                                     wave,   hf,
                                     slope,  pos};
-      run_code_pipe<D, kCap, !kCap && !kBias>(src, q, st, lds0, lane, a.hkv * C::kRow);
+      run_code_pipe<D, kPages, kCap, !kCap && !kBias>(src, q, st, lds0, lane, a.hkv * C::kRow);
     }
     // the new tokens' own
     bool cleaned = false;
@@ -281,23 +280,29 @@ __global__ __launch_bounds__(256, 2) void codes_wide_kernel(CacheAttnArgs p) {
 }  // namespace
 
 hipError_t launch_codes_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream) {
-  const auto launch = [&](auto dim, auto cap, auto bias) {
-    hipLaunchKernelGGL(
-        (codes_wide_kernel<decltype(dim)::value, decltype(cap)::value, decltype(bias)::value>),
-        dim3(a.groups), dim3(256), 0, stream, a);
+  const auto launch = [&](auto dim, auto pages, auto cap, auto bias) {
+    hipLaunchKernelGGL((codes_wide_kernel<decltype(dim)::value, decltype(pages)::value,
+                                          decltype(cap)::value, decltype(bias)::value>),
+                       dim3(a.groups), dim3(256), 0, stream, a);
   };
-  const auto of = [&](auto dim) {
+  const auto of = [&](auto dim, auto pages) {
     const std::true_type yes;
     const std::false_type no;
     if (a.c.sc.x != 0.f)
-      a.c.sc.slopes != nullptr ? launch(dim, yes, yes) : launch(dim, yes, no);
+      a.c.sc.slopes != nullptr ? launch(dim, pages, yes, yes) : launch(dim, pages, yes, no);
     else
-      a.c.sc.slopes != nullptr ? launch(dim, no, yes) : launch(dim, no, no);
+      a.c.sc.slopes != nullptr ? launch(dim, pages, no, yes) : launch(dim, pages, no, no);
+  };
+  const auto with_pages = [&](auto dim) {
+    if ((1 << a.c.page_shift) >= kKeys)
+      of(dim, std::integral_constant<int, 1>{});
+    else
+      of(dim, std::integral_constant<int, kGroups>{});
   };
   if (head_dim == 128)
-    of(std::integral_constant<int, 128>{});
+    with_pages(std::integral_constant<int, 128>{});
   else
-    of(std::integral_constant<int, 64>{});
+    with_pages(std::integral_constant<int, 64>{});
   return hipGetLastError();
 }
 
