@@ -22,15 +22,19 @@ constexpr int kTileKeys = Narrow::kTileKeys;
 constexpr int kStepTiles = Narrow::kStepTiles;
 constexpr int kRows = Narrow::kRows;
 
-// A tile of cached keys: its two groups of 16 rows, and their scales.
+// A tile of cached keys, in one page or two of 16: its rows, as many of them as are
+// valid, and the scales.
+template <int kPages>
 struct CodeRows {
-  Rows16 r[2];
+  int64_t row[kPages];
+  int32_t n[kPages];
 };
+template <int kPages>
 struct Scales {
-  float k[2], v[2];
+  float k[kPages], v[kPages];
 };
 
-template <int D, bool kCap, bool kBias>
+template <int D, int kPages, bool kCap, bool kBias>
 __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
   using T = __bf16;
   using G = Tile<T, D>;       // of the new tokens' keys
@@ -38,6 +42,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
   constexpr int kTile = kTileKeys * G::kRow;
   constexpr int kCodes = kTileKeys * C::kRow;  // half of it
   constexpr int kDmas = 2 * C::kGroupDmas;     // of a K or V tile
+  constexpr int kEach = kTileKeys / kPages;    // keys of a page
   __shared__ __attribute__((aligned(1024))) uint8_t smem[4 * 2 * kTile];
   __shared__ float part[4][kRows][3];
   const CacheArgs& a = p.c;
@@ -91,33 +96,42 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
     const int my_pos = !kBias ? 0 : a.row_pos != nullptr ? a.row_pos[row0 + node] : len + node;
 
     const auto rows_of = [&](int t) {
-      CodeRows y;
+      CodeRows<kPages> y;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        y.r[i] = cached_rows(a, b, len, t * kTileKeys + 16 * i);
+      for (int i = 0; i < kPages; ++i) {
+        const int slot = t * kTileKeys + i * kEach;
+        const Rows16 r = cached_rows(a, b, len, slot);
+        y.row[i] = r.row;
+        y.n[i] = r.n;
+        if constexpr (kEach > 16) {  // the same page's next 16
+          if (r.n == 16) y.n[i] += cached_rows(a, b, len, slot + 16).n;
+        }
       }
       return y;
     };
-    const auto scales_of = [&](const CodeRows& y) {
-      Scales z;
+    const auto scales_of = [&](const CodeRows<kPages>& y) {
+      Scales<kPages> z;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int64_t at = (y.r[i].row >> a.page_shift) * a.hkv + kvh;
+      for (int i = 0; i < kPages; ++i) {
+        const int64_t at = (y.row[i] >> a.page_shift) * a.hkv + kvh;
         z.k[i] = scalar(p.k_scales, at);
         z.v[i] = scalar(p.v_scales, at);
       }
       return z;
     };
-    const auto fetch = [&](const CodeRows& y, int slot, auto v) {
+    const auto fetch = [&](const CodeRows<kPages>& y, int slot, auto v) {
       constexpr bool kV = decltype(v)::value;
       const void* base = kV ? a.v : a.k;
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        C::template dma_rows<kV>((kV ? vt : kt) + slot * kCodes + i * 16 * C::kRow,
-                                 rows_rsrc(reinterpret_cast<unsigned long long>(base) +
-                                               (y.r[i].row * a.hkv + kvh) * C::kRow,
-                                           y.r[i].n, stride, C::kRow),
-                                 kV ? voff : koff, stride);
+      for (int i = 0; i < kPages; ++i) {
+        const i32x4 rs = rows_rsrc(reinterpret_cast<unsigned long long>(base) +
+                                       (y.row[i] * a.hkv + kvh) * C::kRow,
+                                   y.n[i], stride, C::kRow);
+#pragma unroll
+        for (int j = 0; j < kEach; j += 16)
+          C::template dma_rows<kV>((kV ? vt : kt) + slot * kCodes + (i * kEach + j) * C::kRow, rs,
+                                   kV ? voff : koff, stride, j);
+      }
     };
     constexpr std::false_type kK{};
     constexpr std::true_type kV{};
@@ -127,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
     // Products sc of the tile that begins with key j0 (of the cache, or of the new ones),
     // of whose keys this row sees `bits`, to the exponents' form, and the reference moved:
     // what is left is c (times K's scales) and the returned offset.
-    const auto shape = [&](f32x16& sc, uint32_t bits, bool fresh, int j0, float (&f)[2]) {
+    const auto shape = [&](f32x16& sc, uint32_t bits, bool fresh, int j0, const float (&f)[2]) {
       if constexpr (kCap) cap_scores(a.sc, sc);
       if (__builtin_amdgcn_ballot_w64(bits != ~0u)) mask_block(sc, bits >> (4 * hf));
       float off = 0.f;
@@ -139,7 +153,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         };
         if ((fresh ? a.row_pos : a.key_pos) != nullptr) {
           float dist[16];
-  #pragma unroll
+#pragma unroll
           for (int v = 0; v < 16; ++v) {
             const int j = j0 + 4 * hf + key_of(v);
             const int pos =
@@ -171,23 +185,23 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
     const int cend = min(ct, tend);
     int t = first * kStepTiles + wave;
     if (t < cend) {
-      // of this tile and of the next; the scales are asked for behind the rows
-      CodeRows now = rows_of(t), next = rows_of(min(t + kStepTiles, cend - 1));
+      // Of this tile, the next and the one after; the scales are asked for behind the rows.
+      // In the loop, tables and scales are asked for while the weights are made: an answer
+      // that is on its way would hold up reads of LDS, which count with it.
+      CodeRows<kPages> now = rows_of(t), next = rows_of(min(t + kStepTiles, cend - 1));
       fetch(now, 0, kK);
       fetch(now, 0, kV);
       if (t + kStepTiles < cend) {
         fetch(next, 1, kK);
         fetch(next, 1, kV);
       }
-      Scales mine = scales_of(now);
+      CodeRows<kPages> after = rows_of(min(t + 2 * kStepTiles, cend - 1));
+      Scales<kPages> mine = scales_of(now);
       int slot = 0;
       for (; t < cend; t += kStepTiles, slot ^= 1) {
         const bool one = t + kStepTiles < cend, two = t + 2 * kStepTiles < cend;
-        const uint32_t bits = static_cast<uint32_t>(low_bits(now.r[0].n)) |
-                              static_cast<uint32_t>(low_bits(now.r[1].n)) << 16;
-        CodeRows after{};
-        if (two) after = rows_of(t + 2 * kStepTiles);
-        const Scales then = scales_of(next);
+        uint32_t bits = static_cast<uint32_t>(low_bits(now.n[0]));
+        if constexpr (kPages == 2) bits |= static_cast<uint32_t>(low_bits(now.n[1])) << 16;
         if (one)
           wait_vm<3 * kDmas>();  // K is there, V and the next tile may still be on their way
         else
@@ -195,18 +209,25 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         f32x16 sc = qk_codes<D>(kt + slot * kCodes + klane, q);
         wait_lds();  // K is read
         if (two) fetch(after, slot, kK);
+        const CodeRows<kPages> third = rows_of(min(t + 3 * kStepTiles, cend - 1));
+        const Scales<kPages> then = scales_of(next);
         float f[2], base[2], undo[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kPages; ++i) {
           const float ks = usable_scale(mine.k[i]), vs = usable_scale(mine.v[i]);
           f[i] = ks * c;
           if constexpr (kCap || kBias) {
 #pragma unroll
-            for (int v = 8 * i; v < 8 * i + 8; ++v) sc[v] *= ks;
+            for (int v = i * kEach / 2; v < (i + 1) * kEach / 2; ++v) sc[v] *= ks;
             f[i] = c;
           }
           base[i] = -__builtin_amdgcn_logf(vs);
           undo[i] = __builtin_amdgcn_rcpf(vs);
+        }
+        if constexpr (kPages == 1) {
+          f[1] = f[0];
+          base[1] = base[0];
+          undo[1] = undo[0];
         }
         const float off = shape(sc, bits, false, t * kTileKeys, f);
 #pragma unroll
@@ -223,6 +244,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         if (two) fetch(after, slot, kV);
         now = next;
         next = after;
+        after = third;
         mine = then;
       }
     }
@@ -293,23 +315,29 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
 }  // namespace
 
 hipError_t launch_cache_codes(const CacheAttnArgs& a, int head_dim, hipStream_t stream) {
-  const auto launch = [&](auto dim, auto cap, auto bias) {
-    hipLaunchKernelGGL(
-        (cache_codes_kernel<decltype(dim)::value, decltype(cap)::value, decltype(bias)::value>),
-        dim3(a.groups), dim3(256), 0, stream, a);
+  const auto launch = [&](auto dim, auto pages, auto cap, auto bias) {
+    hipLaunchKernelGGL((cache_codes_kernel<decltype(dim)::value, decltype(pages)::value,
+                                           decltype(cap)::value, decltype(bias)::value>),
+                       dim3(a.groups), dim3(256), 0, stream, a);
   };
-  const auto of = [&](auto dim) {
+  const auto of = [&](auto dim, auto pages) {
     const std::true_type yes;
     const std::false_type no;
     if (a.c.sc.x != 0.f)
-      a.c.sc.slopes != nullptr ? launch(dim, yes, yes) : launch(dim, yes, no);
+      a.c.sc.slopes != nullptr ? launch(dim, pages, yes, yes) : launch(dim, pages, yes, no);
     else
-      a.c.sc.slopes != nullptr ? launch(dim, no, yes) : launch(dim, no, no);
+      a.c.sc.slopes != nullptr ? launch(dim, pages, no, yes) : launch(dim, pages, no, no);
+  };
+  const auto with_pages = [&](auto dim) {
+    if ((1 << a.c.page_shift) >= kTileKeys)
+      of(dim, std::integral_constant<int, 1>{});
+    else
+      of(dim, std::integral_constant<int, 2>{});
   };
   if (head_dim == 128)
-    of(std::integral_constant<int, 128>{});
+    with_pages(std::integral_constant<int, 128>{});
   else
-    of(std::integral_constant<int, 64>{});
+    with_pages(std::integral_constant<int, 64>{});
   return hipGetLastError();
 }
 

@@ -55,12 +55,13 @@ struct CodeTile {
     const int row = j * kDmaRows;
     return (off0 ^ (16 * (kV ? swz_v(row) : swz_k(row)))) + row * stride;
   }
-  // DMA of 16 rows into LDS at `lds`.
+  // DMA of 16 rows into LDS at `lds`, the resource's from row `from` (a multiple of 16) on.
   template <bool kV>
-  static __device__ __forceinline__ void dma_rows(int lds, const i32x4& rs, int off0, int stride) {
+  static __device__ __forceinline__ void dma_rows(int lds, const i32x4& rs, int off0, int stride,
+                                                  int from = 0) {
 #pragma unroll
     for (int j = 0; j < kGroupDmas; ++j)
-      dma_b128(lds + j * 1024, dma_off<kV>(off0, j, stride), rs);
+      dma_b128(lds + j * 1024, dma_off<kV>(off0, j, stride) + from * stride, rs);
   }
 
   // A operands of S^T: chunk 2 u + hf of row l32, dims 32 u + 16 hf and on, the first
