@@ -771,6 +771,22 @@ class Rotary:
             check(fn, st)
         return q_out, k_out
 
+    def _turn_back(self, dq, dk, positions, back):
+        """rotate of gradients, which are as the outputs that rotate checked."""
+        torch = _torch()
+        kind = _kinds[dq.dtype]
+        qo, kd, ko = torch.empty_like(dq), None, None
+        if dk is not None:
+            out = torch.empty_like(dk)
+            kd = SiftTensor(dk.data_ptr(), kind, *dk.shape)
+            ko = SiftTensor(out.data_ptr(), kind, *dk.shape)
+        st = lib().sift_rotate(SiftTensor(dq.data_ptr(), kind, *dq.shape), kd, positions.data_ptr(),
+                               self.struct, back, SiftTensor(qo.data_ptr(), kind, *dq.shape), ko,
+                               _stream_ptr(None))
+        if st:
+            check("sift_rotate", st)
+        return qo, None if dk is None else out
+
     def rotate_(self, q, k, positions, back=False, stream=None):
         """rotate in place."""
         return self.rotate(q, k, positions, back, q, k, stream)
@@ -801,11 +817,11 @@ def _turn_function():
             def backward(ctx, dq, dk):
                 positions, = ctx.saved_tensors
                 # (a gradient may be a view, or expanded)
-                args = (dq.contiguous(), dk.contiguous() if ctx.pair else None, positions)
+                dq, dk = dq.contiguous(), dk.contiguous() if ctx.pair else None
                 if torch.is_grad_enabled():   # a gradient of the gradient may be asked for
-                    dq, dk = _turn_class.apply(*args, ctx.rotary, not ctx.back)
+                    dq, dk = _turn_class.apply(dq, dk, positions, ctx.rotary, not ctx.back)
                 else:
-                    dq, dk = ctx.rotary.rotate(*args, not ctx.back)
+                    dq, dk = ctx.rotary._turn_back(dq, dk, positions, not ctx.back)
                 return dq, dk, None, None, None
 
         _turn_class = Turn
