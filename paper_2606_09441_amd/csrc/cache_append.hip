@@ -2,7 +2,8 @@
 // turned by their positions on the way.  HBM bounds it: every number is read once and
 // written once.
 //
-// Pages of the new keys' own type: a wavefront takes a token, or part of its heads.
+// Pages of the new keys' own type: a wavefront takes a token, or part of its heads.  65
+// thousand rows of 8 heads, D = 128, into bf16 pages: 95 us, 5.6 TB/s.
 //
 // e4m3 pages hold x / scale, a scale for each page and kv head: a workgroup takes a
 // page that new keys enter, of a head.  The scale has to be known before the first code
@@ -13,6 +14,9 @@
 //    factor would gain nothing; a power of two loses nothing in the division, and keys
 //    that a page holds already keep their values when its scale grows, but for those
 //    below the smallest normal one.
+//  * 16640 rows of 8 heads into empty pages: 27 us of the kernel, of which 20 are the
+//    bytes' at a copy's rate and the rest a workgroup's way to its first row (sequence,
+//    table) and from its last (maximum, codes).  A token of each of 32 sequences: 5.7 us.
 //  * The bound of a turned pair is sqrt(2) times its larger half, whatever the angle: the
 //    scale depends on no cosine, and is the same for keys moved to other positions.
 
@@ -427,7 +431,10 @@ __global__ __launch_bounds__(256) void lens_kernel(CacheAppendArgs p) {
   p.lens_out[b] = s.len + min(s.n, slots - s.len);
 }
 
-constexpr int64_t kAppendWaves = 4096;  // that a launch of few tokens is split into
+// Wavefronts that a launch of few tokens is split into (us of 8 heads, D = 128, bf16, one
+// a token / 4096 / 32768: 4 tokens 3.5 / 3.2 / 3.2, 400 4.4 / 4.0 / 4.0, 2000 6.4 / 6.4 /
+// 6.6).
+constexpr int64_t kAppendWaves = 4096;
 
 }  // namespace
 

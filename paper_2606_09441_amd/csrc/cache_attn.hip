@@ -287,6 +287,11 @@ __global__ __launch_bounds__(256) void cache_merge_kernel(CacheAttnArgs p, int e
 // 88 / 65, of 32768 48 / 46; 128 rows of 32768 59 / 54, of 16384 40 / 44; 256 rows of
 // 16384 55 / 55, of 4096 29 / 38; 32 rows of 65536 54 / 61.
 constexpr int64_t kNarrowMost = int64_t(24) << 20;
+// e4m3: the narrow units read half as much, the wide ones turn codes into bf16 for fewer
+// rows each.  us of narrow / wide at 48/8 heads: 64 tokens of 16384 slots 61 / 61, of 32768
+// 115 / 92; 22 of 32768 50 / 61, of 65536 98 / 98; 32 of 65536 127 / 104; 8 sequences of
+// 16384, 12 tokens each 148 / 109; 16 of 2048, 64 each 147 / 171.
+constexpr int64_t kNarrowMostCodes = int64_t(48) << 20;
 
 // Workgroups of the merge: as many as are resident at once, since where there are
 // many items most have nothing to merge and a workgroup of its own costs more than
@@ -294,8 +299,9 @@ constexpr int64_t kNarrowMost = int64_t(24) << 20;
 // 512 keys, 65536 items 299 / 218, 8192 items 133 / 125; up to 1024 items the same).
 constexpr int64_t kMergeGroups = 2048;
 
-bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys) {
-  return bf16 && rows_of_kv > kRows && rows_of_kv >= (kNarrowMost + keys - 1) / keys;
+bool cache_attn_wide(Pool pool, int64_t rows_of_kv, int64_t keys) {
+  const int64_t most = pool == Pool::kE4m3 ? kNarrowMostCodes : kNarrowMost;
+  return pool != Pool::kF32 && rows_of_kv > kRows && rows_of_kv >= (most + keys - 1) / keys;
 }
 
 int64_t cache_attn_steps(const CacheArgs& a, bool codes) {
@@ -317,7 +323,7 @@ hipError_t launch_cache_attn(const CacheAttnArgs& a, Pool pool, int head_dim, hi
   const int64_t most = static_cast<int64_t>(std::min(a.c.rows, a.c.max_rows)) * (a.c.hq / a.c.hkv);
   const bool codes = pool == Pool::kE4m3;
   const bool wide = cache_attn_wide(
-      pool != Pool::kF32, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
+      pool, most, (static_cast<int64_t>(a.c.max_pages) << a.c.page_shift) * a.c.num_seqs * a.c.hkv);
   const auto launch = [&](auto elem, auto dim) {
     using T = decltype(elem);
     constexpr int D = decltype(dim)::value;

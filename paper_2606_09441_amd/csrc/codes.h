@@ -1,6 +1,8 @@
 // Tiles of e4m3 codes in LDS, and how lanes read them as bf16 operands: every code is
 // a bf16 number, so nothing is lost but the page's scale, which goes to the scores (K)
-// and to the weights (V).
+// and to the weights (V).  (The 8-bit matrix instructions, which would take K's codes as
+// they are beside queries split in two, add with too few bits: off by 2^-13 of the sum of
+// the products' sizes, as measured over 64 of them, where fp32 allows 2^-24 each.)
 #pragma once
 
 #include "flash.h"

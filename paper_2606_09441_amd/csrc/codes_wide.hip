@@ -1,6 +1,10 @@
 // The attention of many new tokens over a paged cache held in e4m3: units of 128 rows of
 // a (sequence, kv head), as in cache_wide.hip, over the pipeline of codes_pipe.h.  The new
-// tokens' own keys, bf16 tiles, are taken last and one at a time.
+// tokens' own keys, bf16 tiles, are taken last and one at a time.  64 tokens, 48/8 heads, D
+// = 128 over 66048 slots: 150 us of the call with its merge (bf16 152), 700 TFLOP/s, the VALU busy in 59% of the SIMDs' cycles, the
+// MFMAs in 30%: some 430 vector operations a wavefront and tile, 128 of them conversions,
+// beside 32 matrix instructions.  Kernels of their own for tiles in one page keep a scale
+// where four would be, and spill less (25 registers a lane, not 34): 150 us, not 162.
 
 #include "cache.h"
 #include "codes_pipe.h"

@@ -501,7 +501,7 @@ struct CacheAttnArgs {
 constexpr int kCacheRows = 32, kCacheWideRows = 128;
 // rows_of_kv: the most rows of a (sequence, kv head); keys: slots of all of them.
 // A launch's list of steps (cache_attn_steps bounds it) has to be shorter than 2^31.
-bool cache_attn_wide(bool bf16, int64_t rows_of_kv, int64_t keys);
+bool cache_attn_wide(Pool pool, int64_t rows_of_kv, int64_t keys);
 int64_t cache_attn_steps(const CacheArgs& a, bool codes);
 hipError_t launch_cache_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
 hipError_t launch_codes_wide(const CacheAttnArgs& a, int head_dim, hipStream_t stream);
