@@ -290,6 +290,18 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     const bool begun = lo > 0;
     const float old_k = begun ? p.k_scales[sc] : 0.f, old_v = begun ? p.v_scales[sc] : 0.f;
 
+    // this lane's frequencies, for all its rows
+    double freq[8] = {};
+    if constexpr (kTurns == kHalves) {
+      if (8 * c0 < p.r.half)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) freq[e] = rotary::frequency(p.r, 8 * c0 + e);
+    } else if constexpr (kTurns == kPairs) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)  // (8 item + e: the chunks are neighbours)
+        freq[e] = rotary::frequency(p.r, min(8 * item + e, p.r.half - 1));
+    }
+
     // their largest sizes
     const float grow = kRoot2 * p.r.magnitude;  // of dims that turn
     float mk, mv;
@@ -302,14 +314,15 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             v = larger_bits(v, vx[i][j][e]);
-            if (kTurns != kNone && 4 * (j ? c1 : c0) + e < p.r.half)
+            if (kTurns > kHalves && 4 * (j ? c1 : c0) + e < p.r.half)
               r = larger_bits(r, kx[i][j][e]);
             else
               k = larger_bits(k, kx[i][j][e]);
           }
       mk = size_of(k);
       mv = size_of(v);
-      if (kTurns != kNone) mk = fmaxf(mk, size_of(r) * grow);
+      if (kTurns == kHalves && 8 * c0 < p.r.half) mk *= grow;  // all of the item's, or none
+      if (kTurns > kHalves) mk = fmaxf(mk, size_of(r) * grow);
     }
     if (__syncthreads_or(mk == INFINITY || mv == INFINITY)) {  // without what is not finite
       float r = 0.f;
@@ -378,22 +391,22 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) k[j].set(kx[i][j]);
       if constexpr (kTurns == kHalves) {
-        if (8 * c0 < p.r.half) {
-          rotary::Item<__bf16, false> it;
-          it.angles(p.r, pos, item);
-          it.apply(k);
-        }
+        if (8 * c0 < p.r.half)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float c, sn;
+            rotary::turn<__bf16>(p.r, pos, freq[e], c, sn);
+            rotary::rotate(c, sn, k[0].x[e], k[1].x[e]);
+          }
       } else if constexpr (kTurns == kPairs) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int i2 = 4 * (j ? c1 : c0) + e;
-            if (i2 >= p.r.half) continue;
-            float c, sn;
-            rotary::turn<__bf16>(p.r, pos, i2, c, sn);
-            rotary::rotate(c, sn, k[j].x[2 * e], k[j].x[2 * e + 1]);
-          }
+        for (int e = 0; e < 8; ++e) {
+          if (8 * item + e >= p.r.half) break;
+          float c, sn;
+          rotary::turn<__bf16>(p.r, pos, freq[e], c, sn);
+          C& x = k[e >> 2];
+          rotary::rotate(c, sn, x.x[2 * (e & 3)], x.x[2 * (e & 3) + 1]);
+        }
       } else if constexpr (kTurns == kAny) {  // halves of no whole chunks
         const __bf16* const kr = static_cast<const __bf16*>(p.k) + ((src + r) * a.hkv + h) * D;
 #pragma unroll

@@ -24,15 +24,16 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // Cosine and sine of 2 pi turns.
 template <bool kFull>
 __device__ __forceinline__ void unit(double turns, float& c, float& s) {
-  const double r = turns - rint(turns);
   if constexpr (!kFull) {
     // the hardware's, of a fraction of a turn: off by some 1e-6, where the result is
     // rounded to 8 bits of significand
-    c = __builtin_amdgcn_cosf(static_cast<float>(r));
-    s = __builtin_amdgcn_sinf(static_cast<float>(r));
+    const float r = static_cast<float>(__builtin_amdgcn_fract(turns));
+    c = __builtin_amdgcn_cosf(r);
+    s = __builtin_amdgcn_sinf(r);
   } else {
     // the nearest quarter turn, and Taylor's polynomials of the rest, |y| <= pi / 4:
     // the first terms left out are below y^11 / 11! = 1.8e-9 and y^12 / 12! = 1.2e-10
+    const double r = turns - rint(turns);
     const double quarter = rint(4.0 * r);
     const float y = static_cast<float>((r - 0.25 * quarter) * 6.283185307179586);
     const float w = y * y;
@@ -49,14 +50,21 @@ __device__ __forceinline__ void unit(double turns, float& c, float& s) {
   }
 }
 
-// The same of an angle, times the magnitude; back: of the negative angle.
+// Turns a position that frequency i makes.
+__device__ __forceinline__ double frequency(const RotaryArgs& r, int i) {
+  return static_cast<double>(r.inv_freq[i]) * 0.15915494309189535;  // 1 / (2 pi)
+}
+// Cosine and sine of a position's angle, times the magnitude; back: of the negative angle.
 template <typename T>
-__device__ __forceinline__ void turn(const RotaryArgs& r, int position, int i, float& c, float& s) {
-  constexpr double kTurn = 0.15915494309189535;  // 1 / (2 pi)
-  unit<std::is_same<T, float>::value>(
-      static_cast<double>(position) * static_cast<double>(r.inv_freq[i]) * kTurn, c, s);
+__device__ __forceinline__ void turn(const RotaryArgs& r, int position, double frequency, float& c,
+                                     float& s) {
+  unit<std::is_same<T, float>::value>(static_cast<double>(position) * frequency, c, s);
   c *= r.magnitude;
   s *= r.back ? -r.magnitude : r.magnitude;
+}
+template <typename T>
+__device__ __forceinline__ void turn(const RotaryArgs& r, int position, int i, float& c, float& s) {
+  turn<T>(r, position, frequency(r, i), c, s);
 }
 
 // 16 bytes as numbers and back, rounded to the nearest.
