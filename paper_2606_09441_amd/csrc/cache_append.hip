@@ -53,7 +53,7 @@ __device__ __forceinline__ void write_lens(const CacheAppendArgs& p) {
 }
 
 // How a head's dims turn.
-enum Turns { kNone, kHalves, kPairs, kAny };
+enum Turns { kNone, kHalves, kPairs, kAny, kAnyPairs };
 
 // ---------------------------------------------------------------------------
 // pages of the keys' own type
@@ -63,6 +63,7 @@ template <typename T, int kTurns>
 __global__ __launch_bounds__(256) void append_kernel(CacheAppendArgs p, int parts) {
   constexpr int n = Chunk<T>::kCount;
   const CacheArgs& a = p.c;
+  __shared__ u32x4 others[kTurns == kAny ? 4 : 1][kTurns == kAny ? 64 : 1];
   const int lane = threadIdx.x & 63;
   const int slots = a.max_pages << a.page_shift;
   write_lens(p);
@@ -115,21 +116,24 @@ __global__ __launch_bounds__(256) void append_kernel(CacheAppendArgs p, int part
       }
       from = 2 * p.r.half / n;
     }
-    if constexpr (kTurns == kAny) {
-      for (int e = part * 64 + lane; e < a.hkv * p.r.half; e += parts * 64) {
-        const int h = e / p.r.half, i = e - h * p.r.half;
-        const int d0 = p.r.interleaved ? 2 * i : i, d1 = p.r.interleaved ? 2 * i + 1 : p.r.half + i;
-        float c, sn;
-        rotary::turn<T>(p.r, pos, i, c, sn);
-        float x = static_cast<float>(k[h * p.d + d0]), y = static_cast<float>(k[h * p.d + d1]);
-        rotary::rotate(c, sn, x, y);
-        ko[h * p.d + d0] = static_cast<T>(x);
-        ko[h * p.d + d1] = static_cast<T>(y);
-      }
-      const int rest = p.d - 2 * p.r.half;
-      for (int e = part * 64 + lane; e < a.hkv * rest; e += parts * 64) {
-        const int h = e / rest, i = 2 * p.r.half + e - h * rest;
-        ko[h * p.d + i] = k[h * p.d + i];
+    if constexpr (kTurns == kAny || kTurns == kAnyPairs) {
+      constexpr bool kInterleaved = kTurns == kAnyPairs;
+      const int at_once = 64 / chunks;  // heads
+      const int chunk = lane % chunks, sub = lane / chunks;
+      u32x4* const seen = others[kInterleaved ? 0 : threadIdx.x >> 6];
+      rotary::AnyChunk<T, kInterleaved> it;
+      it.angles(p.r, pos, chunk);
+#pragma unroll 2
+      for (int h = part * at_once + sub; h < a.hkv; h += parts * at_once) {
+        const int at = h * p.d + chunk * n;
+        const u32x4 raw = *reinterpret_cast<const u32x4*>(k + at);
+        if constexpr (!kInterleaved) seen[lane] = raw;
+        rotary::lds_order();
+        Chunk<T> x;
+        x.set(raw);
+        it.apply(p.r, x, reinterpret_cast<const T*>(seen + sub * chunks));
+        rotary::lds_order();
+        *reinterpret_cast<u32x4*>(ko + at) = x.get();
       }
       from = chunks;
     }
@@ -246,6 +250,7 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
   using C = Chunk<__bf16>;
   constexpr int kItems = D / 16;  // of a row
   __shared__ float part[2][4];
+  __shared__ u32x4 seen[kTurns == kAny ? 256 : 1][2];
   const CacheArgs& a = p.c;
   const int slots = a.max_pages << a.page_shift;
   write_lens(p);
@@ -408,7 +413,12 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
           rotary::rotate(c, sn, x.x[2 * (e & 3)], x.x[2 * (e & 3) + 1]);
         }
       } else if constexpr (kTurns == kAny) {  // halves of no whole chunks
-        const __bf16* const kr = static_cast<const __bf16*>(p.k) + ((src + r) * a.hkv + h) * D;
+        // (a row's lanes, neighbours in a wavefront, leave it in LDS)
+        seen[threadIdx.x][0] = kx[i][0];
+        seen[threadIdx.x][1] = kx[i][1];
+        rotary::lds_order();
+        const __bf16* const kr =
+            reinterpret_cast<const __bf16*>(&seen[threadIdx.x - item][0]);
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -421,6 +431,7 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
             const float other = static_cast<float>(kr[low ? d + p.r.half : d - p.r.half]);
             k[j].x[e] = fmaf(k[j].x[e], c, low ? -(other * sn) : other * sn);
           }
+        rotary::lds_order();
       }
       const int64_t at = ((row + r) * a.hkv + h) * D;
 #pragma unroll
@@ -508,6 +519,8 @@ hipError_t launch_cache_append(CacheAppendArgs a, Pool pool, hipStream_t stream)
       };
       if (a.r.half == 0)
         go(std::integral_constant<int, kNone>{});
+      else if (!rotary::by_items<T>(a.r, a.d) && a.r.interleaved)
+        go(std::integral_constant<int, kAnyPairs>{});
       else if (!rotary::by_items<T>(a.r, a.d))
         go(std::integral_constant<int, kAny>{});
       else if (a.r.interleaved)

@@ -127,6 +127,60 @@ struct Item {
   }
 };
 
+// A lane's chunk of a head whose pairs lie anywhere: of each of its dims the cosine, the
+// sine with the sign that the other one of its pair takes, and where that one is.
+template <typename T, bool kInterleaved>
+struct AnyChunk {
+  static constexpr int kCount = Chunk<T>::kCount;
+  float c[kCount], s[kCount];
+  int first;  // dim
+  __device__ __forceinline__ void angles(const RotaryArgs& r, int position, int chunk) {
+    first = chunk * kCount;
+#pragma unroll
+    for (int e = 0; e < kCount; ++e) {
+      const int d = first + e;
+      c[e] = 1.f;
+      s[e] = 0.f;
+      if (d >= 2 * r.half) continue;  // stays
+      if (kInterleaved && (e & 1)) {
+        c[e] = c[e - 1];
+        s[e] = -s[e - 1];
+        continue;
+      }
+      const bool low = kInterleaved || d < r.half;
+      turn<T>(r, position, kInterleaved ? d / 2 : low ? d : d - r.half, c[e], s[e]);
+      if (low) s[e] = -s[e];
+    }
+  }
+  // x: the chunk; head: where the head's chunks lie in LDS, as the lanes of this wavefront
+  // left them.
+  __device__ __forceinline__ void apply(const RotaryArgs& r, Chunk<T>& x, const T* head) const {
+    Chunk<T> y;
+#pragma unroll
+    for (int e = 0; e < kCount; ++e) {
+      const int d = first + e;
+      float other;
+      if constexpr (kInterleaved)
+        other = x.x[e ^ 1];
+      else
+        other = static_cast<float>(head[d < r.half ? d + r.half : d - r.half]);
+      y.x[e] = d < 2 * r.half ? fmaf(x.x[e], c[e], other * s[e]) : x.x[e];
+    }
+    x = y;
+  }
+};
+
+// Between a wavefront's writes to LDS of its own and its lanes' reads of them, and back: the
+// hardware keeps their order, so must the compiler.
+__device__ __forceinline__ void lds_order() { asm volatile("" ::: "memory"); }
+
+// Whether rows of D dims go by chunks, pairs wherever they are: whole chunks, a head's in a
+// wavefront.
+template <typename T>
+__host__ __device__ inline bool by_chunks(int d) {
+  return d % Chunk<T>::kCount == 0 && d / Chunk<T>::kCount <= 64;
+}
+
 // Whether rows of D dims go by items: 16-byte chunks of them hold whole pairs, or whole
 // stretches of a half, and a wavefront holds a head's.
 template <typename T>
