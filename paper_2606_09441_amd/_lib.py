@@ -308,13 +308,21 @@ def layout_struct(seg_offsets, prompt_seg_ptr):
     return lay, (so, ps)  # keep the arrays alive with the struct
 
 
+def _device() -> int:
+    """torch.cuda.current_device(), of calls on tensors that are on a GPU: without the
+    check whether there is one."""
+    torch = _torch()
+    get = getattr(torch._C, "_cuda_getDevice", None)
+    return torch.cuda.current_device() if get is None else get()
+
+
 def _stream_ptr(stream):
     if stream is not None:
         return ctypes.c_void_p(stream.cuda_stream)
     torch = _torch()
     raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # without a Stream object
     if raw is not None:
-        return raw(torch.cuda.current_device())
+        return raw(_device())
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
@@ -486,9 +494,12 @@ def _empty(shape, dtype, device, stream):
 
 
 def _desc(fn, t, name, device) -> SiftTensor:
-    if getattr(t, "device", None) != device:
+    try:
+        shape, kind, where = t.shape, _kinds.get(t.dtype), t.device
+    except AttributeError:
+        where = None
+    if where != device:
         raise SiftError(fn, 7, f"{name} is not on {device}")
-    shape, kind = t.shape, _kinds.get(t.dtype)
     if kind is None or len(shape) != 3 or not t.is_contiguous():
         return tensor_desc(t)   # says what is wrong
     return SiftTensor(t.data_ptr(), kind, shape[0], shape[1], shape[2])
@@ -502,7 +513,11 @@ def score_struct(fn, scale, cap, slopes, num_q_heads, device) -> SiftScore:
     """The score transform's arguments, its slopes checked."""
     if slopes is not None:
         require(fn, slopes, "slopes", "float32", num_q_heads, device)
-    return SiftScore(0.0 if scale is None else scale, cap, 0 if slopes is None else slopes.data_ptr())
+        return SiftScore(0.0 if scale is None else scale, cap, slopes.data_ptr())
+    return _PLAIN_SCORE if scale is None and cap == 0.0 else SiftScore(scale or 0.0, cap, 0)
+
+
+_PLAIN_SCORE = SiftScore(0.0, 0.0, 0)   # (never written)
 
 
 def sparse_prefill(q, k, v, seg_offsets, prompt_seg_ptr, la, ca, tile=64, out=None, stream=None):
@@ -830,7 +845,7 @@ def _turn_function():
 
 def _current(fn, device):
     """Kernels go to the current device: the tensors' own."""
-    if device.index != _torch().cuda.current_device():
+    if device.index != _device():
         raise SiftError(fn, 7, f"the tensors are on {device}, which is not the current device")
 
 
@@ -1003,24 +1018,25 @@ class Cache:
         many of each); tree_mask int64 [rows, words] holds each row's visible new
         tokens as bits (None: those up to itself); row_pos int32 [rows].  lse: float32
         [rows, Hq] buffer that receives the rows' log sum exp."""
-        fn = "sift_cache_attention"
+        fn, dev = "sift_cache_attention", self.device
         rows = self._rows(fn, q, row_ptr, row_pos)
         words = 0
         if tree_mask is not None:
             words = (self.max_rows + 63) // 64
             if tree_mask.dim() == 2:
                 words = max(words, tree_mask.shape[1])
-            require(fn, tree_mask, "tree_mask", "int64", q.shape[0] * words, self.device)
-        score = score_struct(fn, scale, cap, slopes, self.hq, self.device)
+            require(fn, tree_mask, "tree_mask", "int64", q.shape[0] * words, dev)
+        score = score_struct(fn, scale, cap, slopes, self.hq, dev)
         if lse is not None:
-            require_laid_out(fn, lse, "lse", "float32", (q.shape[0], self.hq), self.device)
+            require_laid_out(fn, lse, "lse", "float32", (q.shape[0], self.hq), dev)
         if out is None:
             out = _empty_like(q, stream)
-        dev = self.device
-        check(fn, lib().sift_cache_attention(
+        st = lib().sift_cache_attention(
             self._h, self._kv(fn, kv), rows, _desc(fn, q, "q", dev), _desc(fn, k_new, "k_new", dev),
             _desc(fn, v_new, "v_new", dev), _address(tree_mask), words, score,
-            _desc(fn, out, "out", dev), _address(lse), _stream_ptr(stream)))
+            _desc(fn, out, "out", dev), _address(lse), _stream_ptr(stream))
+        if st:
+            check(fn, st)
         return out
 
     def _slot_buffer(self, fn, t, name, dtype="float32"):
