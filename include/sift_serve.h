@@ -131,7 +131,8 @@ typedef struct sift_cache_kv {
   const int32_t* page_lens;    /* [num_seqs][max_pages], or NULL: full pages     */
   const int32_t* key_pos;      /* [num_seqs][Hkv][max_pages * page], or NULL     */
   /* Read with SIFT_E4M3 pools only (programs built without them pass none): a key is
-   * its pool row times its page's and kv head's scale. */
+   * its pool row times its page's and kv head's scale, any from 2^-100 to 2^120 (taken
+   * as the nearer of these where it is below or above; pages without keys: anything). */
   float* k_scales;             /* [num_pages][Hkv]                               */
   float* v_scales;
 } sift_cache_kv;
@@ -173,7 +174,7 @@ sift_status sift_cache_destroy(sift_cache* cache);
  *   q, out       [rows][Hq][D];  k_new, v_new: [rows][Hkv][D], the new tokens'
  *                own keys, which the cache does not hold yet.  All tensors and
  *                the pools SIFT_BF16 or all SIFT_F32, 16-byte aligned; with pools of
- *                SIFT_E4M3 (under any scales) all others SIFT_BF16.
+ *                SIFT_E4M3 all others SIFT_BF16.
  *   tree_mask    device uint64 [rows][mask_words], mask_words >=
  *                ceil(max_rows / 64): bit j % 64 of word j / 64 says whether the
  *                row sees new token j of its sequence (its ancestors and

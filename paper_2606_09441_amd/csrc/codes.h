@@ -135,8 +135,11 @@ __device__ __forceinline__ f32x16 qk_beside_codes(int tile, int l32, int hf, con
   return s;
 }
 
-// A scale as it is used: no page's keys are below what this leaves of them.
-__device__ __forceinline__ float usable_scale(float s) { return fmaxf(s, 0x1p-100f); }
+// A scale as it is used: from 2^-100 to 2^120, what appends make (whatever the scale of a
+// page without keys is, its logarithm is a number).
+__device__ __forceinline__ float usable_scale(float s) {
+  return fminf(fmaxf(s, 0x1p-100f), 0x1p120f);
+}
 
 // O^T += V^T P^T over 32 keys at LDS address addr (lane_v included).
 template <int D>

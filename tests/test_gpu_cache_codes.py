@@ -222,6 +222,27 @@ def test_scales_far_apart():
         check(x, name="far apart", lse_tol=max(LSE_TOL, 131 * 2.0 ** -24 * most))
 
 
+@pytest.mark.parametrize("value", [math.inf, -math.inf, math.nan, 0.0, 3e38])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (20.0, True)])
+@pytest.mark.parametrize("many", [False, True])
+def test_scales_of_pages_without_keys(many, cap, bias, value):
+    """Pages that hold no key may have any scale: those behind a sequence's last, in the
+    same tile, and those that page_lens leave empty."""
+    x = Codes([9000, 340, 0] if many else [1000, 20, 0, 17], [100, 40, 3] if many else [2, 3, 1, 1],
+              8, 1, 64, 16, gaps=True, seed=31, extra_pages=8)
+    x.page_lens[0, 8:16] = 0                        # two whole tiles of 64 keys
+    x.page_lens[0, 19] = x.page_lens[1, 0] = 0
+    x.t["page_lens"] = torch.from_numpy(x.page_lens).to(x.q.device)
+    empty = np.ones(x.scales["k"].shape[0], bool)
+    empty[x.table[x.page_lens > 0]] = False
+    for b, n in enumerate(x.lens):
+        x.table[b, -(-int(n) // x.page):] = int(np.nonzero(empty)[0][0])
+    x.t["table"] = torch.from_numpy(x.table).to(x.q.device)
+    for name in "kv":
+        x.scales[name][torch.from_numpy(empty).to(x.q.device)] = value
+    check(x, cap=cap, bias=bias, name=f"empty pages {value}")
+
+
 def spread(x, value):
     """The plain form where places of V are not finite: they reach the rows that see them
     with a weight above 0."""
