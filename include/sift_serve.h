@@ -217,7 +217,8 @@ sift_status sift_cache_attention(sift_cache* cache, const sift_cache_kv* kv,
  *                NULL: receives the positions of the slots that are written
  *   lens_out     device int32 [num_seqs], may be the lens (a second, small launch), or
  *                NULL: the lens of the next calls.  Without slots only.
- * Rows past a sequence's last slot are left out.  page_lens are neither read nor
+ * Rows past a sequence's last slot are left out, and rows of pages that are not in the
+ * pools (page_table values out of range).  page_lens are neither read nor
  * changed.  The pages that rows enter must be the sequence's own.
  * SIFT_E4M3: a page's scale becomes the least power of two (2^-100 at least) such that
  *   448 times it holds max |x| of the page's new rows of the head (of dims that turn,

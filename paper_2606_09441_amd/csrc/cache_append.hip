@@ -78,9 +78,9 @@ __global__ __launch_bounds__(256) void append_kernel(CacheAppendArgs p, int part
     const Seq s = work.seq(pl.b);
     const int slot = p.slots != nullptr ? scalar(p.slots, token) : s.len + (token - s.row0);
     if (slot < 0 || slot >= slots) continue;
-    const int page = within(
-        scalar(a.table, static_cast<int64_t>(pl.b) * a.max_pages + (slot >> a.page_shift)),
-        a.num_pages - 1);
+    const int page =
+        scalar(a.table, static_cast<int64_t>(pl.b) * a.max_pages + (slot >> a.page_shift));
+    if (page < 0 || page >= a.num_pages) continue;
     const int64_t row =
         (static_cast<int64_t>(page) << a.page_shift) + (slot & ((1 << a.page_shift) - 1));
     const int pos = a.row_pos != nullptr ? scalar(a.row_pos, token) : slot;
@@ -267,8 +267,8 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     const Seq s = work.seq(pl.b);
     const int u = x - pl.at;
     const int h = u % a.hkv, pi = cost.first(s) + u / a.hkv;
-    const int page =
-        within(scalar(a.table, static_cast<int64_t>(pl.b) * a.max_pages + pi), a.num_pages - 1);
+    const int page = scalar(a.table, static_cast<int64_t>(pl.b) * a.max_pages + pi);
+    if (page < 0 || page >= a.num_pages) continue;
     const int base = pi << a.page_shift;              // the page's first slot
     const int lo = max(s.len - base, 0);              // its new rows
     const int hi = min(cost.end(s) - base, 1 << a.page_shift);

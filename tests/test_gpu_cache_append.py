@@ -296,6 +296,23 @@ def test_bad_tables_stay_inside(pool):
                 assert bool((w[:pad * 16] == 0x5a).all()) and bool((w[-pad * 16:] == 0x5a).all())
 
 
+@pytest.mark.parametrize("pool", ["bf16", "f32", "e4m3"])
+def test_rows_of_no_page_are_left_out(pool):
+    """A table's values out of range lead to nobody's page: neither the first nor the last
+    of the pool, and no position, changes."""
+    c = Case([5, 40, 9, 3], [20, 20, 20, 40], 2, 64, 16, pool, 64)
+    num = c.k_pages.shape[0] // c.page
+    c.table[0, 1], c.table[1], c.table[3, 0] = num, -1, -(1 << 31)
+    c.t["table"] = torch.from_numpy(c.table).to(device())
+    some = c.places
+    c.places = lambda slots=None: (p for p in some(slots) if 0 <= p[3] < num * c.page)
+    before = c.snapshot()
+    with c.cache() as cache:
+        out = cache.append(c.kv(), c.k, c.v, row_ptr=c.t["row_ptr"], row_pos=c.t["row_pos"],
+                           pos_out=c.key_pos, rotary=c.rotary())
+        c.verify(before, out, tag=pool)
+
+
 def test_scales_of_unlike_and_odd_values():
     """Rows of sizes far apart, a page of zeros, of the smallest numbers, infinities and
     NaN: held as NaN, without a part in the scale."""
