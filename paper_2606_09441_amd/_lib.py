@@ -807,7 +807,14 @@ class Rotary:
         return self.rotate(q, k, positions, back, q, k, stream)
 
     def __call__(self, q, k, positions):
-        """rotate with gradients for q and k (any order), on the current stream."""
+        """rotate with gradients for q and k (any order), on the current stream.  Not where
+        that is being captured: a backward pass there may meet leaves of other graphs, on
+        streams that are not.  rotate, and rotate(back=True) for the gradients, may be."""
+        torch = _torch()
+        if (torch.is_grad_enabled() and any(getattr(x, "requires_grad", False) for x in (q, k))
+                and torch.cuda.is_current_stream_capturing()):
+            raise SiftError("Rotary", 4, "gradients in a captured graph: take rotate, and "
+                                         "rotate(back=True) for them")
         return _turn_function().apply(q, k, positions, self, False)
 
 

@@ -216,6 +216,28 @@ def test_streams_and_graphs():
         assert torch.equal(bwd, r.rotate(g, None, pos, back=True)[0])
 
 
+def test_no_gradients_in_a_captured_graph():
+    """Refused before anything is recorded; without gradients such a call is as any."""
+    from paper_2606_09441_amd import Rotary, SiftError
+    q, k, pos, f = inputs(50, 4, 2, 64, 64, "bf16", 300)
+    r = Rotary(f)
+    want = r.rotate(q, k, pos)
+    leaf = k.clone().requires_grad_()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(SiftError, match="captured"):
+            r(q, leaf, pos)
+        got = r(q, k, pos)
+        with torch.no_grad():
+            again = r(q, leaf, pos)
+    for _ in range(3):
+        for x in got + again:
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got + again, want + want))
+
+
 def test_moved_keys():
     """Keys turned back from their document's positions and on to the prompt's are, to
     two roundings and both cosines' errors, those turned at once."""
