@@ -936,7 +936,8 @@ class CachePages:
                       v_scales)
         self.sizes = (dev, *(None if t is None else (t.numel(), t.shape)
                              for t in (page_table, lens, page_lens, key_pos)))
-        self.fits = None   # the sizes of the Cache that took these last
+        self.shapes = self.sizes + (k_pages.shape[0], *(None if t is None else t.shape
+                                                        for t in (k_scales, v_scales)))
         ptr = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
         self.struct = SiftCacheKv(ctypes.pointer(kd), ctypes.pointer(vd), page_table.data_ptr(),
                                   lens.data_ptr(), ptr(page_lens), ptr(key_pos), ptr(k_scales),
@@ -970,7 +971,8 @@ class Cache:
         self._slot_sizes = (num_seqs, num_kv_heads, self.slots)
         sizes = (("page_table", (num_seqs, max_pages)), ("lens", (num_seqs,)),
                  ("page_lens", (num_seqs, max_pages)), ("key_pos", self._slot_sizes))
-        self._tables = tuple((name, math.prod(x), x) for name, x in sizes)  # (of this handle alone)
+        self._tables = tuple((name, math.prod(x), x) for name, x in sizes)
+        self._fit = None   # shapes that are these tables'
 
     def close(self):
         if self._h is not None:
@@ -991,7 +993,7 @@ class Cache:
 
     def _kv(self, fn, kv):
         """The tables' sizes, which the library cannot see."""
-        if kv.fits is self._tables:   # as of the last call
+        if kv.shapes == self._fit:
             return kv.struct
         device, *have = kv.sizes
         if device != self.device:
@@ -1006,7 +1008,7 @@ class Cache:
             sizes = (kv.k_pages.shape[0] // self.page, self.hkv)
             for name, t in (("k_scales", kv.k_scales), ("v_scales", kv.v_scales)):
                 require_laid_out(fn, t, name, "float32", sizes, self.device)
-        kv.fits = self._tables
+        self._fit = kv.shapes
         return kv.struct
 
     def _rows(self, fn, q, row_ptr, row_pos):
