@@ -1,10 +1,14 @@
 // The attention of many new tokens over a paged cache held in e4m3: units of 128 rows of
 // a (sequence, kv head), as in cache_wide.hip, over the pipeline of codes_pipe.h.  The new
-// tokens' own keys, bf16 tiles, are taken last and one at a time.  64 tokens, 48/8 heads, D
-// = 128 over 66048 slots: 150 us of the call with its merge (bf16 152), 700 TFLOP/s, the VALU busy in 59% of the SIMDs' cycles, the
-// MFMAs in 30%: some 430 vector operations a wavefront and tile, 128 of them conversions,
-// beside 32 matrix instructions.  Kernels of their own for tiles in one page keep a scale
-// where four would be, and spill less (25 registers a lane, not 34): 150 us, not 162.
+// tokens' own keys, bf16 tiles, are taken last and one at a time.
+//
+// 64 tokens, 48/8 heads, D = 128 over 66048 slots: 150 us of the call with its merge (bf16
+// 152), 690 TFLOP/s.  The vector unit is active in 58% of the SIMDs' cycles (12 operations
+// a matrix instruction, four of them conversions), the matrix cores in 35%, one or the
+// other in 72%.  Twice the slots cost 116 us more: 34 are a workgroup's start and end and
+// the merge of what they share, 33 MB of sums written and read again.  Kernels of their own
+// for tiles in one page keep a scale where four would be, and spill less (25 registers a
+// lane, not 35): 150 us, not 162.
 
 #include "cache.h"
 #include "codes_pipe.h"
