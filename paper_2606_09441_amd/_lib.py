@@ -505,6 +505,13 @@ def _desc(fn, t, name, device) -> SiftTensor:
     return SiftTensor(t.data_ptr(), kind, shape[0], shape[1], shape[2])
 
 
+def _desc_like(d: SiftTensor, t) -> SiftTensor:
+    """That of t, an empty_like of d's tensor."""
+    x = SiftTensor.from_buffer_copy(d)
+    x.data = t.data_ptr()
+    return x
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -772,12 +779,16 @@ class Rotary:
         require(fn, positions, "positions", "int32", qd.tokens, dev)
         if q_out is None:
             q_out = _empty_like(q, stream)
-        qo = _desc(fn, q_out, "q_out", dev)
+            qo = _desc_like(qd, q_out)
+        else:
+            qo = _desc(fn, q_out, "q_out", dev)
         if k is not None:
             kd = _desc(fn, k, "k", dev)
             if k_out is None:
                 k_out = _empty_like(k, stream)
-            ko = _desc(fn, k_out, "k_out", dev)
+                ko = _desc_like(kd, k_out)
+            else:
+                ko = _desc(fn, k_out, "k_out", dev)
         elif k_out is not None:
             raise SiftError(fn, 1, "k_out without k")
         st = lib().sift_rotate(qd, kd, positions.data_ptr(), self.struct, back, qo, ko,
@@ -790,13 +801,12 @@ class Rotary:
         """rotate of gradients, which are as the outputs that rotate checked."""
         torch = _torch()
         kind = _kinds[dq.dtype]
-        qo, kd, ko = torch.empty_like(dq), None, None
+        qd, qo, kd, ko = SiftTensor(dq.data_ptr(), kind, *dq.shape), torch.empty_like(dq), None, None
         if dk is not None:
             out = torch.empty_like(dk)
             kd = SiftTensor(dk.data_ptr(), kind, *dk.shape)
-            ko = SiftTensor(out.data_ptr(), kind, *dk.shape)
-        st = lib().sift_rotate(SiftTensor(dq.data_ptr(), kind, *dq.shape), kd, positions.data_ptr(),
-                               self.struct, back, SiftTensor(qo.data_ptr(), kind, *dq.shape), ko,
+            ko = _desc_like(kd, out)
+        st = lib().sift_rotate(qd, kd, positions.data_ptr(), self.struct, back, _desc_like(qd, qo), ko,
                                _stream_ptr(None))
         if st:
             check("sift_rotate", st)
@@ -1038,12 +1048,16 @@ class Cache:
         score = score_struct(fn, scale, cap, slopes, self.hq, dev)
         if lse is not None:
             require_laid_out(fn, lse, "lse", "float32", (q.shape[0], self.hq), dev)
+        qd = _desc(fn, q, "q", dev)
         if out is None:
             out = _empty_like(q, stream)
+            od = _desc_like(qd, out)
+        else:
+            od = _desc(fn, out, "out", dev)
         st = lib().sift_cache_attention(
-            self._h, self._kv(fn, kv), rows, _desc(fn, q, "q", dev), _desc(fn, k_new, "k_new", dev),
-            _desc(fn, v_new, "v_new", dev), _address(tree_mask), words, score,
-            _desc(fn, out, "out", dev), _address(lse), _stream_ptr(stream))
+            self._h, self._kv(fn, kv), rows, qd, _desc(fn, k_new, "k_new", dev),
+            _desc(fn, v_new, "v_new", dev), _address(tree_mask), words, score, od, _address(lse),
+            _stream_ptr(stream))
         if st:
             check(fn, st)
         return out
