@@ -169,7 +169,8 @@ sift_status sift_cache_create(int32_t num_seqs, int32_t num_q_heads, int32_t num
     return fail();
   // (where bf16 does not go by the wide units, e4m3 does not either)
   const bool wide = sift::cache_attn_wide(
-      sift::Pool::kBf16, max_rows * g, static_cast<int64_t>(num_seqs) * num_kv_heads * max_pages * page);
+      sift::Pool::kBf16, max_rows * g,
+      static_cast<int64_t>(num_seqs) * num_kv_heads * max_pages * page);
   const size_t rows = static_cast<size_t>(2 * 2 * c->cus) *
                       (wide ? sift::kCacheWideRows : sift::kCacheRows);
   const size_t o_bytes = rows * head_dim * sizeof(float);

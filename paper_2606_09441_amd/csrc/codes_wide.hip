@@ -9,9 +9,8 @@
 // and the merge of what they share, 33 MB of sums written and read again.  In the others
 // the vector unit is what counts: with the exponentials' longer issue (four times the
 // others') its operations fill nine tenths of the cycles, and one workgroup on a CU does as
-// many tiles as two.  Kernels of their own
-// for tiles in one page keep a scale where four would be, and spill less (25 registers a
-// lane, not 35): 150 us, not 162.
+// many tiles as two.  Kernels of their own for tiles in one page keep a scale where four
+// would be, and spill less (25 registers a lane, not 35): 150 us, not 162.
 
 #include "cache.h"
 #include "codes_pipe.h"

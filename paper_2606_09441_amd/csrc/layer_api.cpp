@@ -1,7 +1,7 @@
 // C ABI of the pieces the decoder-layer prefill slice adds around the sparse
 // attention: the rotary position embedding (rope.hip; rotary.hip for any table,
-// layout and part of the head), the norms and the SwiGLU product (layer_ops.hip).  The projections are library GEMMs called
-// by the caller.
+// layout and part of the head), the norms and the SwiGLU product (layer_ops.hip).
+// The projections are library GEMMs called by the caller.
 
 #include <hip/hip_runtime.h>
 

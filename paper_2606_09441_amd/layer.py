@@ -3,8 +3,9 @@
 One pre-norm layer of the Llama-3.1-8B architecture (the model of Section 6):
 RMSNorm, the q/k/v projections, rotary embedding (libsift's `sift_rope`, or
 `sift_rotate` where a Rotary is given), the sparse attention (libsift's
-plan: decode + attention over the bits), the output projection and residual, then optionally the SwiGLU MLP.  The
-projections are library GEMMs (torch.matmul -> hipBLASLt on bf16); the norms
+plan: decode + attention over the bits), the output projection and residual,
+then optionally the SwiGLU MLP.  The projections are library GEMMs
+(torch.matmul -> hipBLASLt on bf16); the norms
 and the MLP activation are one kernel each, or torch elementwise ops for
 tensors that those do not take (other types or widths, recorded gradients).  It serves to measure the
 per-layer prefill time of sparse against dense attention, the quantity the
