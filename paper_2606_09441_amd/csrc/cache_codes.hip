@@ -2,10 +2,9 @@
 // and kv head: the units, their split over the workgroups and the merge are those of
 // cache_attn.hip.  HBM bounds it, at half the bytes of bf16.
 //
-// K's scale is a factor of the scores, V's one of the weights, there part of the exponent
-// (2^(s - base) scale = 2^(s - (base - log2 scale))), so that neither costs an operation a
-// key.  Codes become bf16 in registers, exactly, on the way from LDS to the matrix
-// instructions; the new tokens' own keys are bf16 tiles, taken last.
+// K's scale is a factor of the scores, V's one of the conversion and of the weights, there
+// part of the exponent (ValueScale), so that neither costs an operation a key.  Codes become
+// bf16 in registers, exactly, on the way from LDS to the matrix instructions; the new tokens' own keys are bf16 tiles, taken last.
 // 8 sequences of 131072 slots, 32/8 heads, D = 128: 392 us, 5.5 TB/s of HBM; 32 of 200 to
 // 16640 slots 60 us, 4.3 TB/s: ten of them until the first tiles are there and after the
 // last, and workgroups that the memory serves unevenly (they end between 42 and 60 us).
@@ -214,23 +213,27 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
         if (two) fetch(after, slot, kK);
         const CodeRows<kPages> third = rows_of(min(t + 3 * kStepTiles, cend - 1));
         const Scales<kPages> then = scales_of(next);
-        float f[2], base[2], undo[2];
+        float f[2], base[2], undo[2], power[2];
 #pragma unroll
         for (int i = 0; i < kPages; ++i) {
-          const float ks = usable_scale(mine.k[i]), vs = usable_scale(mine.v[i]);
+          const float ks = usable_scale(mine.k[i]);
           f[i] = ks * c;
           if constexpr (kCap || kBias) {
 #pragma unroll
             for (int v = i * kEach / 2; v < (i + 1) * kEach / 2; ++v) sc[v] *= ks;
             f[i] = c;
           }
-          base[i] = -__builtin_amdgcn_logf(vs);
-          undo[i] = __builtin_amdgcn_rcpf(vs);
+          ValueScale vs;
+          vs.set(mine.v[i]);
+          base[i] = vs.lift;
+          undo[i] = vs.undo;
+          power[i] = vs.power;
         }
         if constexpr (kPages == 1) {
           f[1] = f[0];
           base[1] = base[0];
           undo[1] = undo[0];
+          power[1] = power[0];
         }
         const float off = shape(sc, bits, false, t * kTileKeys, f);
 #pragma unroll
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(256, 2) void cache_codes_kernel(CacheAttnArgs p) {
           wait_vm<2 * kDmas>();
         else
           wait_vm<0>();
-        pv_codes<D>(vt + slot * kCodes + vlane, sc, st.o);
+        pv_codes<D>(vt + slot * kCodes + vlane, sc, power, st.o);
         wait_lds();  // V is read
         if (two) fetch(after, slot, kV);
         now = next;

@@ -1,6 +1,6 @@
-// Tiles of e4m3 codes in LDS, and how lanes read them as bf16 operands: every code is
-// a bf16 number, so nothing is lost but the page's scale, which goes to the scores (K)
-// and to the weights (V).  (The 8-bit matrix instructions, which would take K's codes as
+// Tiles of e4m3 codes in LDS, and how lanes read them as bf16 operands: every code, times
+// any power of two of a scale's, is a bf16 number, so nothing is lost.  K's scale goes to
+// the scores, V's power of two into the conversion, and what is left of V's to the weights.  (The 8-bit matrix instructions, which would take K's codes as
 // they are beside queries split in two, add with too few bits: off by 2^-13 of the sum of
 // the products' sizes, as measured over 64 of them, where fp32 allows 2^-24 each.)
 #pragma once
@@ -14,14 +14,14 @@ typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
 
-// Eight codes as bf16.
-__device__ __forceinline__ bf16x8 code_values(u32x2 v) {
+// Eight codes as bf16, times a power of two.
+__device__ __forceinline__ bf16x8 code_values(u32x2 v, float power = 1.f) {
   bf16x8 x;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const uint32_t w = v[i];
-    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false);
-    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true);
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, power, true);
     x[4 * i] = a[0];
     x[4 * i + 1] = a[1];
     x[4 * i + 2] = b[0];
@@ -141,9 +141,30 @@ __device__ __forceinline__ float usable_scale(float s) {
   return fminf(fmaxf(s, 0x1p-100f), 0x1p120f);
 }
 
-// O^T += V^T P^T over 32 keys at LDS address addr (lane_v included).
+// V's scale of a page.  Its power of two goes to the codes, as far as 2^100, where they are
+// finite bf16 numbers yet; the rest, from 1 to 2 and with scales above that to 2^20, is a
+// factor of the weights, there part of the exponent: 2^(s - (base + lift)).  So the weights
+// are of the sizes that they have without a scale: with all of it in the exponent those
+// beside a scale of 2^-100 vanished from 2^-26 on, from the sums too, and beside 2^120 they
+// came to infinity.
+struct ValueScale {
+  float power, lift, undo;  // undo: one over the rest
+  __device__ __forceinline__ void set(float scale) {
+    const uint32_t s = __builtin_bit_cast(uint32_t, usable_scale(scale));
+    const uint32_t e = min(s & 0xff800000u, (100u + 127u) << 23);
+    power = __builtin_bit_cast(float, e);
+    const float rest =  // (times one over the power)
+        __builtin_bit_cast(float, s) * __builtin_bit_cast(float, (254u << 23) - e);
+    lift = -__builtin_amdgcn_logf(rest);
+    undo = __builtin_amdgcn_rcpf(rest);
+  }
+};
+
+// O^T += V^T P^T over 32 keys at LDS address addr (lane_v included); power: of V's scales,
+// of each 16 keys.
 template <int D>
-__device__ __forceinline__ void pv_codes(int addr, const f32x16& p, f32x16 (&o)[D / 32]) {
+__device__ __forceinline__ void pv_codes(int addr, const f32x16& p, const float (&power)[2],
+                                         f32x16 (&o)[D / 32]) {
 #pragma unroll
   for (int st = 0; st < 2; ++st) {
     bf16x8 b;
@@ -151,14 +172,14 @@ __device__ __forceinline__ void pv_codes(int addr, const f32x16& p, f32x16 (&o)[
     for (int i = 0; i < 8; ++i) b[i] = static_cast<__bf16>(p[8 * st + i]);
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
-      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code_values(CodeTile<D>::v_codes(addr, db, st)), b,
-                                                      o[db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          code_values(CodeTile<D>::v_codes(addr, db, st), power[st]), b, o[db], 0, 0, 0);
   }
 }
 
-// Weights of 32 keys of two groups of 16, times their V scales: 2^(c_i s - base_i), where
-// base_i holds the scale's logarithm; undo_i: one over the scale.  l and le as
-// weigh_block's: sums of the weights alone.
+// Weights of 32 keys of two groups of 16, times what is left of their V scales:
+// 2^(c_i s - base_i), where base_i holds the lift.  l and le as weigh_block's: sums of the
+// weights alone.
 __device__ __forceinline__ void weigh_codes(f32x16& s, const float (&c)[2], const float (&base)[2],
                                             const float (&undo)[2], float& l, float& le) {
   const bf16x2 ones = bf16x2{static_cast<__bf16>(1.f), static_cast<__bf16>(1.f)};

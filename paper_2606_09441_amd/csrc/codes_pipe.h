@@ -6,9 +6,9 @@
 // read the same tiles from, and room for three tiles of K and of V: the DMA of a tile has
 // two steps to arrive in.
 //
-// A tile's four groups of 16 keys have scales of their own.  V's are part of the exponents
-// (codes.h), K's a factor of them; where scores are capped or biased K's are multiplied
-// into the scores beside PV.
+// A tile's four groups of 16 keys have scales of their own.  V's are part of the conversions
+// and of the exponents (ValueScale), K's a factor of the exponents; where scores are capped
+// or biased K's are multiplied into the scores beside PV.
 #pragma once
 
 #include "codes.h"
@@ -31,17 +31,13 @@ template <int kPages>
 struct CodeScales {
   float k[kPages], v[kPages];
 };
-// A tile's V scales as the weights take them: 2^-lift, and one over the scale.
+// A tile's V scales.
 template <int kPages>
-struct Lift {
-  float lift[kPages], undo[kPages];
+struct ValueScales {
+  ValueScale g[kPages];
   __device__ __forceinline__ void set(const CodeScales<kPages>& z) {
 #pragma unroll
-    for (int g = 0; g < kPages; ++g) {
-      const float s = usable_scale(z.v[g]);
-      lift[g] = -__builtin_amdgcn_logf(s);
-      undo[g] = __builtin_amdgcn_rcpf(s);
-    }
+    for (int i = 0; i < kPages; ++i) g[i].set(z.v[i]);
   }
 };
 
@@ -74,7 +70,7 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 
   Form f;
   float fk[kPages];  // kPlain: K's scales and the scores'
-  Lift<kPages> w;
+  ValueScales<kPages> w;
   // The bound of a tile's scores from its pages' largest products.
   const auto largest = [&](const float (&m)[kPages]) {
     float x = m[0] * fk[0];
@@ -107,7 +103,8 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 
   // n0, n1 = K Q^T from K slot `slot`, beside the weights of the tile c0, c1 and issue(s)
   const auto qk_and_weigh = [&](int slot, f32x16& n0, f32x16& n1, const f32x16& c0,
-                                const f32x16& c1, const Form& f, const Lift<kPages>& w, auto issue) {
+                                const f32x16& c1, const Form& f,
+                                const ValueScales<kPages>& w, auto issue) {
     const float base = st.base();
     float sum = 0.f, le = 0.f;
     u32x4 x[2][2];
@@ -128,10 +125,10 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 #pragma unroll
       for (int u = 0; u < kEach; u += 2) {
         const int e = s * kEach + u, i = (e >> 3) / kSame;
-        weigh(e, c0, c1, f, kPlain ? fk[i] : f.p0, base + w.lift[i], sum, le);
+        weigh(e, c0, c1, f, kPlain ? fk[i] : f.p0, base + w.g[i].lift, sum, le);
         if (e % (8 * kSame) == 8 * kSame - 2) {  // the page's last
-          st.l = fmaf(sum, w.undo[i], st.l);
-          st.le = fmaf(le, w.undo[i], st.le);
+          st.l = fmaf(sum, w.g[i].undo, st.l);
+          st.le = fmaf(le, w.g[i].undo, st.le);
           sum = le = 0.f;
         }
       }
@@ -152,8 +149,9 @@ __device__ __forceinline__ void run_code_pipe(Src& src, const CodeQ<D>& q, RowSt
 #pragma unroll
     for (int i = 0; i < kPv; ++i) {
       const int db = i % (D / 32);
-      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code_values(x[i % kAhead]),
-                                                        pb[i / (D / 32)], st.o[db], 0, 0, 0);
+      st.o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          code_values(x[i % kAhead], w.g[i / (D / 32) / kSame].power), pb[i / (D / 32)], st.o[db],
+          0, 0, 0);
       with(i);
       const int j = i + kAhead;
       if (j < kPv) x[j % kAhead] = C::v_codes(vaddr + slot, j % (D / 32), j / (D / 32));
