@@ -132,7 +132,8 @@ typedef struct sift_cache_kv {
   const int32_t* key_pos;      /* [num_seqs][Hkv][max_pages * page], or NULL     */
   /* Read with SIFT_E4M3 pools only (programs built without them pass none): a key is
    * its pool row times its page's and kv head's scale, any from 2^-100 to 2^120 (taken
-   * as the nearer of these where it is below or above; pages without keys: anything). */
+   * as the nearer of these where it is below or above, by appends too, and NaN as 2^-100;
+   * pages without keys: anything). */
   float* k_scales;             /* [num_pages][Hkv]                               */
   float* v_scales;
 } sift_cache_kv;

@@ -294,7 +294,9 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     }
     const int64_t sc = static_cast<int64_t>(page) * a.hkv + h;
     const bool begun = lo > 0;
-    const float old_k = begun ? p.k_scales[sc] : 0.f, old_v = begun ? p.v_scales[sc] : 0.f;
+    // (as the attention takes them: what the page holds stays what it was read as)
+    const float old_k = begun ? usable_scale(p.k_scales[sc]) : 0.f;
+    const float old_v = begun ? usable_scale(p.v_scales[sc]) : 0.f;
 
     // this lane's frequencies, for all its rows
     double freq[8] = {};

@@ -23,4 +23,10 @@ constexpr int32_t keys_of_page(int32_t page_len, int32_t in, int32_t left) {
   return within(held < left ? held : left, 16);
 }
 
+// A scale of e4m3 codes as every call takes it: from 2^-100 to 2^120, what appends make
+// (whatever the scale of a page without keys is, its logarithm is a number; of NaN, 2^-100).
+constexpr float usable_scale(float s) {
+  return __builtin_fminf(__builtin_fmaxf(s, 0x1p-100f), 0x1p120f);
+}
+
 }  // namespace sift

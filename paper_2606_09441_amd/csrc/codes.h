@@ -5,6 +5,7 @@
 // the products' sizes, as measured over 64 of them, where fp32 allows 2^-24 each.)
 #pragma once
 
+#include "clamp.h"
 #include "flash.h"
 
 namespace sift {
@@ -133,12 +134,6 @@ __device__ __forceinline__ f32x16 qk_beside_codes(int tile, int l32, int hf, con
                              addr ^ (16 * (4 * (i >> 1) + (i & 1))))),
                          q.x[i], s);
   return s;
-}
-
-// A scale as it is used: from 2^-100 to 2^120, what appends make (whatever the scale of a
-// page without keys is, its logarithm is a number).
-__device__ __forceinline__ float usable_scale(float s) {
-  return fminf(fmaxf(s, 0x1p-100f), 0x1p120f);
 }
 
 // V's scale of a page.  Its power of two goes to the codes, as far as 2^100, where they are

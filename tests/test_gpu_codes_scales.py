@@ -1,8 +1,8 @@
 """GPU: attention over e4m3 pages whose scales lie at the ends of their range, 2^-100 and
 2^120 (sift_cache_attention with SIFT_E4M3 pools): what a page's scale is changes neither
-the weights of its keys nor their sums.
+the weights of its keys nor their sums; and appends to pages whose scales lie beyond.
 
-All sequences have the same pages, so that there are as many units as workgroups and one
+In the former all sequences have the same pages, so that there are as many units as workgroups and one
 goes over a sequence from its first key to its last, with the reference that its first
 tiles left.  Every new token sees the cache and itself."""
 
@@ -141,3 +141,40 @@ def test_values_at_the_ends_of_the_range(units, n, scale, score, page):
         f"{max_abs(lse, ref_lse):.2e}")
     assert max_abs(lse, ref_lse) <= LSE_TOL
     assert e <= 1
+
+
+@pytest.mark.parametrize("page,d", [(16, 64), (64, 128)])
+@pytest.mark.parametrize("scale,taken", [
+    (0.0, 2.0 ** -100), (-1.0, 2.0 ** -100), (2.0 ** -110, 2.0 ** -100), (np.nan, 2.0 ** -100),
+    (1e-40, 2.0 ** -100), (2.0 ** 121, 2.0 ** 120), (1.5 * 2.0 ** 127, 2.0 ** 120),
+    (np.inf, 2.0 ** 120), (2.0 ** -100, 2.0 ** -100), (2.0 ** 120, 2.0 ** 120)])
+def test_appends_take_a_scale_as_the_attention_does(scale, taken, page, d):
+    """A page begun under a scale out of range: new rows of zeros leave the keys that it
+    holds what they were, to the bit, and its scale becomes the one in range."""
+    from paper_2606_09441_amd import Cache, CachePages
+    dev, hkv, held, new = device(), 2, 9, 5
+    rng = np.random.default_rng(1)
+    x = rng.choice([-1.0, 1.0], (2, page, hkv, d)) * np.exp2(rng.integers(-9, -5, (2, page, hkv, d)))
+    was = torch.from_numpy(x.astype(np.float32)).to(dev)
+    k, v = (t.to(E4M3) for t in was)
+    scales = [torch.full((1, hkv), scale, device=dev) for _ in range(2)]
+    lens = torch.tensor([held], dtype=torch.int32, device=dev)
+    kv = CachePages(k, v, torch.zeros(1, 1, dtype=torch.int32, device=dev), lens,
+                    k_scales=scales[0], v_scales=scales[1])
+    none = torch.zeros(1, hkv, d, dtype=torch.bfloat16, device=dev)
+    zeros = torch.zeros(new, hkv, d, dtype=torch.bfloat16, device=dev)
+    with Cache(1, hkv, hkv, d, page=page, max_pages=1, max_rows=1) as cache:
+        before = cache.attention(none, none, none, kv)   # the values' mean
+        grown = cache.append(kv, zeros, zeros)
+        after = cache.attention(none, none, none, kv)
+        torch.cuda.synchronize()
+    assert grown.tolist() == [held + new]
+    mean = was[1, :held].double().sum(0) * taken / (held + 1)
+    # weights in bf16 over their own sum are the same; fp32 sums and the output in bf16
+    size = was[1, :held].double().abs().sum(0) * taken / (held + 1)
+    assert ((before[0].double() - mean).abs() <= mean.abs() * 2.0 ** -8 + size * 2.0 ** -20).all()
+    assert torch.equal(before, after)
+    for t, codes, now in zip(was, (k, v), scales):
+        assert now.tolist() == [[taken] * hkv]
+        assert torch.equal(codes[:held].float(), t[:held])
+        assert not codes[held:held + new].float().any()
