@@ -717,9 +717,10 @@ def rotary_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, context=
                 than context / high (4) kept, and between them a mean of both, linear in
                 context / wavelength
       "parts"   by index: kept up to the floor of where a wavelength makes `high` (32)
-                turns in the context, divided from the ceiling of where it makes `low` (1)
-                on, a mean linear in the index between; the magnitude is
-                1 + 0.1 ln(factor)
+                turns in the context (0 at least), divided from the ceiling of where it
+                makes `low` (1) on (rot_dim - 1 at most: that may lie past the last
+                pair, rot_dim / 2 - 1), a mean linear in the index between; the magnitude
+                is 1 + 0.1 ln(factor)
 
     context: the length trained on."""
     fn = "rotary_frequencies"
@@ -742,8 +743,7 @@ def rotary_frequencies(rot_dim, base=10000.0, scaling=None, factor=1.0, context=
             keep = np.clip((context * freq / (2 * np.pi) - low) / (high - low), 0.0, 1.0)
         else:
             at = lambda turns: rot_dim / 2 * math.log(context / (2 * np.pi * turns)) / math.log(base)  # noqa: E731
-            first = min(max(math.floor(at(high)), 0), rot_dim // 2 - 1)
-            last = min(max(math.ceil(at(low)), 0), rot_dim // 2 - 1)
+            first, last = max(math.floor(at(high)), 0), min(math.ceil(at(low)), rot_dim - 1)
             keep = 1.0 - np.clip((i - first) / max(last - first, 1e-3), 0.0, 1.0)
             magnitude = 1.0 + 0.1 * math.log(factor)
         freq = freq * keep + freq / factor * (1.0 - keep)

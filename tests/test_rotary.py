@@ -51,6 +51,30 @@ def test_tables_scaled_by_parts():
         assert math.isclose(g[i], f[i] / 16 * t + f[i] * (1 - t), rel_tol=2.0 ** -21)
 
 
+@pytest.mark.parametrize("rot,base,context,factor,first,last", [
+    (64, 10000.0, 65536, 4.0, 20, 33),     # 32 ln(65536 / 64 pi) / ln 10^4 = 20.11; 32.15
+    (128, 10000.0, 131072, 4.0, 45, 70),   # 45.03; 69.11
+    (128, 10000.0, 262144, 8.0, 49, 74),   # 49.84; 73.93
+    (64, 10000.0, 4096, 16.0, 10, 23),     # 10.47; 22.51
+    (8, 2.0, 100000, 2.0, 35, 7),          # 35.83, all kept; 55.83
+    (8, 10.0, 64, 2.0, 0, 5),              # -1.99, from 0 on; 4.03
+    (8, 10.0, 5, 2.0, 0, 0),               # -6.42; -0.40: all but the first divided
+])
+def test_parts_whose_ends_lie_past_the_pairs(rot, base, context, factor, first, last):
+    """Between the ends the mean is linear in the index, wherever they lie."""
+    f = base ** (-2.0 * np.arange(rot // 2) / rot)
+    g, _ = rotary_frequencies(rot, base, "parts", factor, context=context)
+    for i in range(rot // 2):
+        if i <= first:
+            t = 0.0
+        elif i >= last:
+            t = 1.0
+        else:
+            t = (i - first) / (last - first)
+        # half a step of float32, and the 64-bit ramp's own error
+        assert math.isclose(g[i], f[i] / factor * t + f[i] * (1 - t), rel_tol=2.0 ** -23), i
+
+
 @pytest.mark.parametrize("args,kw", [
     ((7,), {}), ((0,), {}), ((8, 1.0), {}), ((8,), {"scaling": "linear", "factor": 0.5}),
     ((8,), {"scaling": "smooth", "factor": 2.0}), ((2,), {"scaling": "base", "factor": 2.0}),
