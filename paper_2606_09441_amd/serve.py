@@ -124,6 +124,10 @@ class PromptCache:
             raise SiftError("PromptCache.prefill", 6, "the prompts are prefilled already")
         if la is not None and (cap or slopes is not None):
             raise SiftError("PromptCache.prefill", 4, "the sparse prefill takes no cap and no bias")
+        tokens = self._slots.shape[0]
+        for name, x, heads in (("q", q, self.cache.hq), ("k", k, self.cache.hkv),
+                               ("v", v, self.cache.hkv)):
+            self._check("PromptCache.prefill", name, x, (tokens, heads, self.cache.d))
         self._score = dict(scale=scale, cap=cap, slopes=slopes)
         pages, turn = self.pages, self.rotary
         k, v = _dense(k), _dense(v)
@@ -151,6 +155,14 @@ class PromptCache:
                for a, z in zip(self._query_rows, self._query_rows[1:])]
         self._pending = (kq, vq, torch.cat(own))
         return out
+
+    def _check(self, fn, name, x, shape):
+        """Before anything is written: what is indexed by a prompt's rows has to hold them."""
+        if x.shape != shape or x.dtype != self._dtype:
+            raise SiftError(fn, 2, f"{name} holds {tuple(x.shape)} {x.dtype}, has to be {shape} "
+                                   f"{self._dtype}")
+        if x.device != self.cache.device:
+            raise SiftError(fn, 7, f"{name} is on {x.device}, the cache on {self.cache.device}")
 
     def cut(self, budget, sinks=4, recent=0):
         """Every kv head keeps `budget` keys: the first `sinks`, the last `recent` and
