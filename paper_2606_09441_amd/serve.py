@@ -236,6 +236,10 @@ class PromptCache:
         ptr = self._pointers(q.shape[0], row_ptr)
         pos = self._positions(q.shape[0], row_ptr, row_pos)
         # whatever may be refused comes before the weights and the pages change
+        for name, x in (("k_new", k_new), ("v_new", v_new), ("row_pos", pos),
+                        ("lse", q if self._codes else lse)):
+            if x.shape[0] < q.shape[0]:
+                raise SiftError("PromptCache.append", 2, f"{name} holds {x.shape[0]} rows, q {q.shape[0]}")
         seq, used = self._room("PromptCache.append", k_new, v_new, rows, ptr, self.max_rows)
         if self._codes:   # not cut again: no weights
             added = self._store(k_new[rows], v_new[rows], seq, used, pos[rows], turn=self.rotary)

@@ -75,3 +75,28 @@ def test_prefill_goes_on_with_the_right_ones():
     p, names = prompts()
     p.prefill(**tensors())
     assert names == ["append", "dense", "accumulate"]
+
+
+@pytest.mark.parametrize("codes", [False, True])
+@pytest.mark.parametrize("short", ["k_new", "v_new", "lse", "row_pos"])
+def test_append_takes_as_many_rows_as_the_step(short, codes):
+    """rows are indexes into all of them."""
+    p, names = prompts()
+    p.weights, p._codes, p.used, p.max_rows = torch.zeros(2, HKV, 64), codes, 0, 8
+    p.next_pos = torch.zeros(2, dtype=torch.int32)
+    p.pages.k_pages, p.pages.lens = torch.zeros(128, HKV, D), p.next_pos
+    p._score = dict(scale=None, cap=0.0, slopes=None)
+    t = {"k_new": torch.zeros(8, HKV, D), "v_new": torch.zeros(8, HKV, D),
+         "row_pos": torch.arange(8, dtype=torch.int32)}
+    t = {n: x.to(torch.bfloat16) if x.dim() == 3 else x for n, x in t.items()}
+    t |= {"q": torch.zeros(8, HQ, D, dtype=torch.bfloat16), "lse": torch.zeros(8, HQ)}
+    p.append(**t, rows=torch.tensor([0, 5, 7]))
+    assert names == (["append"] if codes else ["accumulate", "append"])
+    names.clear()
+    t[short] = t[short][:7]
+    if codes and short == "lse":     # not read
+        p.append(**t, rows=torch.tensor([0, 5, 7]))
+        return
+    with pytest.raises(SiftError) as e:
+        p.append(**t, rows=torch.tensor([0, 5, 7]))
+    assert e.value.status == 2 and names == []
