@@ -772,9 +772,11 @@ class Rotary:
     def rotate(self, q, k, positions, back=False, q_out=None, k_out=None, stream=None):
         """(q_out, k_out): q [tokens, Hq, D] and k [tokens, Hkv, D] (or None) turned by
         positions (int32 [tokens]); back: by the negative angles, the gradient of the
-        call.  The outputs are new, or given, and may be the inputs."""
+        call.  The outputs are new, or given, and may be the inputs.  No gradient is
+        recorded (calling the Rotary records one): outputs given must not require one."""
         fn, dev = "sift_rotate", self.device
         _current(fn, dev)
+        given = [x for x in (q_out, k_out) if x is not None]
         qd, kd, ko = _desc(fn, q, "q", dev), None, None
         require(fn, positions, "positions", "int32", qd.tokens, dev)
         if q_out is None:
@@ -791,6 +793,8 @@ class Rotary:
                 ko = _desc(fn, k_out, "k_out", dev)
         elif k_out is not None:
             raise SiftError(fn, 1, "k_out without k")
+        if given:
+            _overwritten(fn, given)
         st = lib().sift_rotate(qd, kd, positions.data_ptr(), self.struct, back, qo, ko,
                                _stream_ptr(stream))
         if st:
@@ -858,6 +862,16 @@ def _turn_function():
 
         _turn_class = Turn
     return _turn_class
+
+
+def _overwritten(fn, ts):
+    """Tensors that a call is about to write: autograd sees that they change, as from its
+    own operations in place, and none may stand in a graph that the call would not be in."""
+    torch = _torch()
+    if torch.is_grad_enabled() and any(x.requires_grad for x in ts):
+        raise SiftError(fn, 4, "an output that requires a gradient, where none is recorded")
+    for x in ts:
+        torch.autograd.graph.increment_version(x)
 
 
 def _current(fn, device):

@@ -50,7 +50,8 @@ class PrefillLayer:
         k = (h @ self.Wk.T).view(n, self.hkv, self.d)
         v = (h @ self.Wv.T).view(n, self.hkv, self.d)
         if isinstance(self.inv_freq, Rotary):
-            self.inv_freq.rotate_(q, k, positions)
+            with _torch().no_grad():   # (the attention records no gradient either)
+                self.inv_freq.rotate_(q, k, positions)
         else:
             rope_(q, k, positions, self.inv_freq)
         a = plan.run(q, k, v, la, ca)
