@@ -845,13 +845,13 @@ def _turn_function():
         class Turn(torch.autograd.Function):
             @staticmethod
             def forward(ctx, q, k, positions, rotary, back):
-                ctx.save_for_backward(positions)
+                ctx.save_for_backward(positions, rotary.inv_freq)   # changed since: an error
                 ctx.rotary, ctx.back, ctx.pair = rotary, back, k is not None
                 return rotary.rotate(q, k, positions, back)
 
             @staticmethod
             def backward(ctx, dq, dk):
-                positions, = ctx.saved_tensors
+                positions, _ = ctx.saved_tensors
                 # (a gradient may be a view, or expanded)
                 dq, dk = dq.contiguous(), dk.contiguous() if ctx.pair else None
                 if torch.is_grad_enabled():   # a gradient of the gradient may be asked for

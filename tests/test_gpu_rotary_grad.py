@@ -56,6 +56,15 @@ def test_a_tensor_saved_for_a_gradient_and_then_turned():
         y.backward()
 
 
+def test_a_table_changed_between_a_call_and_its_gradient():
+    q, k, pos, r = inputs()
+    q.requires_grad_()
+    out, _ = r(q, k, pos)
+    r.inv_freq.mul_(2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
 def test_in_inference_mode():
     q, k, pos, r = inputs()
     want = r.rotate(q, k, pos)
