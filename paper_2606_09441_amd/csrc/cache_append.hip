@@ -294,9 +294,7 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     }
     const int64_t sc = static_cast<int64_t>(page) * a.hkv + h;
     const bool begun = lo > 0;
-    // (as the attention takes them: what the page holds stays what it was read as)
-    const float old_k = begun ? usable_scale(p.k_scales[sc]) : 0.f;
-    const float old_v = begun ? usable_scale(p.v_scales[sc]) : 0.f;
+    float old_k = begun ? p.k_scales[sc] : 0.f, old_v = begun ? p.v_scales[sc] : 0.f;
 
     // this lane's frequencies, for all its rows
     double freq[8] = {};
@@ -366,6 +364,10 @@ __global__ __launch_bounds__(256) void append_codes_kernel(CacheAppendArgs p) {
     for (int w = 0; w < waves; ++w) {
       mk = fmaxf(mk, part[0][w]);
       mv = fmaxf(mv, part[1][w]);
+    }
+    if (begun) {  // as the attention takes them: what the page holds stays what it was read as
+      old_k = usable_scale(old_k);
+      old_v = usable_scale(old_v);
     }
     const float new_k = fmaxf(power_from(old_k), scale_for(mk));
     const float new_v = fmaxf(power_from(old_v), scale_for(mv));
