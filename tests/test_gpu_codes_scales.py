@@ -26,7 +26,7 @@ UNITS = {"narrow": (512, 1, 1), "wide": (64, 32, 32)}
 class Shared:
     """n slots of dims 0 k0 [n] and codes v [n, D], with scales for each page."""
 
-    def __init__(self, units, page, k0, v, k_scale, v_scale):
+    def __init__(self, units, page, k0, v, k_scale, v_scale, q=Q):
         from paper_2606_09441_amd import Cache, CachePages
         self.B, self.new, self.hq = UNITS[units]
         dev, n = device(), len(k0)
@@ -36,7 +36,7 @@ class Shared:
         k[:n, 0] = k0
         codes = np.zeros((pages * page, D), np.float32)
         codes[:n] = v
-        self.k0, self.v_scale = np.asarray(k0, np.float64), v_scale
+        self.k0, self.q = np.asarray(k0, np.float64), q
         self.v = np.asarray(v, np.float64) * np.repeat(np.asarray(v_scale, np.float64), page)[:n, None]
         self.scales = [f32(x).view(pages, 1) for x in (k_scale, v_scale)]
         per_row = self.scales[0].repeat_interleave(page, 0)
@@ -53,7 +53,7 @@ class Shared:
         """(out, lse) of a sequence, on the host; `own`: the new tokens' values."""
         rows, dev = self.B * self.new, device()
         q = torch.zeros(rows, self.hq, D, dtype=torch.bfloat16, device=dev)
-        q[..., 0] = Q
+        q[..., 0] = self.q
         k_new = torch.zeros(rows, 1, D, dtype=torch.bfloat16, device=dev)
         mask = torch.tensor([1 << i for i in range(self.new)] * self.B, device=dev).view(rows, 1)
         lse = torch.full((rows, self.hq), 7.0, device=dev)
@@ -69,7 +69,7 @@ class Shared:
     def exact(self, own, cap=0.0, slopes=None):
         """(out, lse, sum w |v|) in 64 bits, [new, hq, ..]."""
         n, i = len(self.k0), np.arange(self.new)
-        s = np.concatenate([self.k0, [0.0]]) * (Q / 8)
+        s = np.concatenate([self.k0, [0.0]]) * (self.q / 8)
         if cap:
             s = cap * np.tanh(s / cap)
         s = np.broadcast_to(s, (self.new, self.hq, n + 1)).copy()
@@ -138,6 +138,32 @@ def test_values_at_the_ends_of_the_range(units, n, scale, score, page):
     out, lse = x.attention(0.0, **kw)
     e = float((np.abs(out - ref) / (np.abs(ref) * 2.0 ** -8 + size * (2.0 ** -7 + 2e-5))).max())
     say(f"[scales] {units} {page} {score} {scale:.3g}: {e:.2f} of the bound, lse "
+        f"{max_abs(lse, ref_lse):.2e}")
+    assert max_abs(lse, ref_lse) <= LSE_TOL
+    assert e <= 1
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("score", ["plain", "cap", "bias"])
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1.5 * 2.0 ** -99, 2.0 ** 100, 2.0 ** 120])
+@pytest.mark.parametrize("units,n", [("narrow", 300), ("wide", 1030)])
+def test_keys_at_the_ends_of_the_range(units, n, scale, score, page):
+    """The same for K: queries as small as the keys are large leave the scores what they
+    are, and the bounds with them."""
+    rng = np.random.default_rng(6)
+    k0 = np.where(np.arange(n) < 128, 0.0, rng.choice([2.0, 5.0, -7.0], n))
+    v = rng.integers(-7, 8, (n, D)) / 4.0
+    pages = -(-n // page)
+    x = Shared(units, page, k0 * scale, v, np.full(pages, scale), np.ones(pages),
+               Q / 2.0 ** np.floor(np.log2(scale)))
+    kw = {"cap": dict(cap=30.0), "bias": dict(slopes=np.full(x.hq, 2.0 ** -10, np.float32)),
+          "plain": {}}[score]
+    ref, ref_lse, size = x.exact(0.0, **kw)
+    if score == "bias":
+        kw = dict(slopes=torch.from_numpy(kw["slopes"]).to(device()))
+    out, lse = x.attention(0.0, **kw)
+    e = float((np.abs(out - ref) / (np.abs(ref) * 2.0 ** -8 + size * (2.0 ** -7 + 2e-5))).max())
+    say(f"[scales] {units} {page} {score} K {scale:.3g}: {e:.2f} of the bound, lse "
         f"{max_abs(lse, ref_lse):.2e}")
     assert max_abs(lse, ref_lse) <= LSE_TOL
     assert e <= 1
