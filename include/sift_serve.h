@@ -75,8 +75,8 @@ sift_status sift_plan_dense(sift_plan* plan, const sift_tensor* q, const sift_te
  * Rotary positions.  The first rot_dim dims of a head turn in pairs (x, y) by the
  * angle position * inv_freq[i], i < rot_dim / 2:
  *   x' = magnitude * (x cos - y sin),  y' = magnitude * (y cos + x sin)
- * the others stay.  The angle is the product of the integer and the float, reduced
- * without loss (sift_rope rounds that product to fp32).
+ * the others stay.  The angle is formed and reduced to a turn in 64 bits, off by less than
+ * 2^-51 of itself: 2e-7 of a turn at 2^31 radians (sift_rope forms it in fp32).
  *   inv_freq     device float [rot_dim / 2]: any table, so that any scaling of the
  *                frequencies for long contexts is one
  *   rot_dim      even, 2 .. D
@@ -175,7 +175,8 @@ sift_status sift_cache_destroy(sift_cache* cache);
  *   q, out       [rows][Hq][D];  k_new, v_new: [rows][Hkv][D], the new tokens'
  *                own keys, which the cache does not hold yet.  All tensors and
  *                the pools SIFT_BF16 or all SIFT_F32, 16-byte aligned; with pools of
- *                SIFT_E4M3 all others SIFT_BF16.
+ *                SIFT_E4M3 all others SIFT_BF16.  But for fp32 the weights are rounded to
+ *                bf16 for the product with V, and divided by the sum of the rounded ones.
  *   tree_mask    device uint64 [rows][mask_words], mask_words >=
  *                ceil(max_rows / 64): bit j % 64 of word j / 64 says whether the
  *                row sees new token j of its sequence (its ancestors and

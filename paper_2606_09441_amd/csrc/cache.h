@@ -168,7 +168,8 @@ struct Wide {    // a 64-key tile a step
 // first tiles' way, the merge of its wavefronts.  Counted in the split, the workgroups with
 // several short sequences do not end last: us of 32 sequences of 200 to 16640 slots with
 // none / one / two / four 80 / 68 / 68 / 68.4, of 16 such 42 / 36 / 34 / 36, of 20 of 30 to
-// 30000 66 / 50 / 46 / -, of 32 of 300 20 / 18 / 21 / 21.5.
+// 30000 66 / 50 / 46 / -, of 32 of 300 20 / 18 / 21 / 21.5 (so batches of short sequences
+// lose a little: two are for the longer calls).
 struct NarrowCodes : Narrow {
   static constexpr int kLead = 2;
 };

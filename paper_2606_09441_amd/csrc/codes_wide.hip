@@ -2,15 +2,18 @@
 // a (sequence, kv head), as in cache_wide.hip, over the pipeline of codes_pipe.h.  The new
 // tokens' own keys, bf16 tiles, are taken last and one at a time.
 //
-// 64 tokens, 48/8 heads, D = 128 over 66048 slots: 150 us of the call with its merge (bf16
-// 152), 690 TFLOP/s.  The vector unit issues in 58% of the SIMDs' cycles (12 operations a
-// matrix instruction, four of them conversions), the matrix cores are busy in 35%, one or
-// the other in 72%.  Twice the slots cost 116 us more: 34 are a workgroup's start and end
+// 64 tokens, 48/8 heads, D = 128 over 66048 slots: 153 us of the call with its merge, 680
+// TFLOP/s (another card, both caches in turn: 157, bf16 161).  The vector unit issues in 58%
+// of the SIMDs' cycles (12 operations a matrix instruction, four of them conversions), the
+// matrix cores are busy in 35%, one or the other in 72%.  Twice the slots cost 116 us more: 34 are a workgroup's start and end
 // and the merge of what they share, 33 MB of sums written and read again.  In the others
 // the vector unit is what counts: with the exponentials' longer issue (four times the
 // others') its operations fill nine tenths of the cycles, and one workgroup on a CU does as
 // many tiles as two.  Kernels of their own for tiles in one page keep a scale where four
-// would be, and spill less (25 registers a lane, not 35): 150 us, not 162.
+// would be, and spill less (27 registers a lane, not 39): 158 us, not 170 in one run.
+// Capped scores take 186 and biased ones 203: 18.6 vector operations a matrix instruction
+// capped, not 12.2, among them K's scale times every score, which plain ones have in their
+// factor.
 
 #include "cache.h"
 #include "codes_pipe.h"

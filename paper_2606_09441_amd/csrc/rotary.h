@@ -50,7 +50,8 @@ __device__ __forceinline__ void unit(double turns, float& c, float& s) {
   }
 }
 
-// Turns a position that frequency i makes.
+// Turns a position that frequency i makes: the constant and the product are each off by
+// 2^-53 of themselves at most, as is a position's product.
 __device__ __forceinline__ double frequency(const RotaryArgs& r, int i) {
   return static_cast<double>(r.inv_freq[i]) * 0.15915494309189535;  // 1 / (2 pi)
 }
